@@ -599,6 +599,130 @@ gleam_status gleam_remap_export(const gleam_remap* m, uint64_t* d_start, uint64_
                                 uint64_t* d_count, void* stream);
 
 /*
+ * A paged key/value cache. Identifiers of blocks of prompt tokens (gleam_cache_lookup, whose
+ * values may be page numbers) say which pages already hold a prompt's keys and values; the
+ * calls below fill such pages and read them. They are for serving: nothing here has a gradient.
+ *
+ * Keys and values live in n_pages pages of page_tokens places each. Place i of page p holds
+ * head_dim elements of head h at element offset p * stride[0] + i * stride[1] + h * stride[2]
+ * of d_k (d_v), so that [page, place, head] and [page, head, place] layouts are both allowed.
+ *   dtype        GLEAM_FP16 or GLEAM_BF16, of the cache and of what is appended or asked
+ *   page_tokens  a power of two, 16 to 4096
+ *   head_dim     64, 128 or 256
+ *   kv_heads     1 to 65535
+ * d_k and d_v are 16-byte aligned, strides multiples of 8 elements.
+ */
+enum { GLEAM_FP16 = 0, GLEAM_BF16 = 1 };
+typedef struct gleam_kv_pages {
+  void* d_k;
+  void* d_v;
+  uint64_t n_pages;
+  uint32_t page_tokens, kv_heads, head_dim, dtype;
+  int64_t k_stride[3], v_stride[3];
+} gleam_kv_pages;
+
+/*
+ * gleam_rotary_table: d_table (device float[positions][rot_dim]) = for position p the cosines of
+ * p * f_i, i < rot_dim / 2, then their sines, all times `magnitude`. f_i = base^(-2 i / rot_dim),
+ * and for contexts longer than the model was trained on ("factor" times original_positions):
+ *   original_positions = 0   f_i / factor
+ *   otherwise                f_i * (keep + (1 - keep) / factor), keep = clamp((turns - slow) /
+ *                            (fast - slow), 0, 1), turns = original_positions * f_i / (2 pi):
+ *                            dimensions that turn more than `fast` times are kept, those that
+ *                            turn less than `slow` times are stretched (the by-parts
+ *                            interpolation published as YaRN)
+ * Computed in 64 bits, rounded once. rot_dim: a multiple of 2, up to 65536; positions below 2^31.
+ * Errors: GLEAM_E_INVALID, GLEAM_E_HIP.
+ */
+gleam_status gleam_rotary_table(float* d_table, uint64_t positions, uint32_t rot_dim, double base, double factor,
+                                double original_positions, double slow, double fast, double magnitude,
+                                void* stream);
+
+/*
+ * gleam_kv_append: keys and values of n_tokens new tokens go into the cache, keys rotated by
+ * their tokens' positions on the way, and queries (if any) rotated in the same pass. For each
+ * token t and head, in 32 bits with one rounding at the end:
+ *   x <- x * weight / sqrt(mean(x^2) + eps)      where a weight is given (q_heads' and keys' own)
+ *   (a, b) <- (a c - b s, b c + a s)             for the pairs (i, i + rot_dim / 2), or with
+ *                                                `interleaved` (2 i, 2 i + 1), c and s the
+ *                                                table's for d_positions[t]
+ * d_slots[t] = page * page_tokens + place is where the token's keys and values go; a slot that
+ * is not in the cache (-1 for padding) stores nothing, its query is rotated all the same. Two
+ * tokens with one slot leave either's keys. A position outside the table gives NaN.
+ *   q, k, v          device, token and head strides in elements (multiples of 8), 16-byte aligned
+ *   d_q, d_q_out     nullable together; d_q_out is [n_tokens][q_heads][head_dim] and may be d_q
+ *                    itself where that is contiguous
+ *   d_q_weight, d_k_weight  nullable, head_dim elements of dtype, 16-byte aligned
+ *   d_rotary         nullable (no rotation): float[rotary_positions][rot_dim], 16-byte aligned;
+ *                    rot_dim a multiple of 16, at most head_dim
+ * Errors: GLEAM_E_INVALID, GLEAM_E_UNSUPPORTED (2^31 tokens or more), GLEAM_E_HIP.
+ */
+typedef struct gleam_append {
+  const void* d_q;
+  const void* d_k;
+  const void* d_v;
+  void* d_q_out;
+  const int64_t* d_slots;
+  const int32_t* d_positions;
+  const float* d_rotary;
+  const void* d_q_weight;
+  const void* d_k_weight;
+  uint64_t n_tokens, rotary_positions;
+  int64_t q_stride[2], k_stride[2], v_stride[2];
+  uint32_t q_heads, rot_dim, interleaved;
+  float eps;
+} gleam_append;
+
+gleam_status gleam_kv_append(const gleam_kv_pages* kv, const gleam_append* a, void* stream);
+
+/*
+ * gleam_prefix_attention: attention of a ragged batch over the cache, where groups of
+ * sequences share a prefix whose keys and values are read and scored once for the group.
+ *
+ * Sequence s has tokens [d_q_first[s], d_q_first[s+1]) of the n_tokens queries (n of them) and
+ * d_own_len[s] keys of its own in the pages d_own_pages[s][...]. Group g is the sequences
+ * [d_group_first[g], d_group_first[g+1]), which all also see the d_prefix_len[g] keys in the
+ * pages d_prefix_pages[g][...]. Token i (of n) of s sees its group's whole prefix and the own
+ * keys j < d_own_len[s] - n + i + 1: its sequence's last n keys are those of the new tokens. For
+ * each token and query head (q_heads / kv_heads of them share a key head, in order):
+ *   score = scale * q.k,  out = sum exp(score) v / sum exp(score),  lse = log sum exp(score)
+ * Scores, maxima, sums and outputs are kept in 32 bits, exp(score - max) is rounded to dtype
+ * for its product with v, and the output once more. A row that sees nothing gets out = 0 and
+ * lse = -infinity. What a row may not see does not reach it, whatever it holds (NaN too).
+ *
+ * Everything with a d_ is device memory and is read when the kernels run, so a captured call
+ * follows changed lengths and pages. Lengths are taken as at least 0 and at most what the
+ * tables' widths hold; d_q_first and d_group_first as non-decreasing within their ranges; keys
+ * in a page that the cache does not have (-1, say) are not seen.
+ *   q                token and head strides in elements (multiples of 8), 16-byte aligned
+ *   own_width, prefix_width   pages in a row of each table (width * page_tokens < 2^31)
+ *   d_group_first, d_prefix_pages, d_prefix_len   may be null where n_groups is 0
+ *   d_out            [n_tokens][q_heads][head_dim] of dtype, 16-byte aligned
+ *   d_lse            nullable float[n_tokens][q_heads]
+ *   d_ws             device, 256-byte aligned, >= gleam_prefix_attention_ws_bytes(kv, b)
+ * Errors: GLEAM_E_INVALID, GLEAM_E_WORKSPACE, GLEAM_E_UNSUPPORTED (n_tokens * q_heads of 2^31
+ * or more, more than 2^20 sequences or groups), GLEAM_E_HIP. gleam_prefix_attention_ws_bytes
+ * returns 0 for arguments the call refuses; it depends on the shapes, not on pointers.
+ */
+typedef struct gleam_prefix_batch {
+  const void* d_q;
+  const int32_t* d_q_first;
+  const int32_t* d_own_pages;
+  const int32_t* d_own_len;
+  const int32_t* d_group_first;
+  const int32_t* d_prefix_pages;
+  const int32_t* d_prefix_len;
+  uint64_t n_tokens, n_seq, n_groups, own_width, prefix_width;
+  int64_t q_stride[2];
+  uint32_t q_heads;
+  float scale;
+} gleam_prefix_batch;
+
+size_t gleam_prefix_attention_ws_bytes(const gleam_kv_pages* kv, const gleam_prefix_batch* b);
+gleam_status gleam_prefix_attention(const gleam_kv_pages* kv, const gleam_prefix_batch* b, void* d_out,
+                                    float* d_lse, void* d_ws, size_t ws_bytes, void* stream);
+
+/*
  * Calibration (a measurement aid, not a step of the path): read `bytes` bytes at d_src
  * (device, 16-byte aligned, bytes a multiple of 16) once, with the fastest plain read
  * pattern measured on MI355X, and XOR into *d_sink (device u64, caller-initialised) the

@@ -48,7 +48,8 @@ EXPORTS = (
     "gleam_remap_update_bytes", "gleam_remap_update", "gleam_remap_translate", "gleam_remap_export",
     "gleam_cache_lookup_noalloc", "gleam_cache_lookup_noalloc_max_keys", "gleam_detect",
     "gleam_detect_ws_init", "gleam_identify_leaves", "gleam_first_writes_ws_bytes", "gleam_first_writes",
-    "gleam_cache_erase_bytes", "gleam_detect_workspace_bytes", "gleam_preload",
+    "gleam_cache_erase_bytes", "gleam_detect_workspace_bytes", "gleam_preload", "gleam_rotary_table",
+    "gleam_kv_append", "gleam_prefix_attention_ws_bytes", "gleam_prefix_attention",
 )
 
 
@@ -64,13 +65,41 @@ class _Batch(ctypes.Structure):
                 ("block_bytes", ctypes.c_uint32)]
 
 
+class _KvPages(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_pages", ctypes.c_uint64),
+                ("page_tokens", ctypes.c_uint32), ("kv_heads", ctypes.c_uint32), ("head_dim", ctypes.c_uint32),
+                ("dtype", ctypes.c_uint32), ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3)]
+
+
+class _Append(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q_out", ctypes.c_void_p),
+                ("slots", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("rotary", ctypes.c_void_p),
+                ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("n_tokens", ctypes.c_uint64),
+                ("rotary_positions", ctypes.c_uint64), ("q_stride", ctypes.c_int64 * 2),
+                ("k_stride", ctypes.c_int64 * 2), ("v_stride", ctypes.c_int64 * 2), ("q_heads", ctypes.c_uint32),
+                ("rot_dim", ctypes.c_uint32), ("interleaved", ctypes.c_uint32), ("eps", ctypes.c_float)]
+
+
+class _PrefixBatch(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("q_first", ctypes.c_void_p), ("own_pages", ctypes.c_void_p),
+                ("own_len", ctypes.c_void_p), ("group_first", ctypes.c_void_p), ("prefix_pages", ctypes.c_void_p),
+                ("prefix_len", ctypes.c_void_p), ("n_tokens", ctypes.c_uint64), ("n_seq", ctypes.c_uint64),
+                ("n_groups", ctypes.c_uint64), ("own_width", ctypes.c_uint64), ("prefix_width", ctypes.c_uint64),
+                ("q_stride", ctypes.c_int64 * 2), ("q_heads", ctypes.c_uint32), ("scale", ctypes.c_float)]
+
+
 def _load() -> ctypes.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"libgleam.so is not built at {LIB_PATH}; run python -m paper_2607_23115_amd.build")
     lib = ctypes.CDLL(LIB_PATH)
     u64, u32, vp, st = ctypes.c_uint64, ctypes.c_uint32, ctypes.c_void_p, ctypes.c_int32
-    sz = ctypes.c_size_t
+    sz, dbl = ctypes.c_size_t, ctypes.c_double
+    kv, batch = ctypes.POINTER(_KvPages), ctypes.POINTER(_PrefixBatch)
     sigs = {
+        "gleam_rotary_table": ([vp, u64, u32, dbl, dbl, dbl, dbl, dbl, dbl, vp], st),
+        "gleam_kv_append": ([kv, ctypes.POINTER(_Append), vp], st),
+        "gleam_prefix_attention_ws_bytes": ([kv, batch], sz),
+        "gleam_prefix_attention": ([kv, batch, vp, vp, vp, sz, vp], st),
         "gleam_batch_geometry": ([vp, u64, u32, vp, vp], st),
         "gleam_fp_chunks": ([ctypes.POINTER(_Batch), vp, vp, vp], st),
         "gleam_cache_bytes": ([u64], sz),
@@ -804,3 +833,191 @@ def records_to_numpy(records: torch.Tensor) -> np.ndarray:
 def as_u64(t: torch.Tensor) -> np.ndarray:
     """Device int64 tensor -> host uint64 array (same bits)."""
     return t.detach().cpu().numpy().view(np.uint64)
+
+
+# --------------------------------------------------------------------------- #
+# A paged key/value cache
+# --------------------------------------------------------------------------- #
+_KV_TYPES = {torch.float16: 0, torch.bfloat16: 1}  # GLEAM_FP16, GLEAM_BF16
+_I32, _F32 = (torch.int32,), (torch.float32,)
+
+
+def _steps(t: torch.Tensor):
+    """Strides in elements of all dimensions but the last; of a dimension of size 1, which
+    nothing is multiplied by, 0."""
+    return tuple(s if n > 1 else 0 for s, n in zip(t.stride()[:-1], t.shape[:-1]))
+
+
+def _heads(t: torch.Tensor, name: str, like: torch.Tensor, heads: int | None = None):
+    """Check [tokens, heads, head_dim] of the cache's type, whose heads are whole rows."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a tensor on the GPU")
+    if t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, the cache on {like.device}")
+    if t.dtype != like.dtype:
+        raise ValueError(f"{name} must be {like.dtype} as the cache is, not {t.dtype}")
+    if t.dim() != 3 or t.shape[2] != like.shape[3] or (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{name} must be [tokens, {heads or 'heads'}, {like.shape[3]}], not {list(t.shape)}")
+    if t.stride(2) != 1:
+        raise ValueError(f"{name} must have its last dimension contiguous")
+    return t
+
+
+def _kv_struct(k_pages: torch.Tensor, v_pages: torch.Tensor) -> _KvPages:
+    for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise ValueError(f"{name} must be a tensor on the GPU")
+        if t.dim() != 4 or t.stride(3) != 1:
+            raise ValueError(f"{name} must be [pages, page_tokens, kv_heads, head_dim], the last contiguous")
+        if t.dtype not in _KV_TYPES:
+            raise ValueError(f"{name} must be torch.float16 or torch.bfloat16, not {t.dtype}")
+    if k_pages.shape != v_pages.shape or k_pages.dtype != v_pages.dtype or k_pages.device != v_pages.device:
+        raise ValueError("k_pages and v_pages differ in shape, type or device")
+    n, page, heads, d = k_pages.shape
+    return _KvPages(k_pages.data_ptr(), v_pages.data_ptr(), n, page, heads, d, _KV_TYPES[k_pages.dtype],
+                    _steps(k_pages), _steps(v_pages))
+
+
+def rotary_table(positions: int, rot_dim: int, base: float = 10000.0, factor: float = 1.0,
+                 original_positions: int = 0, slow: float = 1.0, fast: float = 32.0, magnitude: float = 1.0,
+                 device="cuda", stream=None) -> torch.Tensor:
+    """float32 [positions, rot_dim]: cosines, then sines, of every position's rot_dim / 2 angles.
+
+    factor > 1 stretches the angles for contexts longer than the model was trained on: all of
+    them, or, where original_positions (the trained length) is given, those dimensions that
+    turn fewer than `fast` times over it, fully below `slow`."""
+    if torch.device(device).type != "cuda":
+        raise ValueError("a rotary table lives in GPU memory: device must be a CUDA device")
+    if positions < 0 or rot_dim < 0:
+        raise ValueError("positions and rot_dim must not be negative")
+    with _on_stream(stream, torch.device(device)) as hs:
+        table = torch.empty((positions, rot_dim), dtype=torch.float32, device=device)
+        _check(lib.gleam_rotary_table(_ptr(table), positions, rot_dim, base, factor, original_positions, slow, fast,
+                                      magnitude, hs))
+    return table
+
+
+def kv_append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, slots: torch.Tensor,
+              q: torch.Tensor | None = None, q_out: torch.Tensor | None = None,
+              positions: torch.Tensor | None = None, rotary: torch.Tensor | None = None, interleaved: bool = False,
+              q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, eps: float = 1e-6,
+              stream=None) -> torch.Tensor | None:
+    """Store keys and values of new tokens in the cache, keys normed and rotated on the way;
+    returns the queries normed and rotated the same (None without queries).
+
+    k, v [tokens, kv_heads, head_dim] and q [tokens, q_heads, head_dim] may be strided views (of
+    one product's output, say). k_pages, v_pages: [pages, page_tokens, kv_heads, head_dim], any
+    order in memory of the first three. slots int64: page * page_tokens + place of each token,
+    -1 to store nothing. rotary: rotary_table()'s, with positions int32. q_weight, k_weight
+    [head_dim]: norm each head of q, of k."""
+    kv = _kv_struct(k_pages, v_pages)
+    n, heads = k.shape[0] if isinstance(k, torch.Tensor) and k.dim() else 0, k_pages.shape[2]
+    _heads(k, "k", k_pages, heads)
+    _heads(v, "v", k_pages, heads)
+    if v.shape[0] != n:
+        raise ValueError("k and v differ in tokens")
+    if q is not None:
+        _heads(q, "q", k_pages)
+        if q.shape[0] != n:
+            raise ValueError("q and k differ in tokens")
+    elif q_out is not None or q_weight is not None:
+        raise ValueError("q_out and q_weight need q")
+    _dev(slots, "slots", _U64, n)
+    rot, table = 0, 0
+    if rotary is not None:
+        _dev(rotary, "rotary", _F32)
+        _dev(positions, "positions", _I32, n)
+        if rotary.dim() != 2:
+            raise ValueError("rotary must be [positions, rot_dim]")
+        table, rot = rotary.shape
+    for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        _dev(t, name, (k_pages.dtype,), k_pages.shape[3], optional=True)
+    for t, name in ((slots, "slots"), (rotary, "rotary"), (positions, "positions"), (q_weight, "q_weight"),
+                    (k_weight, "k_weight"), (q_out, "q_out")):
+        if t is not None and t.device != k_pages.device:
+            raise ValueError(f"{name} is on {t.device}, the cache on {k_pages.device}")
+    with _on_stream(stream, k_pages.device) as hs:
+        if q is not None:
+            if q_out is None:
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            elif _dev(q_out, "q_out", (q.dtype,)).shape != q.shape:
+                raise ValueError("q_out and q differ in shape")
+        with_q = q is not None and q.shape[1] > 0
+        args = _Append(_ptr(q) if with_q else None, k.data_ptr(), v.data_ptr(), _ptr(q_out) if with_q else None,
+                       slots.data_ptr(), _ptr(positions), _ptr(rotary), _ptr(q_weight), _ptr(k_weight), n, table,
+                       _steps(q) if with_q else (0, 0), _steps(k), _steps(v), q.shape[1] if with_q else 0, rot,
+                       int(interleaved), eps)
+        _check(lib.gleam_kv_append(ctypes.byref(kv), ctypes.byref(args), hs))
+    return q_out
+
+
+def prefix_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, q_first: torch.Tensor,
+                     own_pages: torch.Tensor, own_len: torch.Tensor, group_first: torch.Tensor | None = None,
+                     prefix_pages: torch.Tensor | None = None, prefix_len: torch.Tensor | None = None,
+                     scale: float | None = None, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                     want_lse: bool = False, ws: torch.Tensor | None = None, stream=None):
+    """Attention of a ragged batch over the paged cache: (out [tokens, q_heads, head_dim], lse
+    float32 [tokens, q_heads] or None).
+
+    q [tokens, q_heads, head_dim]; sequence s has tokens q_first[s] to q_first[s + 1] and
+    own_len[s] keys, the last of them its new tokens', in pages own_pages[s]. Sequences
+    group_first[g] to group_first[g + 1] also see all prefix_len[g] keys in prefix_pages[g],
+    which are read once for the group. All of these are int32 on the GPU, unused places of the
+    page tables -1. scale: head_dim ** -0.5 where none is given. ws: a workspace from
+    prefix_attention_workspace() of these shapes."""
+    kv = _kv_struct(k_pages, v_pages)
+    _heads(q, "q", k_pages)
+    n_seq, n_groups, own_width, prefix_width = own_len.numel(), 0, 0, 0
+    _dev(q_first, "q_first", _I32, n_seq + 1)
+    _dev(own_len, "own_len", _I32)
+    _dev(own_pages, "own_pages", _I32)
+    if own_pages.dim() != 2 or own_pages.shape[0] != n_seq:
+        raise ValueError(f"own_pages must be [{n_seq}, pages], not {list(own_pages.shape)}")
+    own_width = own_pages.shape[1]
+    if group_first is not None or prefix_pages is not None or prefix_len is not None:
+        _dev(prefix_len, "prefix_len", _I32)
+        n_groups = prefix_len.numel()
+        _dev(group_first, "group_first", _I32, n_groups + 1)
+        _dev(prefix_pages, "prefix_pages", _I32)
+        if prefix_pages.dim() != 2 or prefix_pages.shape[0] != n_groups:
+            raise ValueError(f"prefix_pages must be [{n_groups}, pages], not {list(prefix_pages.shape)}")
+        prefix_width = prefix_pages.shape[1]
+    for t, name in ((q_first, "q_first"), (own_pages, "own_pages"), (own_len, "own_len"), (lse, "lse"), (ws, "ws"),
+                    (group_first, "group_first"), (prefix_pages, "prefix_pages"), (prefix_len, "prefix_len"),
+                    (out, "out")):
+        if t is not None and t.device != k_pages.device:
+            raise ValueError(f"{name} is on {t.device}, the cache on {k_pages.device}")
+    tokens, heads, d = q.shape
+    b = _PrefixBatch(q.data_ptr(), q_first.data_ptr(), own_pages.data_ptr(), own_len.data_ptr(), _ptr(group_first),
+                     _ptr(prefix_pages), _ptr(prefix_len), tokens, n_seq, n_groups, own_width, prefix_width,
+                     _steps(q), heads, d ** -0.5 if scale is None else scale)
+    with _on_stream(stream, k_pages.device) as hs:
+        if out is None:
+            out = torch.empty((tokens, heads, d), dtype=q.dtype, device=q.device)
+        elif _dev(out, "out", (q.dtype,)).shape != q.shape:
+            raise ValueError("out and q differ in shape")
+        if lse is None and want_lse:
+            lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device)
+        elif lse is not None and _dev(lse, "lse", _F32).shape != q.shape[:2]:
+            raise ValueError("lse must be [tokens, q_heads]")
+        if ws is None:
+            ws = torch.empty(_attention_ws(kv, b), dtype=torch.uint8, device=q.device)
+        _dev(ws, "ws", _U8)
+        _check(lib.gleam_prefix_attention(ctypes.byref(kv), ctypes.byref(b), out.data_ptr(), _ptr(lse),
+                                          ws.data_ptr(), ws.numel(), hs))
+    return out, lse
+
+
+def _attention_ws(kv: _KvPages, b: _PrefixBatch) -> int:
+    n = int(lib.gleam_prefix_attention_ws_bytes(ctypes.byref(kv), ctypes.byref(b)))
+    if n == 0:
+        raise GleamError(E_INVALID, lib.gleam_last_error().decode())
+    return n
+
+
+def prefix_attention_workspace(k_pages: torch.Tensor, v_pages: torch.Tensor, tokens: int, q_heads: int, n_seq: int,
+                               n_groups: int = 0) -> torch.Tensor:
+    """A workspace for prefix_attention() calls of these shapes on this cache (calls that may
+    overlap need one each)."""
+    b = _PrefixBatch(n_tokens=tokens, n_seq=n_seq, n_groups=n_groups, q_heads=q_heads)
+    return torch.empty(_attention_ws(_kv_struct(k_pages, v_pages), b), dtype=torch.uint8, device=k_pages.device)

@@ -108,7 +108,8 @@ extern "C" gleam_status gleam_preload(void) {
   clear_error();
   hipError_t (*const loads[])() = {preload_fp_chunks, preload_cache,    preload_compact, preload_detect,
                                    preload_identify,  preload_first_write, preload_md5,  preload_lifecycle,
-                                   preload_transfer,  preload_remap,    preload_calib};
+                                   preload_transfer,  preload_remap,    preload_calib,   preload_kv_append,
+                                  preload_prefix_attention};
   for (auto load : loads) {
     const hipError_t e = load();
     if (e != hipSuccess) {

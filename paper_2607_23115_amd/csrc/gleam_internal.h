@@ -100,8 +100,10 @@ hipError_t preload_detect();
 hipError_t preload_first_write();
 hipError_t preload_fp_chunks();
 hipError_t preload_identify();
+hipError_t preload_kv_append();
 hipError_t preload_lifecycle();
 hipError_t preload_md5();
+hipError_t preload_prefix_attention();
 hipError_t preload_remap();
 hipError_t preload_transfer();
 

@@ -1,0 +1,816 @@
+// Attention of a ragged batch over a paged key/value cache, in which groups of sequences share a
+// prefix: prefix keys and values are read and scored once for all rows of a group.
+//
+// A row's result over any set of keys is (m, l, o): m the largest score, l = sum exp(score - m),
+// o = sum exp(score - m) v. Two sets join as m = max, l and o weighted by exp(their m - m), so
+// keys can be walked in any order and pieces: one pass over the keys with running m, l, o; long
+// walks cut into chunks for several workgroups; the shared prefix and a sequence's own keys as
+// separate pieces of one row. Scores are kept times log2(e), so that every exponential is one
+// hardware exp2.
+//
+// Three launches: plan_kernel cuts the lengths it finds on the device into units
+// (prefix_plan.h), attend_kernel takes a unit per workgroup, join_kernel joins the pieces.
+//
+// A unit is 16 rows of one key head. Four waves take turns at 32 keys each, straight from memory
+// to registers in the layouts of v_mfma_f32_16x16x32: nothing is exchanged between lanes but the
+// maximum over a wave's keys.
+//   scores  S^T = K Q^T, a product for each 16 keys. A lane holds, as K's row operand, 8 dims of
+//           key (lane % 16), and gets the scores of row (lane % 16) with keys 4 g .. 4 g + 3, g =
+//           lane / 16.
+//   output  O^T = V^T P^T over 32 keys at once. The order of keys within a product is free: taking
+//           keys {4g..4g+3} of the first 16 and of the second 16 as the eight that lane group g
+//           brings makes its own scores, once exponentiated, P's operand as they are. As V's
+//           operand a lane holds those 8 keys' dims (lane % 16) * D/16 .. + D/16, loaded row by
+//           row and transposed within the lane.
+// With few rows this is bound by reading the keys and values once.
+
+#include "kv_pages.h"
+#include "launch_shape.h"
+#include "prefix_plan.h"
+
+namespace gleam {
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kPlanThreads = 1024;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr uint64_t kMostSeq = 1ull << 20;
+
+struct Item {
+  uint32_t token_first, tokens;  // rows: tokens * ratio
+  uint32_t prefix_row, prefix_keys;  // the shared pages' row of the table and how many keys; 0: none
+  uint32_t own_row, own_keys;        // the sequence's own
+  uint32_t chunks, per;              // chunks and steps of each; 0: no keys at all
+  uint32_t unit_first, part_first;   // the first unit, the first row of partial results
+  uint32_t partial;                  // results go to the workspace
+  uint32_t pad[5];
+};
+
+struct PlanHeader {
+  uint32_t units;
+  uint32_t joins;  // some row needs join_kernel
+};
+
+struct Ws {  // device addresses within the workspace
+  PlanHeader* head;
+  int32_t* q_first;      // [n_seq + 1] as used: clamped, non-decreasing
+  int32_t* group_first;  // [n_groups + 1]
+  int32_t* seq_group;    // [n_seq], -1: none
+  uint32_t* unit_first;  // [n_groups + n_seq + 1]
+  Item* items;           // groups, then sequences
+  float* part_o;         // [partials][head_dim]
+  float* part_ml;        // [partials][2]: m (log2), l
+  size_t bytes;
+};
+
+struct AttendArgs {
+  const uint8_t* q;
+  int64_t q_token, q_head;  // bytes
+  const uint8_t* k;
+  const uint8_t* v;
+  int64_t k_page, k_place, k_head, v_page, v_place, v_head;  // bytes
+  const int32_t* q_first;
+  const int32_t* own_pages;
+  const int32_t* own_len;
+  const int32_t* group_first;
+  const int32_t* prefix_pages;
+  const int32_t* prefix_len;
+  uint32_t n_tokens, n_seq, n_groups, own_width, prefix_width;
+  uint32_t q_heads, kv_heads, ratio, page_log2, n_pages, target;
+  float scale_log2;
+  uint8_t* out;
+  float* lse;
+  Ws ws;
+};
+
+Ws ws_at(uint8_t* base, const PlanShape& s, uint32_t head_dim) {
+  Ws w{};
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    uint8_t* p = base + at;
+    at += (bytes + 255) & ~(size_t)255;
+    return p;
+  };
+  const uint64_t items = s.n_groups + s.n_seq, partials = most_partials(s);
+  w.head = reinterpret_cast<PlanHeader*>(take(sizeof(PlanHeader)));
+  w.q_first = reinterpret_cast<int32_t*>(take((s.n_seq + 1) * 4));
+  w.group_first = reinterpret_cast<int32_t*>(take((s.n_groups + 1) * 4));
+  w.seq_group = reinterpret_cast<int32_t*>(take(s.n_seq * 4));
+  w.unit_first = reinterpret_cast<uint32_t*>(take((items + 1) * 4));
+  w.items = reinterpret_cast<Item*>(take(items * sizeof(Item)));
+  w.part_o = reinterpret_cast<float*>(take(partials * head_dim * 4));
+  w.part_ml = reinterpret_cast<float*>(take(partials * 8));
+  w.bytes = at;
+  return w;
+}
+
+// --------------------------------------------------------------------------------------- //
+// plan
+// --------------------------------------------------------------------------------------- //
+struct SumOp {
+  template <class V> __device__ V operator()(V a, V b) const { return a + b; }
+};
+struct MaxOp {
+  template <class V> __device__ V operator()(V a, V b) const { return a > b ? a : b; }
+};
+
+// Inclusive scan over the workgroup; every thread calls it. `total` gets the last value.
+template <class V, class Op>
+__device__ V block_scan(V v, V* lds, V* total, Op op) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const V u = __shfl_up(v, o, 64);
+    if (lane >= o) v = op(u, v);
+  }
+  if (lane == 63) lds[wave] = v;
+  __syncthreads();
+  V all = lds[0];
+  for (int w = 1; w < kPlanThreads / 64; ++w) {
+    if (w == wave) v = op(all, v);
+    all = op(all, lds[w]);
+  }
+  *total = all;
+  __syncthreads();
+  return v;
+}
+
+// src[0..n] as non-decreasing values within [0, most], into dst.
+__device__ void tidy_offsets(const int32_t* src, int32_t* dst, uint32_t n, int32_t most, int32_t* lds) {
+  int32_t carry = 0;
+  for (uint32_t i0 = 0; i0 <= n; i0 += kPlanThreads) {
+    const uint32_t i = i0 + threadIdx.x;
+    int32_t v = i <= n ? src[i] : 0;
+    v = v < 0 ? 0 : v > most ? most : v;
+    int32_t total;
+    v = block_scan(v, lds, &total, MaxOp());
+    if (i <= n) dst[i] = v > carry ? v : carry;
+    carry = carry > total ? carry : total;
+  }
+}
+
+__device__ uint32_t clamp_keys(int32_t n, uint32_t width, uint32_t page_log2) {
+  const uint32_t most = width << page_log2;
+  return n < 0 ? 0 : (uint32_t)n > most ? most : (uint32_t)n;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a) {
+  __shared__ uint64_t lds[kPlanThreads / 64];
+  int32_t* lds32 = reinterpret_cast<int32_t*>(lds);
+  const Ws& w = a.ws;
+  const uint32_t n_items = a.n_groups + a.n_seq;
+  if (a.n_seq == 0) {  // no sequence covers any token
+    if (threadIdx.x == 0) {
+      w.head->units = 0;
+      w.head->joins = 1;
+    }
+    return;
+  }
+  tidy_offsets(a.q_first, w.q_first, a.n_seq, (int32_t)a.n_tokens, lds32);
+  for (uint32_t s = threadIdx.x; s < a.n_seq; s += kPlanThreads) w.seq_group[s] = -1;
+  __syncthreads();
+  if (a.n_groups) {
+    tidy_offsets(a.group_first, w.group_first, a.n_groups, (int32_t)a.n_seq, lds32);
+    __syncthreads();
+    // the last group that starts at or before the sequence, if it has not ended there
+    const int32_t from = w.group_first[0], to = w.group_first[a.n_groups];
+    for (uint32_t s = threadIdx.x; s < a.n_seq; s += kPlanThreads) {
+      if ((int32_t)s < from || (int32_t)s >= to) continue;
+      uint32_t lo = 0, hi = a.n_groups;  // group_first[lo] <= s < group_first[hi]
+      while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (w.group_first[mid] <= (int32_t)s) lo = mid;
+        else hi = mid;
+      }
+      w.seq_group[s] = (int32_t)lo;
+    }
+  }
+  __syncthreads();
+
+  // the items without their cuts, and the cost of all
+  uint64_t cost = 0;
+  uint32_t empty_rows = w.q_first[0] > 0 || w.q_first[a.n_seq] < (int32_t)a.n_tokens;
+  for (uint32_t i = threadIdx.x; i < n_items; i += kPlanThreads) {
+    Item it{};
+    if (i < a.n_groups) {
+      const int32_t s0 = w.group_first[i], s1 = w.group_first[i + 1];
+      it.token_first = (uint32_t)w.q_first[s0];
+      it.tokens = (uint32_t)w.q_first[s1] - it.token_first;
+      it.prefix_row = i;
+      if (!joint_group((uint64_t)it.tokens * a.ratio, (uint64_t)(s1 - s0)))
+        it.prefix_keys = clamp_keys(a.prefix_len[i], a.prefix_width, a.page_log2);
+      it.partial = 1;
+    } else {
+      const uint32_t s = i - a.n_groups;
+      it.token_first = (uint32_t)w.q_first[s];
+      it.tokens = (uint32_t)w.q_first[s + 1] - it.token_first;
+      it.own_row = s;
+      it.own_keys = clamp_keys(a.own_len[s], a.own_width, a.page_log2);
+      const int32_t g = w.seq_group[s];
+      if (g >= 0) {
+        const uint32_t keys = clamp_keys(a.prefix_len[g], a.prefix_width, a.page_log2);
+        const int32_t s0 = w.group_first[g], s1 = w.group_first[g + 1];
+        const uint64_t rows = (uint64_t)(w.q_first[s1] - w.q_first[s0]) * a.ratio;
+        if (joint_group(rows, (uint64_t)(s1 - s0))) {
+          it.prefix_row = (uint32_t)g;
+          it.prefix_keys = keys;
+        } else {
+          it.partial = keys > 0;
+        }
+      }
+    }
+    const uint32_t steps = it.tokens ? steps_of(it.prefix_keys) + steps_of(it.own_keys) : 0;
+    cost += item_cost(it.tokens * a.ratio, steps) * a.kv_heads;
+    if (i >= a.n_groups && it.tokens && steps == 0) empty_rows = 1;
+    w.items[i] = it;
+  }
+  uint64_t all_cost;
+  block_scan(cost, lds, &all_cost, SumOp());
+
+  // chunks, units and partial rows
+  uint32_t units = 0, joins = empty_rows;
+  uint64_t parts = 0;
+  for (uint32_t i0 = 0; i0 < n_items; i0 += kPlanThreads) {
+    const uint32_t i = i0 + threadIdx.x;
+    Item it{};
+    if (i < n_items) it = w.items[i];
+    const uint32_t steps = it.tokens ? steps_of(it.prefix_keys) + steps_of(it.own_keys) : 0;
+    const Cut cut = cut_steps(steps, chunk_steps(it.tokens * a.ratio, all_cost, a.target));
+    it.chunks = cut.chunks;
+    it.per = cut.per;
+    if (cut.chunks > 1) it.partial = 1;
+    const uint32_t n_units = tiles_of(it.tokens * a.ratio) * a.kv_heads * cut.chunks;
+    const uint64_t n_parts = it.partial ? (uint64_t)it.tokens * a.q_heads * cut.chunks : 0;
+    uint32_t unit_total;
+    uint64_t part_total;
+    const uint32_t unit_end = block_scan(n_units, reinterpret_cast<uint32_t*>(lds), &unit_total, SumOp());
+    const uint64_t part_end = block_scan(n_parts, lds, &part_total, SumOp());
+    if (i < n_items) {
+      it.unit_first = units + unit_end - n_units;
+      it.part_first = (uint32_t)(parts + part_end - n_parts);
+      w.items[i] = it;
+      w.unit_first[i] = it.unit_first;
+    }
+    joins |= n_parts > 0;
+    units += unit_total;
+    parts += part_total;
+  }
+  joins = __syncthreads_or((int)joins);
+  if (threadIdx.x == 0) {
+    w.unit_first[n_items] = units;
+    w.head->units = units;
+    w.head->joins = joins;
+  }
+}
+
+// The last i of [0, n) with first[i] <= x, found by a wave: 64 probes a round. first is
+// non-decreasing and first[0] <= x; x is the same in all lanes.
+template <class V>
+__device__ uint32_t wave_search(const V* first, uint32_t n, V x) {
+  const uint32_t lane = threadIdx.x & 63;
+  uint32_t lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const uint32_t stride = (hi - lo + 63) / 64;
+    const uint32_t at = lo + lane * stride;
+    const uint64_t le = __ballot(at < hi && first[at < hi ? at : lo] <= x);
+    const uint32_t last = 63 - __clzll((long long)le);
+    const uint32_t from = lo + last * stride;
+    const uint32_t to = from + stride;
+    lo = from;
+    hi = to < hi ? to : hi;
+  }
+  return lo;
+}
+
+// --------------------------------------------------------------------------------------- //
+// attend
+// --------------------------------------------------------------------------------------- //
+template <class T> struct Mfma;
+template <> struct Mfma<Fp16> {
+  static __device__ f32x4 run(f16x8 a, f16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+  }
+};
+template <> struct Mfma<Bf16> {
+  static __device__ f32x4 run(bf16x8 a, bf16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+};
+
+union Pack8 {
+  u32x4v u;
+  f16x8 h;
+  bf16x8 b;
+};
+__device__ inline void put(Pack8& p, int i, float x, Fp16) { p.h[i] = (_Float16)x; }
+__device__ inline void put(Pack8& p, int i, float x, Bf16) { p.b[i] = (__bf16)x; }
+__device__ inline f16x8 get(const Pack8& p, Fp16) { return p.h; }
+__device__ inline bf16x8 get(const Pack8& p, Bf16) { return p.b; }
+
+// Of two 16-bit values in a dword, those that are infinite or NaN are cleared, and marked with a
+// 1.0 in `up` (+infinity, NaN) and `down` (-infinity, NaN).
+template <class T>
+__device__ inline uint32_t split_special(uint32_t x, uint32_t* up, uint32_t* down) {
+  uint32_t keep = 0, u = 0, d = 0;
+#pragma unroll
+  for (int i = 0; i < 32; i += 16) {
+    const uint32_t b = (x >> i) & 0xffffu;
+    if ((b & T::kExp) != T::kExp) {
+      keep |= b << i;
+    } else {
+      const bool nan = (b & 0x7fffu) != T::kExp;
+      if (nan || !(b & 0x8000u)) u |= T::kOne << i;
+      if (nan || (b & 0x8000u)) d |= T::kOne << i;
+    }
+  }
+  *up = u;
+  *down = d;
+  return keep;
+}
+template <class T>
+__device__ inline bool has_special(uint32_t x) {
+  return (x & T::kExp) == T::kExp || ((x >> 16) & T::kExp) == T::kExp;
+}
+
+// Where 16 keys from `key` on (a multiple of 16, so within a page) are.
+struct Keys16 {
+  const uint8_t* k;
+  const uint8_t* v;
+  uint32_t n;  // how many of them exist
+};
+__device__ inline Keys16 keys16(const AttendArgs& a, const int32_t* pages, uint32_t key, uint32_t keys, uint32_t head) {
+  Keys16 t{a.k, a.v, 0};
+  if (key >= keys) return t;
+  const uint32_t page = (uint32_t)pages[key >> a.page_log2];
+  if (page >= a.n_pages) return t;
+  const uint32_t place = key & ((1u << a.page_log2) - 1);
+  t.k = a.k + (int64_t)page * a.k_page + (int64_t)place * a.k_place + (int64_t)head * a.k_head;
+  t.v = a.v + (int64_t)page * a.v_page + (int64_t)place * a.v_place + (int64_t)head * a.v_head;
+  t.n = keys - key < 16 ? keys - key : 16;
+  return t;
+}
+
+template <class T, int D>
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(AttendArgs a) {
+  typedef typename T::scalar scalar;
+  constexpr int kDims = D / 16;       // dims a lane brings of a value row
+  constexpr int kWords = kDims / 2;   // as dwords
+  constexpr int kKMfma = D / 32;      // products over a key's dims
+  constexpr int kPad = D + 4;         // row of the workgroup's partial outputs in LDS
+  __shared__ __attribute__((aligned(16))) float lds_o[kWaves][kSmallRows][kPad];
+  __shared__ float lds_m[kWaves][kSmallRows], lds_l[kWaves][kSmallRows];
+
+  const Ws& w = a.ws;
+  if (blockIdx.x >= w.head->units) return;
+  const uint32_t n_items = a.n_groups + a.n_seq;
+  const uint32_t at = __builtin_amdgcn_readfirstlane((int)wave_search<uint32_t>(w.unit_first, n_items, blockIdx.x));
+  const Item it = w.items[at];
+  const uint32_t rows = it.tokens * a.ratio;
+  uint32_t u = blockIdx.x - it.unit_first;
+  const uint32_t head = u % a.kv_heads;
+  u /= a.kv_heads;
+  const uint32_t chunk = u % it.chunks, tile = u / it.chunks;
+
+  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const uint32_t n = lane & 15, g = lane >> 4;
+  const uint32_t row = tile * kSmallRows + n;
+  const bool row_live = row < rows;
+  const uint32_t token = it.token_first + (row_live ? row / a.ratio : 0);
+  const uint32_t q_head = head * a.ratio + (row_live ? row % a.ratio : 0);
+
+  // keys of the sequence's own that the row sees; the fewest of the tile's rows
+  const int64_t behind = (int64_t)it.own_keys - it.tokens + 1;
+  const int64_t sees = behind + (row_live ? row / a.ratio : 0);
+  const uint32_t own_seen = sees < 0 ? 0 : (uint32_t)sees;
+  const int64_t fewest = behind + tile * kSmallRows / a.ratio;
+  const uint32_t own_least = fewest < 0 ? 0 : (uint32_t)fewest;
+  uint32_t last_row = tile * kSmallRows + kSmallRows - 1;
+  if (last_row >= rows) last_row = rows - 1;
+  const int64_t furthest = behind + last_row / a.ratio;
+  const uint32_t own_most = furthest < 0 ? 0 : furthest > it.own_keys ? it.own_keys : (uint32_t)furthest;
+
+  Pack8 q[kKMfma];
+#pragma unroll
+  for (int i = 0; i < kKMfma; ++i) {
+    q[i].u = (u32x4v)0u;
+    if (row_live)
+      q[i].u = *reinterpret_cast<const u32x4v*>(a.q + (int64_t)token * a.q_token + (int64_t)q_head * a.q_head +
+                                                (i * 32 + g * 8) * 2);
+  }
+
+  const int32_t* const prefix_pages = a.prefix_pages + (uint64_t)it.prefix_row * a.prefix_width;
+  const int32_t* const own_pages = a.own_pages + (uint64_t)it.own_row * a.own_width;
+  const uint32_t prefix_halves = 2 * steps_of(it.prefix_keys);
+  const uint32_t all_halves = prefix_halves + (own_most + 31) / 32;
+  uint32_t end = 2 * (chunk + 1) * it.per;
+  if (end > all_halves) end = all_halves;
+
+  float m = -INFINITY, l = 0.f;
+  f32x4 o[kDims];
+#pragma unroll
+  for (int j = 0; j < kDims; ++j) o[j] = (f32x4)0.f;
+
+  for (uint32_t half = 2 * chunk * it.per + wave; half < end; half += kWaves) {
+    const bool shared = half < prefix_halves;
+    const uint32_t key = 32 * (shared ? half : half - prefix_halves);
+    const uint32_t keys = shared ? it.prefix_keys : it.own_keys;
+    const int32_t* pages = shared ? prefix_pages : own_pages;
+    const Keys16 t[2] = {keys16(a, pages, key, keys, head), keys16(a, pages, key + 16, keys, head)};
+
+    Pack8 kk[2][kKMfma];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < kKMfma; ++i) {
+        kk[b][i].u = (u32x4v)0u;
+        if (n < t[b].n)
+          kk[b][i].u = *reinterpret_cast<const u32x4v*>(t[b].k + (int64_t)n * a.k_place + (i * 32 + g * 8) * 2);
+      }
+    uint32_t vv[8][kWords];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t r = 4 * g + (e & 3);
+      const bool live = r < t[e >> 2].n;
+      const uint8_t* p = t[e >> 2].v + (int64_t)r * a.v_place + n * (kDims * 2);
+      if constexpr (kDims == 4) {
+        u32x2v x = (u32x2v)0u;
+        if (live) x = *reinterpret_cast<const u32x2v*>(p);
+        vv[e][0] = x[0];
+        vv[e][1] = x[1];
+      } else {
+#pragma unroll
+        for (int c = 0; c < kDims / 8; ++c) {
+          u32x4v x = (u32x4v)0u;
+          if (live) x = *reinterpret_cast<const u32x4v*>(p + 16 * c);
+#pragma unroll
+          for (int d = 0; d < 4; ++d) vv[e][4 * c + d] = x[d];
+        }
+      }
+    }
+
+    f32x4 s[2] = {(f32x4)0.f, (f32x4)0.f};
+#pragma unroll
+    for (int i = 0; i < kKMfma; ++i) {
+      s[0] = Mfma<T>::run(get(kk[0][i], T()), get(q[i], T()), s[0]);
+      s[1] = Mfma<T>::run(get(kk[1][i], T()), get(q[i], T()), s[1]);
+    }
+    // whether some row of the tile must not see some key of these 32
+    const uint32_t least = shared ? it.prefix_keys : own_least;
+    const bool masked = key + 32 > least || t[0].n < 16 || t[1].n < 16;
+    const uint32_t seen = shared ? it.prefix_keys : own_seen;
+    float x[8], top = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x[e] = s[e >> 2][e & 3] * a.scale_log2;
+      if (masked) {
+        const uint32_t r = 4 * g + (e & 3);
+        if (key + (e >> 2) * 16 + r >= seen || r >= t[e >> 2].n) x[e] = -INFINITY;
+      }
+      top = fmaxf(top, x[e]);
+    }
+    top = fmaxf(top, __shfl_xor(top, 16, 64));
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    const float m_new = fmaxf(m, top);
+    const float m_use = m_new == -INFINITY ? 0.f : m_new;  // nothing seen so far: all exponentials are 0
+    const float alpha = __builtin_amdgcn_exp2f(m - m_use);
+    m = m_new;
+    l *= alpha;
+    Pack8 p;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float y = __builtin_amdgcn_exp2f(x[e] - m_use);
+      l += y;
+      put(p, e, y, T());
+    }
+    if (__any(alpha != 1.f)) {
+#pragma unroll
+      for (int j = 0; j < kDims; ++j) o[j] *= alpha;
+    }
+    // An infinite or NaN value would reach rows that may not see it as 0 * infinity: such values
+    // are taken out and added afterwards where they are seen.
+    bool special = false;
+    if (!shared && masked) {
+      bool any = false;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int c = 0; c < kWords; ++c) any |= has_special<T>(vv[e][c]);
+      special = __any(any);
+    }
+    if (!special) {
+#pragma unroll
+      for (int c = 0; c < kWords; ++c) {
+        Pack8 lo, hi;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          lo.u[e] = __builtin_amdgcn_perm(vv[2 * e + 1][c], vv[2 * e][c], 0x05040100u);
+          hi.u[e] = __builtin_amdgcn_perm(vv[2 * e + 1][c], vv[2 * e][c], 0x07060302u);
+        }
+        o[2 * c] = Mfma<T>::run(get(lo, T()), get(p, T()), o[2 * c]);
+        o[2 * c + 1] = Mfma<T>::run(get(hi, T()), get(p, T()), o[2 * c + 1]);
+      }
+    } else {
+      Pack8 sight;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t r = 4 * g + (e & 3);
+        put(sight, e, key + (e >> 2) * 16 + r < seen && r < t[e >> 2].n ? 1.f : 0.f, T());
+      }
+#pragma unroll
+      for (int c = 0; c < kWords; ++c) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          Pack8 plain, up, down;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t both = __builtin_amdgcn_perm(vv[2 * e + 1][c], vv[2 * e][c], h ? 0x07060302u : 0x05040100u);
+            uint32_t pos, neg;
+            plain.u[e] = split_special<T>(both, &pos, &neg);
+            up.u[e] = pos;
+            down.u[e] = neg;
+          }
+          const int j = 2 * c + h;
+          o[j] = Mfma<T>::run(get(plain, T()), get(p, T()), o[j]);
+          const f32x4 pos = Mfma<T>::run(get(up, T()), get(sight, T()), (f32x4)0.f);
+          const f32x4 neg = Mfma<T>::run(get(down, T()), get(sight, T()), (f32x4)0.f);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            if (pos[r] > 0.f) o[j][r] += INFINITY;
+            if (neg[r] > 0.f) o[j][r] -= INFINITY;
+          }
+        }
+      }
+    }
+  }
+
+  // the four waves' results, joined through LDS
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  if (g == 0) {
+    lds_m[wave][n] = m;
+    lds_l[wave][n] = l;
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int j = 0; j < kDims; j += 4) {
+      const f32x4 x = {o[j][r], o[j + 1][r], o[j + 2][r], o[j + 3][r]};
+      *reinterpret_cast<f32x4*>(&lds_o[wave][n][(g * 4 + r) * kDims + j]) = x;
+    }
+  __syncthreads();
+  constexpr int kQuads = D / 4;
+  for (int i = threadIdx.x; i < (int)kSmallRows * kQuads; i += kThreads) {
+    const uint32_t rr = i / kQuads, c = i % kQuads, in = tile * kSmallRows + rr;
+    if (in >= rows) continue;
+    float top = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) top = fmaxf(top, lds_m[v][rr]);
+    float sum = 0.f;
+    f32x4 acc = (f32x4)0.f;
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) {
+      const float lv = lds_l[v][rr];
+      if (lv == 0.f) continue;  // saw nothing
+      const float f = __builtin_amdgcn_exp2f(lds_m[v][rr] - top);
+      sum += f * lv;
+      acc += f * *reinterpret_cast<const f32x4*>(&lds_o[v][rr][4 * c]);
+    }
+    if (it.partial) {
+      const uint64_t at_row = it.part_first + ((uint64_t)head * it.chunks + chunk) * rows + in;
+      *reinterpret_cast<f32x4*>(w.part_o + at_row * D + 4 * c) = acc;
+      if (c == 0) {
+        w.part_ml[2 * at_row] = top;
+        w.part_ml[2 * at_row + 1] = sum;
+      }
+    } else {
+      const uint32_t t = it.token_first + in / a.ratio, h = head * a.ratio + in % a.ratio;
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      scalar y[4];
+#pragma unroll
+      for (int d = 0; d < 4; ++d) y[d] = (scalar)(acc[d] * inv);
+      const uint64_t to = (uint64_t)t * a.q_heads + h;
+      *reinterpret_cast<uint64_t*>(a.out + (to * D + 4 * c) * 2) = *reinterpret_cast<const uint64_t*>(y);
+      if (c == 0 && a.lse) a.lse[to] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    }
+  }
+}
+
+// --------------------------------------------------------------------------------------- //
+// join
+// --------------------------------------------------------------------------------------- //
+// One wave per row: the pieces' maxima and sums are read 64 at a time, then their outputs, each
+// lane D/64 dims. Rows that no piece covers are set to nothing seen.
+template <class T, int D>
+__global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a) {
+  typedef typename T::scalar scalar;
+  constexpr int kDims = D / 64;
+  const Ws& w = a.ws;
+  if (!w.head->joins) return;
+  const uint32_t lane = threadIdx.x & 63;
+  const uint32_t waves = gridDim.x * kWaves, all = a.n_tokens * a.q_heads;
+  for (uint32_t r = blockIdx.x * kWaves + (threadIdx.x >> 6); r < all; r += waves) {
+    const uint32_t token = r / a.q_heads, h = r - token * a.q_heads;
+    const uint32_t head = h / a.ratio;
+    uint32_t first[2] = {0, 0}, count[2] = {0, 0}, step[2] = {0, 0};  // the group's pieces, the sequence's
+    if (a.n_seq > 0 && (int32_t)token >= w.q_first[0] && (int32_t)token < w.q_first[a.n_seq]) {
+      const uint32_t s = wave_search<int32_t>(w.q_first, a.n_seq + 1, (int32_t)token);
+      const Item own = w.items[a.n_groups + s];
+      if (!own.partial && own.chunks) continue;  // written already
+      if (own.partial) {
+        const uint32_t rows = own.tokens * a.ratio;
+        first[1] = own.part_first + head * own.chunks * rows + (token - own.token_first) * a.ratio + h % a.ratio;
+        count[1] = own.chunks;
+        step[1] = rows;
+        const int32_t gr = w.seq_group[s];
+        if (gr >= 0) {
+          const Item pre = w.items[gr];
+          const uint32_t all_rows = pre.tokens * a.ratio;
+          first[0] = pre.part_first + head * pre.chunks * all_rows + (token - pre.token_first) * a.ratio + h % a.ratio;
+          count[0] = pre.chunks;
+          step[0] = all_rows;
+        }
+      }
+    }
+    float m = -INFINITY, l = 0.f;
+    float acc[kDims] = {};
+    const uint32_t pieces = count[0] + count[1];
+    for (uint32_t p0 = 0; p0 < pieces; p0 += 64) {
+      const uint32_t p = p0 + lane;
+      const uint32_t at = p < count[0] ? first[0] + p * step[0] : first[1] + (p - count[0]) * step[1];
+      float pm = -INFINITY, pl = 0.f;
+      if (p < pieces) {
+        pm = w.part_ml[2 * (uint64_t)at];
+        pl = w.part_ml[2 * (uint64_t)at + 1];
+      }
+      float top = pm;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+      const float m_new = fmaxf(m, top);
+      const float m_use = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = __builtin_amdgcn_exp2f(m - m_use);
+      const float f = __builtin_amdgcn_exp2f(pm - m_use);
+      m = m_new;
+      l = l * alpha + f * pl;  // per lane: summed over the lanes at the end
+#pragma unroll
+      for (int d = 0; d < kDims; ++d) acc[d] *= alpha;
+      const uint32_t here = pieces - p0 < 64 ? pieces - p0 : 64;
+      for (uint32_t i = 0; i < here; ++i) {
+        const float fi = __shfl(f, (int)i, 64);
+        const uint32_t from = (uint32_t)__shfl((int)at, (int)i, 64);
+        if (fi == 0.f) continue;
+        const float* src = w.part_o + (uint64_t)from * D + lane * kDims;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) acc[d] += fi * src[d];
+      }
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) l += __shfl_xor(l, o, 64);
+    const bool none = l == 0.f;
+    const float inv = none ? 0.f : 1.f / l;
+    scalar* out = reinterpret_cast<scalar*>(a.out) + (uint64_t)r * D + lane * kDims;
+#pragma unroll
+    for (int d = 0; d < kDims; ++d) out[d] = (scalar)(acc[d] * inv);
+    if (a.lse && lane == 0) a.lse[r] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+  }
+}
+
+// Sets the error text with the call's name; *shape and *args as the kernels take them.
+gleam_status validate_attention(const gleam_kv_pages* kv, const gleam_prefix_batch* b, PlanShape* shape) {
+  const char* const who = "gleam_prefix_attention";
+  gleam_status st = validate_kv(kv, who);
+  if (st != GLEAM_OK) return st;
+  if (!b) {
+    set_error("%s: null batch", who);
+    return GLEAM_E_INVALID;
+  }
+  if (b->q_heads == 0 || b->q_heads % kv->kv_heads != 0 || b->q_heads > 65535) {
+    set_error("%s: q_heads must be a multiple of kv_heads, up to 65535", who);
+    return GLEAM_E_INVALID;
+  }
+  if (b->n_tokens > (uint64_t)INT32_MAX / b->q_heads) {
+    set_error("%s: n_tokens * q_heads of 2^31 or more", who);
+    return GLEAM_E_UNSUPPORTED;
+  }
+  if (b->n_seq > kMostSeq || b->n_groups > kMostSeq) {
+    set_error("%s: more than 2^20 sequences or groups", who);
+    return GLEAM_E_UNSUPPORTED;
+  }
+  if (b->own_width > (uint64_t)INT32_MAX / kv->page_tokens || b->prefix_width > (uint64_t)INT32_MAX / kv->page_tokens) {
+    set_error("%s: a table row of 2^31 keys or more", who);
+    return GLEAM_E_INVALID;
+  }
+  shape->n_tokens = b->n_tokens;
+  shape->n_seq = b->n_seq;
+  shape->n_groups = b->n_groups;
+  shape->kv_heads = kv->kv_heads;
+  shape->ratio = b->q_heads / kv->kv_heads;
+  shape->target = 1024;
+  if (most_units(*shape) > max_workgroups(kThreads) || most_partials(*shape) > UINT32_MAX) {
+    set_error("%s: more work than one launch holds", who);
+    return GLEAM_E_UNSUPPORTED;
+  }
+  return GLEAM_OK;
+}
+
+template <class T, int D>
+gleam_status launch_all(const AttendArgs& a, uint32_t units, uint32_t joins, hipStream_t stream) {
+  hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a);
+  gleam_status st = launch_status("plan_kernel");
+  if (st != GLEAM_OK) return st;
+  hipLaunchKernelGGL((attend_kernel<T, D>), dim3(units), dim3(kThreads), 0, stream, a);
+  if ((st = launch_status("attend_kernel")) != GLEAM_OK) return st;
+  hipLaunchKernelGGL((join_kernel<T, D>), dim3(joins), dim3(kThreads), 0, stream, a);
+  return launch_status("join_kernel");
+}
+
+}  // namespace
+
+hipError_t preload_prefix_attention() {
+  hipFuncAttributes attr;
+  return hipFuncGetAttributes(&attr, reinterpret_cast<const void*>(&plan_kernel));
+}
+
+}  // namespace gleam
+
+extern "C" size_t gleam_prefix_attention_ws_bytes(const gleam_kv_pages* kv, const gleam_prefix_batch* b) {
+  using namespace gleam;
+  clear_error();
+  PlanShape s{};
+  if (validate_attention(kv, b, &s) != GLEAM_OK) return 0;
+  return ws_at(nullptr, s, kv->head_dim).bytes;
+}
+
+extern "C" gleam_status gleam_prefix_attention(const gleam_kv_pages* kv, const gleam_prefix_batch* b, void* d_out,
+                                               float* d_lse, void* d_ws, size_t ws_bytes, void* stream) {
+  using namespace gleam;
+  clear_error();
+  const char* const who = "gleam_prefix_attention";
+  PlanShape shape{};
+  gleam_status st = validate_attention(kv, b, &shape);
+  if (st != GLEAM_OK) return st;
+  if (b->n_tokens == 0) return GLEAM_OK;
+  if ((st = validate_heads(b->d_q, b->q_stride, "q", who)) != GLEAM_OK) return st;
+  const int64_t whole[2] = {0, 0};
+  if ((st = validate_heads(d_out, whole, "out", who)) != GLEAM_OK) return st;
+  if (b->n_seq > 0 && (!b->d_q_first || !b->d_own_len || (b->own_width > 0 && !b->d_own_pages))) {
+    set_error("%s: null q_first, own_len or own_pages", who);
+    return GLEAM_E_INVALID;
+  }
+  if (b->n_groups > 0 && (!b->d_group_first || !b->d_prefix_len || (b->prefix_width > 0 && !b->d_prefix_pages))) {
+    set_error("%s: groups need group_first, prefix_len and prefix_pages", who);
+    return GLEAM_E_INVALID;
+  }
+  if (!d_ws || !aligned256(d_ws)) {
+    set_error("%s: workspace must be non-null and 256-byte aligned", who);
+    return GLEAM_E_INVALID;
+  }
+  AttendArgs a{};
+  a.ws = ws_at(static_cast<uint8_t*>(d_ws), shape, kv->head_dim);
+  if (ws_bytes < a.ws.bytes) {
+    set_error("%s: workspace of %zu bytes, %zu needed", who, ws_bytes, a.ws.bytes);
+    return GLEAM_E_WORKSPACE;
+  }
+  a.q = static_cast<const uint8_t*>(b->d_q);
+  a.q_token = 2 * b->q_stride[0];
+  a.q_head = 2 * b->q_stride[1];
+  a.k = static_cast<const uint8_t*>(kv->d_k);
+  a.v = static_cast<const uint8_t*>(kv->d_v);
+  a.k_page = 2 * kv->k_stride[0];
+  a.k_place = 2 * kv->k_stride[1];
+  a.k_head = 2 * kv->k_stride[2];
+  a.v_page = 2 * kv->v_stride[0];
+  a.v_place = 2 * kv->v_stride[1];
+  a.v_head = 2 * kv->v_stride[2];
+  a.q_first = b->d_q_first;
+  a.own_pages = b->d_own_pages;
+  a.own_len = b->d_own_len;
+  a.group_first = b->d_group_first;
+  a.prefix_pages = b->d_prefix_pages;
+  a.prefix_len = b->d_prefix_len;
+  a.n_tokens = (uint32_t)b->n_tokens;
+  a.n_seq = (uint32_t)b->n_seq;
+  a.n_groups = (uint32_t)b->n_groups;
+  a.own_width = (uint32_t)b->own_width;
+  a.prefix_width = (uint32_t)b->prefix_width;
+  a.q_heads = b->q_heads;
+  a.kv_heads = kv->kv_heads;
+  a.ratio = shape.ratio;
+  a.page_log2 = (uint32_t)log2_exact(kv->page_tokens);
+  a.n_pages = (uint32_t)kv->n_pages;
+  a.target = shape.target;
+  a.scale_log2 = b->scale * kLog2e;
+  a.out = static_cast<uint8_t*>(d_out);
+  a.lse = d_lse;
+  const uint32_t units = (uint32_t)most_units(shape);
+  const uint64_t waves = (b->n_tokens * b->q_heads + kWaves - 1) / kWaves;
+  const uint32_t joins = (uint32_t)(waves < 2048 ? waves : 2048);
+  hipStream_t s = (hipStream_t)stream;
+  if (kv->dtype == GLEAM_FP16) {
+    return kv->head_dim == 64    ? launch_all<Fp16, 64>(a, units, joins, s)
+           : kv->head_dim == 128 ? launch_all<Fp16, 128>(a, units, joins, s)
+                                 : launch_all<Fp16, 256>(a, units, joins, s);
+  }
+  return kv->head_dim == 64    ? launch_all<Bf16, 64>(a, units, joins, s)
+         : kv->head_dim == 128 ? launch_all<Bf16, 128>(a, units, joins, s)
+                               : launch_all<Bf16, 256>(a, units, joins, s);
+}

@@ -1,0 +1,88 @@
+// How prefix_attention cuts its work, as plain arithmetic (a CPU test compiles this file by
+// itself; on the GPU one workgroup runs it over the lengths it finds there).
+//
+// An item is a set of rows (one row for each token and query head of a key head) with the keys
+// that all of them may see: a group's tokens with the group's prefix, or a sequence's tokens
+// with its own keys. A sequence's item holds the group's prefix too ("joint") where sharing
+// would save nothing: in a group of one, and where sequences have so many rows that each fills
+// tiles of its own. Keys are walked in steps; an item's steps are cut into chunks, its rows into
+// tiles, and a unit is one tile of one key head over one chunk. What a row gathers from several
+// chunks, or from its group's item and its own, goes through partial results in the workspace
+// and is joined afterwards.
+#pragma once
+
+#include <stdint.h>
+
+#ifdef __HIPCC__
+#define GLEAM_HD __host__ __device__ inline
+#else
+#define GLEAM_HD inline
+#endif
+
+namespace gleam {
+
+constexpr uint32_t kStep = 64;        // keys in a step
+constexpr uint32_t kSmallRows = 16;   // rows of a tile
+constexpr uint32_t kJointRows = 64;   // sequences of a group with this many rows on average keep to themselves
+constexpr uint32_t kMinSteps = 2;     // steps of the shortest chunk: one round of a workgroup's four waves
+
+struct PlanShape {  // what the host knows
+  uint64_t n_tokens, n_seq, n_groups;
+  uint32_t kv_heads, ratio;  // ratio: query heads per key head
+  uint32_t target;           // units wanted: what fills the GPU
+};
+
+GLEAM_HD uint64_t div_up(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
+
+GLEAM_HD uint32_t steps_of(uint32_t keys) { return (keys + kStep - 1) / kStep; }
+
+GLEAM_HD bool joint_group(uint64_t rows, uint64_t seqs) { return seqs <= 1 || rows >= kJointRows * seqs; }
+
+GLEAM_HD uint32_t tiles_of(uint32_t rows) { return (rows + kSmallRows - 1) / kSmallRows; }
+
+// What an item costs a key head: its tiles' steps.
+GLEAM_HD uint64_t item_cost(uint32_t rows, uint32_t steps) { return (uint64_t)tiles_of(rows) * steps; }
+
+// Steps of a chunk of an item of `rows` rows: no more than `target` chunks of all items' tiles
+// together, apart from each tile's first. `cost`: all items', of all key heads.
+GLEAM_HD uint32_t chunk_steps(uint32_t rows, uint64_t cost, uint32_t target) {
+  (void)rows;
+  const uint64_t c = div_up(cost, target);
+  return c < kMinSteps ? kMinSteps : c > 0x7fffffffu ? 0x7fffffffu : (uint32_t)c;
+}
+
+// Chunks of an item, and its own steps per chunk: as even as the count allows.
+struct Cut {
+  uint32_t chunks, per;
+};
+GLEAM_HD Cut cut_steps(uint32_t steps, uint32_t most) {
+  Cut c{0, 1};
+  if (steps == 0) return c;
+  c.chunks = (steps + most - 1) / most;
+  c.per = (steps + c.chunks - 1) / c.chunks;
+  c.chunks = (steps + c.per - 1) / c.per;
+  return c;
+}
+
+// The bounds that the launch and the workspace are sized by, from what the host knows.
+//
+// Units: sum of tiles * kv_heads * chunks, where chunks < steps / chunk_steps + 1, so at most
+// target + kv_heads * tiles. Tiles: an item of n rows has at most n / kSmallRows + 1 of them, and
+// a token's rows are in two items at most, its group's and its sequence's.
+GLEAM_HD uint64_t most_units(const PlanShape& s) {
+  const uint64_t rows = s.n_tokens * s.ratio;
+  const uint64_t tiles = s.n_groups + s.n_seq + 2 * rows / kSmallRows;
+  return s.target + s.kv_heads * tiles;
+}
+
+// Rows of partial results: an item that is cut, or shares its rows with another, has
+// rows * kv_heads * chunks. Shared: groups that are not joint have fewer than kJointRows rows a
+// sequence, in two items, for their first chunks. Cut: chunks >= 2 makes chunks <= 2 * steps /
+// chunk_steps, and rows <= kSmallRows * tiles, so 2 * kSmallRows * target at most.
+GLEAM_HD uint64_t most_partials(const PlanShape& s) {
+  const uint64_t rows = s.n_tokens * s.ratio, apart = kJointRows * s.n_seq;
+  const uint64_t shared = s.n_groups ? 2 * (rows < apart ? rows : apart) * s.kv_heads : 0;
+  return shared + 2ull * kSmallRows * s.target;
+}
+
+}  // namespace gleam
