@@ -25,13 +25,11 @@ struct Fp16 {
   typedef f16x8 vec8;
   // exponent bits of a 16-bit value: all set in infinities and NaN
   static constexpr uint32_t kExp = 0x7c00u;
-  static constexpr uint32_t kOne = 0x3c00u;
 };
 struct Bf16 {
   typedef __bf16 scalar;
   typedef bf16x8 vec8;
   static constexpr uint32_t kExp = 0x7f80u;
-  static constexpr uint32_t kOne = 0x3f80u;
 };
 
 }  // namespace gleam

@@ -307,32 +307,24 @@ __device__ inline void put(Pack8& p, int i, float x, Bf16) { p.b[i] = (__bf16)x;
 __device__ inline f16x8 get(const Pack8& p, Fp16) { return p.h; }
 __device__ inline bf16x8 get(const Pack8& p, Bf16) { return p.b; }
 
-// Of two 16-bit values in a dword, those that are infinite or NaN are cleared, and marked with a
-// 1.0 in `up` (+infinity, NaN) and `down` (-infinity, NaN).
+// An infinite or NaN value of a key that some rows of a tile may not see would reach them as
+// 0 * infinity. Where a tile has such keys, its values are looked at, the infinite and NaN ones
+// are taken as 0 in the products, and add_special adds them at the end to the rows that see them.
+
+// Bit 15 of each half of the result: the exponent of the 16-bit value there is all ones (the
+// lowest exponent bit added to it carries into the sign's place).
 template <class T>
-__device__ inline uint32_t split_special(uint32_t x, uint32_t* up, uint32_t* down) {
-  uint32_t keep = 0, u = 0, d = 0;
-#pragma unroll
-  for (int i = 0; i < 32; i += 16) {
-    const uint32_t b = (x >> i) & 0xffffu;
-    if ((b & T::kExp) != T::kExp) {
-      keep |= b << i;
-    } else {
-      const bool nan = (b & 0x7fffu) != T::kExp;
-      if (nan || !(b & 0x8000u)) u |= T::kOne << i;
-      if (nan || (b & 0x8000u)) d |= T::kOne << i;
-    }
-  }
-  *up = u;
-  *down = d;
-  return keep;
+__device__ inline uint32_t special_bits(uint32_t x) {
+  constexpr uint32_t low = T::kExp & (0u - T::kExp);
+  return ((x & (T::kExp * 0x10001u)) + low * 0x10001u) & 0x80008000u;
 }
 template <class T>
-__device__ inline bool has_special(uint32_t x) {
-  return (x & T::kExp) == T::kExp || ((x >> 16) & T::kExp) == T::kExp;
+__device__ inline uint32_t clear_special(uint32_t x) {
+  return x & ~((special_bits<T>(x) >> 15) * 0xffffu);
 }
 
-// Where 16 keys from `key` on (a multiple of 16, so within a page) are.
+// Where the keys from `key` on are, up to the 16 that lie in its page (key a multiple of 8; fewer
+// than 16 are used where it is not one of 16).
 struct Keys16 {
   const uint8_t* k;
   const uint8_t* v;
@@ -350,30 +342,50 @@ __device__ inline Keys16 keys16(const AttendArgs& a, const int32_t* pages, uint3
   return t;
 }
 
+// Calls add(i, value) for kN values, with 0 in the place of finite ones.
+template <class T, int kN, class Add>
+__device__ inline void add_special(const uint8_t* v, const Add& add) {
+#pragma unroll
+  for (int i = 0; i < kN; i += 4) {
+    const u32x2v x = *reinterpret_cast<const u32x2v*>(v + 2 * i);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const uint32_t bits = (x[c >> 1] >> (16 * (c & 1))) & 0xffffu;
+      // as 32-bit bits, 0 for a finite value; no branches, there are many of these
+      const uint32_t wide = T::kExp == 0x7f80u ? bits << 16
+                                               : (bits & 0x8000u) << 16 | 0x7f800000u | (bits & 0x3ffu) << 13;
+      add(i + c, __uint_as_float(wide & (0u - (special_bits<T>(bits) >> 15))));
+    }
+  }
+}
+
+// A unit, as its workgroup finds it.
+struct Unit {
+  Item it;
+  uint32_t head, chunk, tile;
+};
+
+// 16 rows, the waves taking turns at the keys.
 template <class T, int D>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(AttendArgs a) {
+__device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit, char* lds) {
   typedef typename T::scalar scalar;
   constexpr int kDims = D / 16;       // dims a lane brings of a value row
   constexpr int kWords = kDims / 2;   // as dwords
   constexpr int kKMfma = D / 32;      // products over a key's dims
   constexpr int kPad = D + 4;         // row of the workgroup's partial outputs in LDS
-  __shared__ __attribute__((aligned(16))) float lds_o[kWaves][kSmallRows][kPad];
-  __shared__ float lds_m[kWaves][kSmallRows], lds_l[kWaves][kSmallRows];
-
-  const Ws& w = a.ws;
-  if (blockIdx.x >= w.head->units) return;
-  const uint32_t n_items = a.n_groups + a.n_seq;
-  const uint32_t at = __builtin_amdgcn_readfirstlane((int)wave_search<uint32_t>(w.unit_first, n_items, blockIdx.x));
-  const Item it = w.items[at];
+  typedef float RowsO[kFewRows][kPad];
+  typedef float Rows[kFewRows];
+  RowsO* const lds_o = reinterpret_cast<RowsO*>(lds);
+  Rows* const lds_m = reinterpret_cast<Rows*>(lds + kWaves * sizeof(RowsO));
+  Rows* const lds_l = lds_m + kWaves;
+  const Item& it = unit.it;
+  const uint32_t head = unit.head, chunk = unit.chunk, tile = unit.tile;
   const uint32_t rows = it.tokens * a.ratio;
-  uint32_t u = blockIdx.x - it.unit_first;
-  const uint32_t head = u % a.kv_heads;
-  u /= a.kv_heads;
-  const uint32_t chunk = u % it.chunks, tile = u / it.chunks;
+  const Ws& w = a.ws;
 
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const uint32_t n = lane & 15, g = lane >> 4;
-  const uint32_t row = tile * kSmallRows + n;
+  const uint32_t row = tile * kFewRows + n;
   const bool row_live = row < rows;
   const uint32_t token = it.token_first + (row_live ? row / a.ratio : 0);
   const uint32_t q_head = head * a.ratio + (row_live ? row % a.ratio : 0);
@@ -382,9 +394,9 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(Atte
   const int64_t behind = (int64_t)it.own_keys - it.tokens + 1;
   const int64_t sees = behind + (row_live ? row / a.ratio : 0);
   const uint32_t own_seen = sees < 0 ? 0 : (uint32_t)sees;
-  const int64_t fewest = behind + tile * kSmallRows / a.ratio;
+  const int64_t fewest = behind + tile * kFewRows / a.ratio;
   const uint32_t own_least = fewest < 0 ? 0 : (uint32_t)fewest;
-  uint32_t last_row = tile * kSmallRows + kSmallRows - 1;
+  uint32_t last_row = tile * kFewRows + kFewRows - 1;
   if (last_row >= rows) last_row = rows - 1;
   const int64_t furthest = behind + last_row / a.ratio;
   const uint32_t own_most = furthest < 0 ? 0 : furthest > it.own_keys ? it.own_keys : (uint32_t)furthest;
@@ -405,6 +417,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(Atte
   uint32_t end = 2 * (chunk + 1) * it.per;
   if (end > all_halves) end = all_halves;
 
+  bool special = false;
   float m = -INFINITY, l = 0.f;
   f32x4 o[kDims];
 #pragma unroll
@@ -486,59 +499,43 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(Atte
 #pragma unroll
       for (int j = 0; j < kDims; ++j) o[j] *= alpha;
     }
-    // An infinite or NaN value would reach rows that may not see it as 0 * infinity: such values
-    // are taken out and added afterwards where they are seen.
-    bool special = false;
     if (!shared && masked) {
-      bool any = false;
+      uint32_t any = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e)
 #pragma unroll
-        for (int c = 0; c < kWords; ++c) any |= has_special<T>(vv[e][c]);
-      special = __any(any);
+        for (int c = 0; c < kWords; ++c) any |= special_bits<T>(vv[e][c]);
+      if (__any(any != 0)) {
+        special = true;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+          for (int c = 0; c < kWords; ++c) vv[e][c] = clear_special<T>(vv[e][c]);
+      }
     }
-    if (!special) {
 #pragma unroll
-      for (int c = 0; c < kWords; ++c) {
-        Pack8 lo, hi;
+    for (int c = 0; c < kWords; ++c) {
+      Pack8 lo, hi;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          lo.u[e] = __builtin_amdgcn_perm(vv[2 * e + 1][c], vv[2 * e][c], 0x05040100u);
-          hi.u[e] = __builtin_amdgcn_perm(vv[2 * e + 1][c], vv[2 * e][c], 0x07060302u);
-        }
-        o[2 * c] = Mfma<T>::run(get(lo, T()), get(p, T()), o[2 * c]);
-        o[2 * c + 1] = Mfma<T>::run(get(hi, T()), get(p, T()), o[2 * c + 1]);
+      for (int e = 0; e < 4; ++e) {
+        lo.u[e] = __builtin_amdgcn_perm(vv[2 * e + 1][c], vv[2 * e][c], 0x05040100u);
+        hi.u[e] = __builtin_amdgcn_perm(vv[2 * e + 1][c], vv[2 * e][c], 0x07060302u);
       }
-    } else {
-      Pack8 sight;
+      o[2 * c] = Mfma<T>::run(get(lo, T()), get(p, T()), o[2 * c]);
+      o[2 * c + 1] = Mfma<T>::run(get(hi, T()), get(p, T()), o[2 * c + 1]);
+    }
+  }
+  if (special) {  // the same halves again: those that were looked at
+    for (uint32_t half = 2 * chunk * it.per + wave; half < end; half += kWaves) {
+      const uint32_t key = 32 * (half - prefix_halves);
+      if (half < prefix_halves || key + 32 <= own_least) continue;
+      for (uint32_t i = 0; i < 32; ++i) {
+        const Keys16 t = keys16(a, own_pages, key + (i & 16), it.own_keys, head);
+        if ((i & 15) >= t.n || key + i >= own_seen) continue;
+        const uint8_t* const v = t.v + (int64_t)(i & 15) * a.v_place;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t r = 4 * g + (e & 3);
-        put(sight, e, key + (e >> 2) * 16 + r < seen && r < t[e >> 2].n ? 1.f : 0.f, T());
-      }
-#pragma unroll
-      for (int c = 0; c < kWords; ++c) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          Pack8 plain, up, down;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t both = __builtin_amdgcn_perm(vv[2 * e + 1][c], vv[2 * e][c], h ? 0x07060302u : 0x05040100u);
-            uint32_t pos, neg;
-            plain.u[e] = split_special<T>(both, &pos, &neg);
-            up.u[e] = pos;
-            down.u[e] = neg;
-          }
-          const int j = 2 * c + h;
-          o[j] = Mfma<T>::run(get(plain, T()), get(p, T()), o[j]);
-          const f32x4 pos = Mfma<T>::run(get(up, T()), get(sight, T()), (f32x4)0.f);
-          const f32x4 neg = Mfma<T>::run(get(down, T()), get(sight, T()), (f32x4)0.f);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            if (pos[r] > 0.f) o[j][r] += INFINITY;
-            if (neg[r] > 0.f) o[j][r] -= INFINITY;
-          }
-        }
+        for (int r = 0; r < 4; ++r)
+          add_special<T, kDims>(v + (g * 4 + r) * kDims * 2, [&](int j, float x) { o[j][r] += x; });
       }
     }
   }
@@ -559,8 +556,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(Atte
     }
   __syncthreads();
   constexpr int kQuads = D / 4;
-  for (int i = threadIdx.x; i < (int)kSmallRows * kQuads; i += kThreads) {
-    const uint32_t rr = i / kQuads, c = i % kQuads, in = tile * kSmallRows + rr;
+  for (int i = threadIdx.x; i < (int)kFewRows * kQuads; i += kThreads) {
+    const uint32_t rr = i / kQuads, c = i % kQuads, in = tile * kFewRows + rr;
     if (in >= rows) continue;
     float top = -INFINITY;
 #pragma unroll
@@ -593,6 +590,339 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(Atte
       if (c == 0 && a.lse) a.lse[to] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
     }
   }
+}
+
+// 128 rows, 32 a wave, over keys that the workgroup stages in LDS, one sub-step ahead.
+//
+// Products are v_mfma_f32_32x32x16 in the same orientation: S^T = K Q^T, O^T = V^T P^T, a lane
+// holding one row's scores with keys 8 i + 4 h .. + 3 (h = lane / 32), which again are P's operand
+// as they are when V's brings keys {4h..} and {8 + 4h..} of each 16. V's operand, 8 keys of one
+// dim, comes from rows in LDS through the transposing ds_read_b64_tr_b16: 16 lanes read 4 keys of
+// 16 dims, and lane i gets dim i of all 4. Rows in LDS are swizzled so that the lanes of one read
+// fall into different banks: 16-byte pieces of K by the row, 32-byte pieces of V by the row's
+// place among the 4.
+template <int D>
+struct Staged {
+  static constexpr int kKeys = D == 256 ? 32 : 64;      // keys of a sub-step
+  static constexpr int kSubs = kStep / kKeys;           // sub-steps of a step
+  static constexpr int kRow = 2 * D;                    // bytes of a row
+  static constexpr int kPieces = kRow / 16;             // 16-byte pieces of a row
+  static constexpr int kRows = kKeys / kWaves;          // rows that a wave stages
+  static constexpr int kLoads = kRows * kPieces / 64;   // 16-byte loads of a lane for them
+  static constexpr int kTile = kKeys * kRow;            // bytes of K or V
+  static constexpr int kBytes = 4 * kTile + 2 * kWaves * 4;  // two of each, and flags
+  static __device__ uint32_t k_at(uint32_t row, uint32_t piece) {
+    return row * kRow + ((piece ^ (D == 64 ? (row >> 1) & 7 : row & 15)) << 4);
+  }
+  static __device__ uint32_t v_swizzle(uint32_t row) { return D == 64 ? ((row >> 1) & 1) << 1 : (row & 3) << 1; }
+  static __device__ uint32_t v_at(uint32_t row, uint32_t piece) {
+    return row * kRow + (((piece >> 1) ^ v_swizzle(row)) << 5) + ((piece & 1) << 4);
+  }
+};
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+template <class T> struct Mfma32;
+template <> struct Mfma32<Fp16> {
+  static __device__ f32x16 run(f16x8 a, f16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+  }
+};
+template <> struct Mfma32<Bf16> {
+  static __device__ f32x16 run(bf16x8 a, bf16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+};
+
+__device__ inline u32x2v read_transposed(const char* p) {
+  union {
+    s16x4 s;
+    u32x2v u;
+  } x;
+  x.s = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (__attribute__((address_space(3))) s16x4*)(__attribute__((address_space(3))) void*)const_cast<char*>(p));
+  return x.u;
+}
+
+// max and sum of a lane's value and that of the lane 32 away
+__device__ inline float max_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float sum_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+template <class T, int D>
+__device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& unit, char* lds) {
+  typedef typename T::scalar scalar;
+  typedef Staged<D> St;
+  constexpr int kKTiles = St::kKeys / 32, kQ = D / 16, kO = D / 32;
+  char* const lds_k = lds;
+  char* const lds_v = lds + 2 * St::kTile;
+  uint32_t* const lds_flags = reinterpret_cast<uint32_t*>(lds + 4 * St::kTile);
+  const Item& it = unit.it;
+  const uint32_t head = unit.head, rows = it.tokens * a.ratio;
+  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const uint32_t n = lane & 31, h = lane >> 5;
+  const uint32_t wave_row = unit.tile * kTileRows + 32 * wave;
+  const uint32_t row = wave_row + n;
+  const bool row_live = row < rows;
+  const uint32_t token = it.token_first + (row_live ? row / a.ratio : 0);
+  const uint32_t q_head = head * a.ratio + (row_live ? row % a.ratio : 0);
+
+  // keys of the sequence's own that the lane's row sees, the fewest and most of the wave's rows,
+  // and of the workgroup's
+  const int64_t behind = (int64_t)it.own_keys - it.tokens + 1;
+  auto seen_by = [&](uint32_t r) {
+    if (r >= rows) r = rows - 1;
+    const int64_t x = behind + r / a.ratio;
+    return x < 0 ? 0u : (uint32_t)x;
+  };
+  const uint32_t own_seen = seen_by(row), own_least = seen_by(wave_row);
+  const uint32_t own_wave_most = wave_row < rows ? seen_by(wave_row + 31) : 0;
+  const uint32_t own_group_least = seen_by(unit.tile * kTileRows);
+  const uint32_t own_most = seen_by(unit.tile * kTileRows + kTileRows - 1);
+
+  // Scores are scaled after the product; a scale below zero is taken from the queries' signs, so
+  // that the largest score is the largest product's.
+  const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;
+  const float scale = fabsf(a.scale_log2);
+  Pack8 q[kQ];
+#pragma unroll
+  for (int i = 0; i < kQ; ++i) {
+    q[i].u = (u32x4v)0u;
+    if (row_live)
+      q[i].u = *reinterpret_cast<const u32x4v*>(a.q + (int64_t)token * a.q_token + (int64_t)q_head * a.q_head +
+                                                (i * 16 + h * 8) * 2);
+    q[i].u ^= flip;
+  }
+
+  const int32_t* const prefix_pages = a.prefix_pages + (uint64_t)it.prefix_row * a.prefix_width;
+  const int32_t* const own_pages = a.own_pages + (uint64_t)it.own_row * a.own_width;
+  const uint32_t prefix_subs = St::kSubs * steps_of(it.prefix_keys);
+  const uint32_t all_subs = prefix_subs + (own_most + St::kKeys - 1) / St::kKeys;
+  uint32_t end = St::kSubs * (unit.chunk + 1) * it.per;
+  if (end > all_subs) end = all_subs;
+  uint32_t sub = St::kSubs * unit.chunk * it.per;
+
+  // the wave's rows of a sub-step, from memory to registers and from there to LDS
+  u32x4v stage_k[St::kLoads], stage_v[St::kLoads];
+  uint32_t stage_flags = 0;  // 1: values were cleared; from bit 8 on how many of the rows exist
+  auto stage_load = [&](uint32_t s) {
+    const bool shared = s < prefix_subs;
+    const uint32_t key = (shared ? s : s - prefix_subs) * St::kKeys + wave * St::kRows;
+    const uint32_t keys = shared ? it.prefix_keys : it.own_keys;
+    const Keys16 t = keys16(a, shared ? prefix_pages : own_pages, key, keys, head);
+    stage_flags = (t.n < (uint32_t)St::kRows ? t.n : (uint32_t)St::kRows) << 8;
+#pragma unroll
+    for (int i = 0; i < St::kLoads; ++i) {
+      const uint32_t r = (i * 64 + lane) / St::kPieces, piece = (i * 64 + lane) % St::kPieces;
+      stage_k[i] = stage_v[i] = (u32x4v)0u;
+      if (r < t.n) {
+        stage_k[i] = *reinterpret_cast<const u32x4v*>(t.k + (int64_t)r * a.k_place + piece * 16);
+        stage_v[i] = *reinterpret_cast<const u32x4v*>(t.v + (int64_t)r * a.v_place + piece * 16);
+      }
+    }
+  };
+  auto stage_store = [&](uint32_t s, uint32_t buf) {
+    if (s >= prefix_subs && (s - prefix_subs + 1) * St::kKeys > own_group_least) {
+      uint32_t any = 0;
+#pragma unroll
+      for (int i = 0; i < St::kLoads; ++i)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) any |= special_bits<T>(stage_v[i][c]);
+      if (__any(any != 0)) {
+        stage_flags |= 1;
+#pragma unroll
+        for (int i = 0; i < St::kLoads; ++i)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) stage_v[i][c] = clear_special<T>(stage_v[i][c]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < St::kLoads; ++i) {
+      const uint32_t r = wave * St::kRows + (i * 64 + lane) / St::kPieces, piece = (i * 64 + lane) % St::kPieces;
+      *reinterpret_cast<u32x4v*>(lds_k + buf * St::kTile + St::k_at(r, piece)) = stage_k[i];
+      *reinterpret_cast<u32x4v*>(lds_v + buf * St::kTile + St::v_at(r, piece)) = stage_v[i];
+    }
+    if (lane == 0) lds_flags[buf * kWaves + wave] = stage_flags;
+  };
+
+  bool special = false;
+  float m = -INFINITY, l = 0.f;  // m: of the products, not yet scaled
+  f32x16 o[kO];
+#pragma unroll
+  for (int i = 0; i < kO; ++i) o[i] = (f32x16)0.f;
+
+  // where the lane reads: K rows and pieces, V quads of keys and dims
+  const uint32_t k_lane = St::k_at(n, h);
+  uint32_t v_lane[kO];
+  {
+    const uint32_t quad = (lane & 15) >> 2, half = (lane >> 4) & 1;
+#pragma unroll
+    for (int i = 0; i < kO; ++i) {
+      const uint32_t r = 4 * h + quad;
+      v_lane[i] = r * St::kRow + (((2 * i + half) ^ St::v_swizzle(r)) << 5) + (lane & 3) * 8;
+    }
+  }
+
+  if (sub < end) {
+    stage_load(sub);
+    stage_store(sub, 0);
+  }
+  __syncthreads();
+  for (uint32_t buf = 0; sub < end; ++sub, buf ^= 1) {
+    const bool more = sub + 1 < end;
+    if (more) stage_load(sub + 1);
+    const bool shared = sub < prefix_subs;
+    const uint32_t key = (shared ? sub : sub - prefix_subs) * St::kKeys;
+    if (wave_row < rows && (shared || key < own_wave_most)) {
+      const char* const kb = lds_k + buf * St::kTile;
+      const char* const vb = lds_v + buf * St::kTile;
+      const u32x4v flags4 = *reinterpret_cast<const u32x4v*>(lds_flags + buf * kWaves);
+      uint32_t exist[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const uint32_t f = (uint32_t)__builtin_amdgcn_readfirstlane((int)flags4[c]);
+        exist[c] = f >> 8;
+        special |= f & 1;
+      }
+      f32x16 s[kKTiles];
+#pragma unroll
+      for (int t = 0; t < kKTiles; ++t) {
+        s[t] = (f32x16)0.f;
+#pragma unroll
+        for (int i = 0; i < kQ; ++i) {
+          Pack8 k;
+          k.u = *reinterpret_cast<const u32x4v*>(kb + t * 32 * St::kRow + (k_lane ^ (i << 5)));
+          s[t] = Mfma32<T>::run(get(k, T()), get(q[i], T()), s[t]);
+        }
+      }
+      const bool all_exist = exist[0] + exist[1] + exist[2] + exist[3] == (uint32_t)St::kKeys;
+      if (!all_exist || (!shared && key + St::kKeys > own_least)) {
+        const uint32_t seen = shared ? it.prefix_keys : own_seen;
+#pragma unroll
+        for (int t = 0; t < kKTiles; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int in = 32 * t + 8 * (r / 4) + r % 4;  // and 4 h on
+            if (key + in + 4 * h >= seen || in % St::kRows + 4 * h >= exist[in / St::kRows]) s[t][r] = -INFINITY;
+          }
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int t = 0; t < kKTiles; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
+      top = max_halves(top);
+      if (__any(top > m)) {
+        const float m_new = fmaxf(m, top);
+        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - m_new) * scale);
+        m = m_new;
+        l *= alpha;
+#pragma unroll
+        for (int i = 0; i < kO; ++i) o[i] *= alpha;
+      }
+      const float bias = m == -INFINITY ? 0.f : -m * scale;  // nothing seen so far: all exponentials are 0
+      Pack8 p[kKTiles * 2];
+#pragma unroll
+      for (int t = 0; t < kKTiles; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float y = __builtin_amdgcn_exp2f(fmaf(s[t][r], scale, bias));
+          l += y;
+          put(p[2 * t + r / 8], r % 8, y, T());
+        }
+#pragma unroll
+      for (int kk = 0; kk < 2 * kKTiles; ++kk)
+#pragma unroll
+        for (int i = 0; i < kO; ++i) {
+          Pack8 v;
+          const u32x2v x = read_transposed(vb + kk * 16 * St::kRow + v_lane[i]);
+          const u32x2v y = read_transposed(vb + (kk * 16 + 8) * St::kRow + v_lane[i]);
+          v.u = (u32x4v){x[0], x[1], y[0], y[1]};
+          o[i] = Mfma32<T>::run(get(v, T()), get(p[kk], T()), o[i]);
+        }
+    }
+    if (more) stage_store(sub + 1, buf ^ 1);
+    __syncthreads();
+  }
+
+  l = sum_halves(l);
+  if (!row_live) return;
+  if (special) {
+    uint32_t key = own_group_least & ~(St::kKeys - 1u);  // the first sub-step that was looked at
+    const uint32_t first = St::kSubs * unit.chunk * it.per;
+    if (first > prefix_subs && (first - prefix_subs) * St::kKeys > key) key = (first - prefix_subs) * St::kKeys;
+    const uint32_t to = (end - prefix_subs) * St::kKeys;
+    for (; key < to && key < own_seen; ++key) {
+      const Keys16 t = keys16(a, own_pages, key & ~15u, it.own_keys, head);
+      if ((key & 15) >= t.n) continue;
+      const uint8_t* const v = t.v + (int64_t)(key & 15) * a.v_place + 8 * h;
+#pragma unroll
+      for (int i = 0; i < kO; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+          add_special<T, 4>(v + (32 * i + 2 * r) * 2, [&](int c, float x) { o[i][r + c] += x; });
+    }
+  }
+  const float top = m == -INFINITY ? -INFINITY : m * scale;
+  if (it.partial) {
+    const uint64_t at_row = it.part_first + ((uint64_t)head * it.chunks + unit.chunk) * rows + row;
+    float* const to = a.ws.part_o + at_row * D + 4 * h;
+#pragma unroll
+    for (int i = 0; i < kO; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *reinterpret_cast<f32x4*>(to + 32 * i + 2 * r) = (f32x4){o[i][r], o[i][r + 1], o[i][r + 2], o[i][r + 3]};
+    if (h == 0) {
+      a.ws.part_ml[2 * at_row] = top;
+      a.ws.part_ml[2 * at_row + 1] = l;
+    }
+  } else {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const uint64_t to = (uint64_t)token * a.q_heads + q_head;
+    scalar* const out = reinterpret_cast<scalar*>(a.out) + to * D + 4 * h;
+#pragma unroll
+    for (int i = 0; i < kO; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        scalar y[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) y[c] = (scalar)(o[i][r + c] * inv);
+        *reinterpret_cast<uint64_t*>(out + 32 * i + 2 * r) = *reinterpret_cast<const uint64_t*>(y);
+      }
+    if (h == 0 && a.lse) a.lse[to] = l == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * kLn2;
+  }
+}
+
+template <int D>
+constexpr int lds_bytes() {
+  constexpr int few = kWaves * kFewRows * (D + 4 + 2) * 4, tile = Staged<D>::kBytes;
+  return few > tile ? few : tile;
+}
+
+template <class T, int D>
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(AttendArgs a) {
+  __shared__ __attribute__((aligned(16))) char lds[lds_bytes<D>()];
+  const Ws& w = a.ws;
+  if (blockIdx.x >= w.head->units) return;
+  const uint32_t n_items = a.n_groups + a.n_seq;
+  const uint32_t at = __builtin_amdgcn_readfirstlane((int)wave_search<uint32_t>(w.unit_first, n_items, blockIdx.x));
+  Unit unit;
+  unit.it = w.items[at];
+  const uint32_t rows = unit.it.tokens * a.ratio;
+  uint32_t u = blockIdx.x - unit.it.unit_first;
+  unit.head = u % a.kv_heads;
+  u /= a.kv_heads;
+  unit.chunk = u % unit.it.chunks;
+  // a prompt's last rows see the most keys: they come first
+  unit.tile = tiles_of(rows) - 1 - u / unit.it.chunks;
+  if (rows <= kMostFew) attend_few<T, D>(a, unit, lds);
+  else attend_tile<T, D>(a, unit, lds);
 }
 
 // --------------------------------------------------------------------------------------- //

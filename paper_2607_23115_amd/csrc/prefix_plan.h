@@ -22,9 +22,12 @@
 namespace gleam {
 
 constexpr uint32_t kStep = 64;        // keys in a step
-constexpr uint32_t kSmallRows = 16;   // rows of a tile
-constexpr uint32_t kJointRows = 64;   // sequences of a group with this many rows on average keep to themselves
-constexpr uint32_t kMinSteps = 2;     // steps of the shortest chunk: one round of a workgroup's four waves
+constexpr uint32_t kFewRows = 16, kTileRows = 128;  // rows of a tile, of the two kinds
+constexpr uint32_t kMostFew = 32;     // items of up to this many rows take tiles of the first kind
+constexpr uint32_t kJointRows = 128;  // sequences of a group with this many rows on average keep to themselves
+constexpr uint32_t kMinFewSteps = 2;  // steps of the shortest chunk: one round of a workgroup's four waves
+// and of the second kind, whose partial results are 64 KiB a unit (128 rows of 128 dims)
+constexpr uint32_t kMinTileSteps = 8;
 
 struct PlanShape {  // what the host knows
   uint64_t n_tokens, n_seq, n_groups;
@@ -38,17 +41,18 @@ GLEAM_HD uint32_t steps_of(uint32_t keys) { return (keys + kStep - 1) / kStep; }
 
 GLEAM_HD bool joint_group(uint64_t rows, uint64_t seqs) { return seqs <= 1 || rows >= kJointRows * seqs; }
 
-GLEAM_HD uint32_t tiles_of(uint32_t rows) { return (rows + kSmallRows - 1) / kSmallRows; }
+GLEAM_HD uint32_t tile_rows(uint32_t rows) { return rows <= kMostFew ? kFewRows : kTileRows; }
+GLEAM_HD uint32_t tiles_of(uint32_t rows) { return (rows + tile_rows(rows) - 1) / tile_rows(rows); }
 
-// What an item costs a key head: its tiles' steps.
+// What an item costs a key head: its tiles' steps (a step of 16 rows is bound by reading its
+// keys and values, one of 128 by their products: much the same time).
 GLEAM_HD uint64_t item_cost(uint32_t rows, uint32_t steps) { return (uint64_t)tiles_of(rows) * steps; }
 
 // Steps of a chunk of an item of `rows` rows: no more than `target` chunks of all items' tiles
 // together, apart from each tile's first. `cost`: all items', of all key heads.
 GLEAM_HD uint32_t chunk_steps(uint32_t rows, uint64_t cost, uint32_t target) {
-  (void)rows;
-  const uint64_t c = div_up(cost, target);
-  return c < kMinSteps ? kMinSteps : c > 0x7fffffffu ? 0x7fffffffu : (uint32_t)c;
+  const uint64_t c = div_up(cost, target), least = rows <= kMostFew ? kMinFewSteps : kMinTileSteps;
+  return c < least ? (uint32_t)least : c > 0x7fffffffu ? 0x7fffffffu : (uint32_t)c;
 }
 
 // Chunks of an item, and its own steps per chunk: as even as the count allows.
@@ -67,22 +71,23 @@ GLEAM_HD Cut cut_steps(uint32_t steps, uint32_t most) {
 // The bounds that the launch and the workspace are sized by, from what the host knows.
 //
 // Units: sum of tiles * kv_heads * chunks, where chunks < steps / chunk_steps + 1, so at most
-// target + kv_heads * tiles. Tiles: an item of n rows has at most n / kSmallRows + 1 of them, and
-// a token's rows are in two items at most, its group's and its sequence's.
+// target + kv_heads * tiles. Tiles: an item of n rows has at most n / kFewRows + 1 of them, and
+// at most n / kTileRows + 2, and a token's rows are in two items at most, its group's and its
+// sequence's.
 GLEAM_HD uint64_t most_units(const PlanShape& s) {
-  const uint64_t rows = s.n_tokens * s.ratio;
-  const uint64_t tiles = s.n_groups + s.n_seq + 2 * rows / kSmallRows;
-  return s.target + s.kv_heads * tiles;
+  const uint64_t rows = 2 * s.n_tokens * s.ratio, items = s.n_groups + s.n_seq;
+  const uint64_t few = items + rows / kFewRows, tile = 2 * items + rows / kTileRows;
+  return s.target + s.kv_heads * (few < tile ? few : tile);
 }
 
 // Rows of partial results: an item that is cut, or shares its rows with another, has
 // rows * kv_heads * chunks. Shared: groups that are not joint have fewer than kJointRows rows a
 // sequence, in two items, for their first chunks. Cut: chunks >= 2 makes chunks <= 2 * steps /
-// chunk_steps, and rows <= kSmallRows * tiles, so 2 * kSmallRows * target at most.
+// chunk_steps, and rows <= kTileRows * tiles, so 2 * kTileRows * target at most.
 GLEAM_HD uint64_t most_partials(const PlanShape& s) {
   const uint64_t rows = s.n_tokens * s.ratio, apart = kJointRows * s.n_seq;
   const uint64_t shared = s.n_groups ? 2 * (rows < apart ? rows : apart) * s.kv_heads : 0;
-  return shared + 2ull * kSmallRows * s.target;
+  return shared + 2ull * kTileRows * s.target;
 }
 
 }  // namespace gleam
