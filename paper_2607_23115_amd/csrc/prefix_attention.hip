@@ -8,8 +8,10 @@
 // separate pieces of one row. Scores are kept times log2(e), so that every exponential is one
 // hardware exp2.
 //
-// Three launches: plan_kernel cuts the lengths it finds on the device into units
-// (prefix_plan.h), attend_kernel takes a unit per workgroup, join_kernel joins the pieces.
+// attend_kernel takes a unit per workgroup, join_kernel joins the pieces. The lengths found on the
+// device are cut into units (prefix_plan.h) by plan_kernel, or, in a batch of up to 63 items, by
+// every wave of attend_kernel for itself, an item a lane: that takes about a microsecond, a launch
+// and the wait for it several.
 //
 // A unit is 16 rows of one key head. Four waves take turns at 32 keys each, straight from memory
 // to registers in the layouts of v_mfma_f32_16x16x32: nothing is exchanged between lanes but the
@@ -35,6 +37,8 @@ constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kPlanThreads = 1024;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr uint64_t kMostSeq = 1ull << 20;
+constexpr uint32_t kWideJoin = 4096;   // up to this many rows are joined by a workgroup each
+constexpr uint32_t kMostJoins = 2048;  // workgroups of the others: those that the GPU holds at once
 
 struct Item {
   uint32_t token_first, tokens;  // rows: tokens * ratio
@@ -114,19 +118,44 @@ struct MaxOp {
   template <class V> __device__ V operator()(V a, V b) const { return a > b ? a : b; }
 };
 
-// Inclusive scan over the workgroup; every thread calls it. `total` gets the last value.
+// The value that a DPP control brings to each lane, `none` where it brings nothing.
+template <int kCtrl, int kRows>
+__device__ inline uint32_t dpp(uint32_t v, uint32_t none) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, kCtrl, kRows, 0xf, false);
+}
+template <int kCtrl, int kRows>
+__device__ inline int32_t dpp(int32_t v, int32_t none) {
+  return __builtin_amdgcn_update_dpp(none, v, kCtrl, kRows, 0xf, false);
+}
+template <int kCtrl, int kRows>
+__device__ inline uint64_t dpp(uint64_t v, uint64_t none) {
+  return (uint64_t)dpp<kCtrl, kRows>((uint32_t)(v >> 32), (uint32_t)(none >> 32)) << 32 |
+         dpp<kCtrl, kRows>((uint32_t)v, (uint32_t)none);
+}
+
+// Inclusive scan over a wave of values that 0 leaves as they are: shifts by 1, 2, 4 and 8 within
+// rows of 16 lanes, then the last lanes of rows 0 and 2 to the rows after them, then lane 31 to
+// the upper half.
+template <class V, class Op>
+__device__ V wave_scan(V v, Op op) {
+  v = op(dpp<0x111, 0xf>(v, (V)0), v);
+  v = op(dpp<0x112, 0xf>(v, (V)0), v);
+  v = op(dpp<0x114, 0xf>(v, (V)0), v);
+  v = op(dpp<0x118, 0xf>(v, (V)0), v);
+  v = op(dpp<0x142, 0xa>(v, (V)0), v);
+  v = op(dpp<0x143, 0xc>(v, (V)0), v);
+  return v;
+}
+
+// The same over the workgroup; every thread calls it. `total` gets the last value.
 template <class V, class Op>
 __device__ V block_scan(V v, V* lds, V* total, Op op) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const V u = __shfl_up(v, o, 64);
-    if (lane >= o) v = op(u, v);
-  }
+  v = wave_scan(v, op);
   if (lane == 63) lds[wave] = v;
   __syncthreads();
   V all = lds[0];
-  for (int w = 1; w < kPlanThreads / 64; ++w) {
+  for (int w = 1; w < (int)(blockDim.x >> 6); ++w) {
     if (w == wave) v = op(all, v);
     all = op(all, lds[w]);
   }
@@ -135,130 +164,222 @@ __device__ V block_scan(V v, V* lds, V* total, Op op) {
   return v;
 }
 
-// src[0..n] as non-decreasing values within [0, most], into dst.
-__device__ void tidy_offsets(const int32_t* src, int32_t* dst, uint32_t n, int32_t most, int32_t* lds) {
+__device__ inline int32_t clamp_to(int32_t v, int32_t most) { return v < 0 ? 0 : v > most ? most : v; }
+
+__device__ inline uint32_t clamp_keys(int32_t n, uint32_t width, uint32_t page_log2) {
+  return (uint32_t)clamp_to(n, (int32_t)(width << page_log2));
+}
+
+// Item i without its cut. q(i), g(i): the offsets, already tidy; own(s), prefix(g): lengths as
+// given; group_of(s): -1 for none. All lanes call them, with indexes in range.
+template <class Q, class G, class Own, class Prefix, class GroupOf>
+__device__ Item make_item(const AttendArgs& a, uint32_t i, const Q& q, const G& g, const Own& own,
+                          const Prefix& prefix, const GroupOf& group_of) {
+  const bool is_group = i < a.n_groups;
+  const uint32_t s = is_group || i >= a.n_groups + a.n_seq ? 0 : i - a.n_groups;
+  const uint32_t t0 = (uint32_t)q(s), t1 = (uint32_t)q(s + 1);
+  const uint32_t own_keys = clamp_keys(own(s), a.own_width, a.page_log2);
+  uint32_t shared = 0, g0 = 0, g1 = 0, row = 0;  // the group's prefix
+  if (a.n_groups) {
+    const int32_t of_seq = group_of(s), in = is_group ? (int32_t)i : of_seq;
+    row = in < 0 ? 0 : (uint32_t)in;
+    const uint32_t s0 = (uint32_t)g(row), s1 = (uint32_t)g(row + 1);
+    g0 = (uint32_t)q(s0);
+    g1 = (uint32_t)q(s1);
+    const uint32_t keys = clamp_keys(prefix(row), a.prefix_width, a.page_log2);
+    if (in >= 0) shared = keys;
+    // keys that the group's item has, and the sequence's has not
+    if (joint_group((uint64_t)(g1 - g0) * a.ratio, s1 - s0) == is_group) {
+      if (is_group) shared = 0;
+      else row = ~0u;
+    }
+  }
+  Item it{};
+  if (is_group) {
+    it.token_first = g0;
+    it.tokens = g1 - g0;
+    it.prefix_row = row;
+    it.prefix_keys = shared;
+    it.partial = 1;
+  } else {
+    it.token_first = t0;
+    it.tokens = t1 - t0;
+    it.own_row = s;
+    it.own_keys = own_keys;
+    it.partial = row == ~0u && shared > 0;
+    it.prefix_row = row == ~0u ? 0 : row;
+    it.prefix_keys = row == ~0u ? 0 : shared;
+  }
+  return it;
+}
+
+__device__ inline uint32_t item_steps(const Item& it) {
+  return it.tokens ? steps_of(it.prefix_keys) + steps_of(it.own_keys) : 0;
+}
+
+// Cuts an item, cost being all items'; its units and rows of partial results, as one number (both
+// sums stay below 2^32: most_units, most_partials).
+__device__ inline uint64_t cut_item(const AttendArgs& a, Item& it, uint64_t cost) {
+  const uint32_t rows = it.tokens * a.ratio;
+  const Cut cut = cut_steps(item_steps(it), chunk_steps(rows, cost, a.target));
+  it.chunks = cut.chunks;
+  it.per = cut.per;
+  if (cut.chunks > 1) it.partial = 1;
+  const uint64_t parts = it.partial ? (uint64_t)it.tokens * a.q_heads * cut.chunks : 0;
+  return (uint64_t)(tiles_of(rows) * a.kv_heads * cut.chunks) << 32 | parts;
+}
+
+// The plan of a batch of up to 63 items as every wave has it: item i in lane i.
+constexpr uint32_t kWaveItems = 63;
+
+struct WavePlan {
+  Item it;          // of the lane
+  int32_t q;        // tidy offset, of the lane
+  int32_t group;    // of sequence `lane`
+  uint32_t units, joins;
+};
+
+__device__ WavePlan plan_in_wave(const AttendArgs& a) {
+  const uint32_t lane = threadIdx.x & 63, n_items = a.n_groups + a.n_seq;
+  WavePlan w;
+  int32_t q = lane <= a.n_seq ? a.q_first[lane] : (int32_t)a.n_tokens;
+  int32_t g = a.n_groups && lane <= a.n_groups ? a.group_first[lane] : (int32_t)a.n_seq;
+  const int32_t own = lane < a.n_seq ? a.own_len[lane] : 0;
+  const int32_t prefix = lane < a.n_groups ? a.prefix_len[lane] : 0;
+  q = wave_scan(clamp_to(q, (int32_t)a.n_tokens), MaxOp());
+  w.q = q;
+  w.group = -1;
+  if (a.n_groups) {
+    g = wave_scan(clamp_to(g, (int32_t)a.n_seq), MaxOp());
+    // the last group that starts at or before the sequence, if it has not ended there
+    for (uint32_t i = 0; i < a.n_groups; ++i) {
+      const int32_t from = __builtin_amdgcn_readlane(g, (int)i), to = __builtin_amdgcn_readlane(g, (int)i + 1);
+      if ((int32_t)lane >= from && (int32_t)lane < to) w.group = (int32_t)i;
+    }
+  }
+  auto of = [](int32_t v) { return [v](uint32_t i) { return __shfl(v, (int)i, 64); }; };
+  w.it = make_item(a, lane, of(q), of(g), of(own), of(prefix), of(w.group));
+  if (lane >= n_items) w.it = Item{};
+  const uint32_t steps = item_steps(w.it);
+  const uint64_t cost = wave_scan(item_cost(w.it.tokens * a.ratio, steps) * a.kv_heads, SumOp());
+  const uint64_t mine = cut_item(a, w.it, __shfl(cost, 63, 64));
+  const uint64_t sum = wave_scan(mine, SumOp());
+  w.it.unit_first = (uint32_t)((sum - mine) >> 32);
+  w.it.part_first = (uint32_t)(sum - mine);
+  w.units = (uint32_t)(__shfl(sum, 63, 64) >> 32);
+  const bool empty = lane >= a.n_groups && w.it.tokens && steps == 0;
+  w.joins = __any(empty || (uint32_t)mine != 0) || __shfl(q, 0, 64) > 0 ||
+            __shfl(q, (int)a.n_seq, 64) < (int32_t)a.n_tokens;
+  return w;
+}
+
+// For join_kernel: what plan_kernel leaves behind. By one wave.
+__device__ inline void write_plan(const AttendArgs& a, const WavePlan& plan) {
+  const Ws& w = a.ws;
+  const uint32_t lane = threadIdx.x & 63;
+  if (lane <= a.n_seq) w.q_first[lane] = plan.q;
+  if (lane < a.n_seq) w.seq_group[lane] = plan.group;
+  if (lane < a.n_groups + a.n_seq) w.items[lane] = plan.it;
+  if (lane == 0) w.head->joins = plan.joins;
+}
+
+// Lane i's item, in all lanes.
+__device__ inline Item item_of_lane(const Item& it, uint32_t i) {
+  auto get = [i](uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, (int)i); };
+  Item r{};
+  r.token_first = get(it.token_first);
+  r.tokens = get(it.tokens);
+  r.prefix_row = get(it.prefix_row);
+  r.prefix_keys = get(it.prefix_keys);
+  r.own_row = get(it.own_row);
+  r.own_keys = get(it.own_keys);
+  r.chunks = get(it.chunks);
+  r.per = get(it.per);
+  r.unit_first = get(it.unit_first);
+  r.part_first = get(it.part_first);
+  r.partial = get(it.partial);
+  return r;
+}
+
+// Offsets of up to this many sequences and groups are kept in LDS, of more in the workspace.
+constexpr uint32_t kPlanLds = 4096;
+
+// src[0..n] as non-decreasing values within [0, most], into dst and out (which may be one).
+__device__ void tidy_offsets(const int32_t* src, int32_t* dst, int32_t* out, uint32_t n, int32_t most, int32_t* lds) {
   int32_t carry = 0;
-  for (uint32_t i0 = 0; i0 <= n; i0 += kPlanThreads) {
+  for (uint32_t i0 = 0; i0 <= n; i0 += blockDim.x) {
     const uint32_t i = i0 + threadIdx.x;
-    int32_t v = i <= n ? src[i] : 0;
-    v = v < 0 ? 0 : v > most ? most : v;
-    int32_t total;
+    int32_t v = clamp_to(i <= n ? src[i] : 0, most), total;
     v = block_scan(v, lds, &total, MaxOp());
-    if (i <= n) dst[i] = v > carry ? v : carry;
+    v = v > carry ? v : carry;
+    if (i <= n) dst[i] = out[i] = v;
     carry = carry > total ? carry : total;
   }
 }
 
-__device__ uint32_t clamp_keys(int32_t n, uint32_t width, uint32_t page_log2) {
-  const uint32_t most = width << page_log2;
-  return n < 0 ? 0 : (uint32_t)n > most ? most : (uint32_t)n;
-}
-
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a) {
   __shared__ uint64_t lds[kPlanThreads / 64];
+  __shared__ int32_t lds_q[kPlanLds + 1], lds_g[kPlanLds + 1];
   int32_t* lds32 = reinterpret_cast<int32_t*>(lds);
   const Ws& w = a.ws;
   const uint32_t n_items = a.n_groups + a.n_seq;
-  if (a.n_seq == 0) {  // no sequence covers any token
-    if (threadIdx.x == 0) {
-      w.head->units = 0;
-      w.head->joins = 1;
-    }
-    return;
-  }
-  tidy_offsets(a.q_first, w.q_first, a.n_seq, (int32_t)a.n_tokens, lds32);
-  for (uint32_t s = threadIdx.x; s < a.n_seq; s += kPlanThreads) w.seq_group[s] = -1;
+  int32_t* const q = a.n_seq <= kPlanLds ? lds_q : w.q_first;
+  int32_t* const g = a.n_groups <= kPlanLds ? lds_g : w.group_first;
+  tidy_offsets(a.q_first, q, w.q_first, a.n_seq, (int32_t)a.n_tokens, lds32);
+  if (a.n_groups) tidy_offsets(a.group_first, g, w.group_first, a.n_groups, (int32_t)a.n_seq, lds32);
   __syncthreads();
-  if (a.n_groups) {
-    tidy_offsets(a.group_first, w.group_first, a.n_groups, (int32_t)a.n_seq, lds32);
-    __syncthreads();
-    // the last group that starts at or before the sequence, if it has not ended there
-    const int32_t from = w.group_first[0], to = w.group_first[a.n_groups];
-    for (uint32_t s = threadIdx.x; s < a.n_seq; s += kPlanThreads) {
-      if ((int32_t)s < from || (int32_t)s >= to) continue;
-      uint32_t lo = 0, hi = a.n_groups;  // group_first[lo] <= s < group_first[hi]
-      while (hi - lo > 1) {
-        const uint32_t mid = (lo + hi) / 2;
-        if (w.group_first[mid] <= (int32_t)s) lo = mid;
-        else hi = mid;
-      }
-      w.seq_group[s] = (int32_t)lo;
+  auto group_of = [&](uint32_t s) {
+    if ((int32_t)s < g[0] || (int32_t)s >= g[a.n_groups]) return -1;
+    uint32_t lo = 0, hi = a.n_groups;  // g[lo] <= s < g[hi]
+    while (hi - lo > 1) {
+      const uint32_t mid = (lo + hi) / 2;
+      if (g[mid] <= (int32_t)s) lo = mid;
+      else hi = mid;
     }
-  }
-  __syncthreads();
+    return (int32_t)lo;
+  };
+  auto of = [](const int32_t* v) { return [v](uint32_t i) { return v[i]; }; };
 
   // the items without their cuts, and the cost of all
   uint64_t cost = 0;
-  uint32_t empty_rows = w.q_first[0] > 0 || w.q_first[a.n_seq] < (int32_t)a.n_tokens;
-  for (uint32_t i = threadIdx.x; i < n_items; i += kPlanThreads) {
-    Item it{};
-    if (i < a.n_groups) {
-      const int32_t s0 = w.group_first[i], s1 = w.group_first[i + 1];
-      it.token_first = (uint32_t)w.q_first[s0];
-      it.tokens = (uint32_t)w.q_first[s1] - it.token_first;
-      it.prefix_row = i;
-      if (!joint_group((uint64_t)it.tokens * a.ratio, (uint64_t)(s1 - s0)))
-        it.prefix_keys = clamp_keys(a.prefix_len[i], a.prefix_width, a.page_log2);
-      it.partial = 1;
-    } else {
-      const uint32_t s = i - a.n_groups;
-      it.token_first = (uint32_t)w.q_first[s];
-      it.tokens = (uint32_t)w.q_first[s + 1] - it.token_first;
-      it.own_row = s;
-      it.own_keys = clamp_keys(a.own_len[s], a.own_width, a.page_log2);
-      const int32_t g = w.seq_group[s];
-      if (g >= 0) {
-        const uint32_t keys = clamp_keys(a.prefix_len[g], a.prefix_width, a.page_log2);
-        const int32_t s0 = w.group_first[g], s1 = w.group_first[g + 1];
-        const uint64_t rows = (uint64_t)(w.q_first[s1] - w.q_first[s0]) * a.ratio;
-        if (joint_group(rows, (uint64_t)(s1 - s0))) {
-          it.prefix_row = (uint32_t)g;
-          it.prefix_keys = keys;
-        } else {
-          it.partial = keys > 0;
-        }
-      }
-    }
-    const uint32_t steps = it.tokens ? steps_of(it.prefix_keys) + steps_of(it.own_keys) : 0;
+  uint32_t joins = q[0] > 0 || q[a.n_seq] < (int32_t)a.n_tokens;
+  Item first{};  // of the thread; those of later rounds go through the workspace
+  for (uint32_t i = threadIdx.x; i < n_items; i += blockDim.x) {
+    Item it = make_item(a, i, of(q), of(g), of(a.own_len), of(a.prefix_len), group_of);
+    const uint32_t steps = item_steps(it);
     cost += item_cost(it.tokens * a.ratio, steps) * a.kv_heads;
-    if (i >= a.n_groups && it.tokens && steps == 0) empty_rows = 1;
-    w.items[i] = it;
+    if (i >= a.n_groups && it.tokens && steps == 0) joins = 1;
+    if (i < blockDim.x) first = it;
+    else w.items[i] = it;
+    if (a.n_groups && i >= a.n_groups) w.seq_group[i - a.n_groups] = group_of(i - a.n_groups);
   }
   uint64_t all_cost;
   block_scan(cost, lds, &all_cost, SumOp());
 
   // chunks, units and partial rows
-  uint32_t units = 0, joins = empty_rows;
-  uint64_t parts = 0;
-  for (uint32_t i0 = 0; i0 < n_items; i0 += kPlanThreads) {
+  uint64_t before = 0;
+  for (uint32_t i0 = 0; i0 < n_items; i0 += blockDim.x) {
     const uint32_t i = i0 + threadIdx.x;
-    Item it{};
-    if (i < n_items) it = w.items[i];
-    const uint32_t steps = it.tokens ? steps_of(it.prefix_keys) + steps_of(it.own_keys) : 0;
-    const Cut cut = cut_steps(steps, chunk_steps(it.tokens * a.ratio, all_cost, a.target));
-    it.chunks = cut.chunks;
-    it.per = cut.per;
-    if (cut.chunks > 1) it.partial = 1;
-    const uint32_t n_units = tiles_of(it.tokens * a.ratio) * a.kv_heads * cut.chunks;
-    const uint64_t n_parts = it.partial ? (uint64_t)it.tokens * a.q_heads * cut.chunks : 0;
-    uint32_t unit_total;
-    uint64_t part_total;
-    const uint32_t unit_end = block_scan(n_units, reinterpret_cast<uint32_t*>(lds), &unit_total, SumOp());
-    const uint64_t part_end = block_scan(n_parts, lds, &part_total, SumOp());
+    Item it = first;
+    if (i0 > 0) {
+      it = Item{};
+      if (i < n_items) it = w.items[i];
+    }
+    const uint64_t mine = cut_item(a, it, all_cost);
+    uint64_t total;
+    const uint64_t at = before + block_scan(mine, lds, &total, SumOp()) - mine;
     if (i < n_items) {
-      it.unit_first = units + unit_end - n_units;
-      it.part_first = (uint32_t)(parts + part_end - n_parts);
+      it.unit_first = (uint32_t)(at >> 32);
+      it.part_first = (uint32_t)at;
       w.items[i] = it;
       w.unit_first[i] = it.unit_first;
     }
-    joins |= n_parts > 0;
-    units += unit_total;
-    parts += part_total;
+    joins |= (uint32_t)mine != 0;
+    before += total;
   }
   joins = __syncthreads_or((int)joins);
   if (threadIdx.x == 0) {
-    w.unit_first[n_items] = units;
-    w.head->units = units;
+    w.head->units = (uint32_t)(before >> 32);
     w.head->joins = joins;
   }
 }
@@ -909,11 +1030,19 @@ template <class T, int D>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(AttendArgs a) {
   __shared__ __attribute__((aligned(16))) char lds[lds_bytes<D>()];
   const Ws& w = a.ws;
-  if (blockIdx.x >= w.head->units) return;
   const uint32_t n_items = a.n_groups + a.n_seq;
-  const uint32_t at = __builtin_amdgcn_readfirstlane((int)wave_search<uint32_t>(w.unit_first, n_items, blockIdx.x));
   Unit unit;
-  unit.it = w.items[at];
+  if (n_items <= kWaveItems) {
+    const WavePlan plan = plan_in_wave(a);
+    if (blockIdx.x == 0 && threadIdx.x < 64) write_plan(a, plan);
+    if (blockIdx.x >= plan.units) return;
+    const uint32_t lane = threadIdx.x & 63;
+    const uint64_t le = __ballot(lane < n_items && plan.it.unit_first <= blockIdx.x);
+    unit.it = item_of_lane(plan.it, 63 - __clzll((long long)le));
+  } else {
+    if (blockIdx.x >= w.head->units) return;
+    unit.it = w.items[__builtin_amdgcn_readfirstlane((int)wave_search<uint32_t>(w.unit_first, n_items, blockIdx.x))];
+  }
   const uint32_t rows = unit.it.tokens * a.ratio;
   uint32_t u = blockIdx.x - unit.it.unit_first;
   unit.head = u % a.kv_heads;
@@ -928,32 +1057,45 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(Atte
 // --------------------------------------------------------------------------------------- //
 // join
 // --------------------------------------------------------------------------------------- //
-// One wave per row: the pieces' maxima and sums are read 64 at a time, then their outputs, each
-// lane D/64 dims. Rows that no piece covers are set to nothing seen.
-template <class T, int D>
+// D/4 lanes take a piece of a row, 4 dims each. Where there are many rows they join all of its
+// pieces, 64 / (D/4) rows a wave; with few rows (kWide) a workgroup's lanes share the pieces of
+// one. Four pieces are in flight at a time. Bound by reading the pieces, or with few by the time
+// of two loads. Rows that no piece covers are set to nothing seen.
+template <class T, int D, bool kWide>
 __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a) {
   typedef typename T::scalar scalar;
-  constexpr int kDims = D / 64;
+  constexpr uint32_t kLanes = D / 4, kTeams = kThreads / kLanes;
+  constexpr uint32_t kRows = kWide ? 1 : kTeams, kStride = kWide ? kTeams : 1;
+  __shared__ __attribute__((aligned(16))) float lds_o[kWide ? kTeams : 1][D];
+  __shared__ float lds_m[kTeams], lds_l[kTeams];
   const Ws& w = a.ws;
-  if (!w.head->joins) return;
-  const uint32_t lane = threadIdx.x & 63;
-  const uint32_t waves = gridDim.x * kWaves, all = a.n_tokens * a.q_heads;
-  for (uint32_t r = blockIdx.x * kWaves + (threadIdx.x >> 6); r < all; r += waves) {
+  if (a.n_seq > 0 && !w.head->joins) return;  // attend_kernel wrote every row
+  const uint32_t team = threadIdx.x / kLanes, dim = threadIdx.x % kLanes * 4;
+  const uint32_t all = a.n_tokens * a.q_heads;
+  const int32_t t0 = a.n_seq ? w.q_first[0] : 0, t1 = a.n_seq ? w.q_first[a.n_seq] : 0;
+  // the rows of a workgroup are side by side: of few tokens, and the first one's sequence is found by all
+  for (uint32_t r0 = blockIdx.x * kRows; r0 < all; r0 += gridDim.x * kRows) {
+    const uint32_t token0 = r0 / a.q_heads;
+    uint32_t s = 0;
+    if ((int32_t)token0 >= t0 && (int32_t)token0 < t1) s = wave_search<int32_t>(w.q_first, a.n_seq + 1, (int32_t)token0);
+    const uint32_t r = r0 + (kWide ? 0 : team);
+    if (r >= all) continue;
     const uint32_t token = r / a.q_heads, h = r - token * a.q_heads;
     const uint32_t head = h / a.ratio;
     uint32_t first[2] = {0, 0}, count[2] = {0, 0}, step[2] = {0, 0};  // the group's pieces, the sequence's
-    if (a.n_seq > 0 && (int32_t)token >= w.q_first[0] && (int32_t)token < w.q_first[a.n_seq]) {
-      const uint32_t s = wave_search<int32_t>(w.q_first, a.n_seq + 1, (int32_t)token);
-      const Item own = w.items[a.n_groups + s];
-      if (!own.partial && own.chunks) continue;  // written already
-      if (own.partial) {
+    if ((int32_t)token >= t0 && (int32_t)token < t1) {
+      while (w.q_first[s + 1] <= (int32_t)token) ++s;
+      const Item& own = w.items[a.n_groups + s];
+      const uint32_t chunks = own.chunks, partial = own.partial;
+      if (!partial && chunks) continue;  // written already
+      if (partial) {
         const uint32_t rows = own.tokens * a.ratio;
-        first[1] = own.part_first + head * own.chunks * rows + (token - own.token_first) * a.ratio + h % a.ratio;
-        count[1] = own.chunks;
+        first[1] = own.part_first + head * chunks * rows + (token - own.token_first) * a.ratio + h % a.ratio;
+        count[1] = chunks;
         step[1] = rows;
-        const int32_t gr = w.seq_group[s];
+        const int32_t gr = a.n_groups ? w.seq_group[s] : -1;
         if (gr >= 0) {
-          const Item pre = w.items[gr];
+          const Item& pre = w.items[gr];
           const uint32_t all_rows = pre.tokens * a.ratio;
           first[0] = pre.part_first + head * pre.chunks * all_rows + (token - pre.token_first) * a.ratio + h % a.ratio;
           count[0] = pre.chunks;
@@ -961,46 +1103,69 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a) {
         }
       }
     }
-    float m = -INFINITY, l = 0.f;
-    float acc[kDims] = {};
     const uint32_t pieces = count[0] + count[1];
-    for (uint32_t p0 = 0; p0 < pieces; p0 += 64) {
-      const uint32_t p = p0 + lane;
-      const uint32_t at = p < count[0] ? first[0] + p * step[0] : first[1] + (p - count[0]) * step[1];
-      float pm = -INFINITY, pl = 0.f;
-      if (p < pieces) {
-        pm = w.part_ml[2 * (uint64_t)at];
-        pl = w.part_ml[2 * (uint64_t)at + 1];
-      }
-      float top = pm;
+    float m = -INFINITY, l = 0.f;
+    f32x4 acc = (f32x4)0.f;
+    for (uint32_t p0 = kWide ? team : 0; p0 < pieces; p0 += 4 * kStride) {
+      float pm[4], pl[4];
+      f32x4 x[4];
 #pragma unroll
-      for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-      const float m_new = fmaxf(m, top);
+      for (uint32_t u = 0; u < 4; ++u) {
+        const uint32_t p = p0 + u * kStride;
+        pm[u] = -INFINITY;
+        pl[u] = 0.f;
+        x[u] = (f32x4)0.f;
+        if (p < pieces) {
+          const uint64_t at = p < count[0] ? first[0] + p * step[0] : first[1] + (p - count[0]) * step[1];
+          pm[u] = w.part_ml[2 * at];
+          pl[u] = w.part_ml[2 * at + 1];
+          x[u] = *reinterpret_cast<const f32x4*>(w.part_o + at * D + dim);
+        }
+      }
+      float m_new = m;
+#pragma unroll
+      for (uint32_t u = 0; u < 4; ++u) m_new = fmaxf(m_new, pm[u]);
       const float m_use = m_new == -INFINITY ? 0.f : m_new;
       const float alpha = __builtin_amdgcn_exp2f(m - m_use);
-      const float f = __builtin_amdgcn_exp2f(pm - m_use);
       m = m_new;
-      l = l * alpha + f * pl;  // per lane: summed over the lanes at the end
+      l *= alpha;
+      acc *= alpha;
 #pragma unroll
-      for (int d = 0; d < kDims; ++d) acc[d] *= alpha;
-      const uint32_t here = pieces - p0 < 64 ? pieces - p0 : 64;
-      for (uint32_t i = 0; i < here; ++i) {
-        const float fi = __shfl(f, (int)i, 64);
-        const uint32_t from = (uint32_t)__shfl((int)at, (int)i, 64);
-        if (fi == 0.f) continue;
-        const float* src = w.part_o + (uint64_t)from * D + lane * kDims;
-#pragma unroll
-        for (int d = 0; d < kDims; ++d) acc[d] += fi * src[d];
+      for (uint32_t u = 0; u < 4; ++u) {
+        if (pl[u] == 0.f) continue;  // saw nothing
+        const float f = __builtin_amdgcn_exp2f(pm[u] - m_use);
+        l += f * pl[u];
+        acc += f * x[u];
       }
     }
+    if constexpr (kWide) {
+      if (dim == 0) {
+        lds_m[team] = m;
+        lds_l[team] = l;
+      }
+      *reinterpret_cast<f32x4*>(&lds_o[team][dim]) = acc;
+      __syncthreads();
+      if (team != 0) return;  // one row a workgroup
+      m = lds_m[0];
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) l += __shfl_xor(l, o, 64);
+      for (uint32_t i = 1; i < kTeams; ++i) m = fmaxf(m, lds_m[i]);
+      l = 0.f;
+      acc = (f32x4)0.f;
+#pragma unroll
+      for (uint32_t i = 0; i < kTeams; ++i) {
+        if (lds_l[i] == 0.f) continue;
+        const float f = __builtin_amdgcn_exp2f(lds_m[i] - m);
+        l += f * lds_l[i];
+        acc += f * *reinterpret_cast<const f32x4*>(&lds_o[i][dim]);
+      }
+    }
     const bool none = l == 0.f;
     const float inv = none ? 0.f : 1.f / l;
-    scalar* out = reinterpret_cast<scalar*>(a.out) + (uint64_t)r * D + lane * kDims;
+    scalar y[4];
 #pragma unroll
-    for (int d = 0; d < kDims; ++d) out[d] = (scalar)(acc[d] * inv);
-    if (a.lse && lane == 0) a.lse[r] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    for (int d = 0; d < 4; ++d) y[d] = (scalar)(acc[d] * inv);
+    *reinterpret_cast<uint64_t*>(a.out + ((uint64_t)r * D + dim) * 2) = *reinterpret_cast<const uint64_t*>(y);
+    if (a.lse && dim == 0) a.lse[r] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
   }
 }
 
@@ -1035,6 +1200,9 @@ gleam_status validate_attention(const gleam_kv_pages* kv, const gleam_prefix_bat
   shape->kv_heads = kv->kv_heads;
   shape->ratio = b->q_heads / kv->kv_heads;
   shape->target = 1024;
+  const uint64_t most = steps_of((uint32_t)(b->own_width * kv->page_tokens)) +
+                        (uint64_t)steps_of((uint32_t)(b->prefix_width * kv->page_tokens));
+  shape->most_steps = (uint32_t)most;
   if (most_units(*shape) > max_workgroups(kThreads) || most_partials(*shape) > UINT32_MAX) {
     set_error("%s: more work than one launch holds", who);
     return GLEAM_E_UNSUPPORTED;
@@ -1043,13 +1211,28 @@ gleam_status validate_attention(const gleam_kv_pages* kv, const gleam_prefix_bat
 }
 
 template <class T, int D>
-gleam_status launch_all(const AttendArgs& a, uint32_t units, uint32_t joins, hipStream_t stream) {
-  hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a);
-  gleam_status st = launch_status("plan_kernel");
-  if (st != GLEAM_OK) return st;
-  hipLaunchKernelGGL((attend_kernel<T, D>), dim3(units), dim3(kThreads), 0, stream, a);
-  if ((st = launch_status("attend_kernel")) != GLEAM_OK) return st;
-  hipLaunchKernelGGL((join_kernel<T, D>), dim3(joins), dim3(kThreads), 0, stream, a);
+gleam_status launch_all(const AttendArgs& a, uint32_t units, hipStream_t stream) {
+  gleam_status st;
+  const uint32_t items = a.n_groups + a.n_seq;
+  if (items > kWaveItems && a.n_seq > 0) {
+    // as few threads as hold the items: a barrier of 16 waves takes longer than one of 4
+    const uint32_t threads = items <= 256 ? 256 : kPlanThreads;
+    hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(threads), 0, stream, a);
+    if ((st = launch_status("plan_kernel")) != GLEAM_OK) return st;
+  }
+  if (units > 0) {
+    hipLaunchKernelGGL((attend_kernel<T, D>), dim3(units), dim3(kThreads), 0, stream, a);
+    if ((st = launch_status("attend_kernel")) != GLEAM_OK) return st;
+  }
+  const uint32_t rows = a.n_tokens * a.q_heads;
+  if (rows <= kWideJoin) {
+    hipLaunchKernelGGL((join_kernel<T, D, true>), dim3(rows), dim3(kThreads), 0, stream, a);
+  } else {
+    constexpr uint32_t per = kThreads / (D / 4);
+    const uint32_t groups = (rows + per - 1) / per;
+    hipLaunchKernelGGL((join_kernel<T, D, false>), dim3(groups < kMostJoins ? groups : kMostJoins), dim3(kThreads), 0,
+                       stream, a);
+  }
   return launch_status("join_kernel");
 }
 
@@ -1119,7 +1302,7 @@ extern "C" gleam_status gleam_prefix_attention(const gleam_kv_pages* kv, const g
   a.prefix_len = b->d_prefix_len;
   a.n_tokens = (uint32_t)b->n_tokens;
   a.n_seq = (uint32_t)b->n_seq;
-  a.n_groups = (uint32_t)b->n_groups;
+  a.n_groups = b->n_seq ? (uint32_t)b->n_groups : 0;
   a.own_width = (uint32_t)b->own_width;
   a.prefix_width = (uint32_t)b->prefix_width;
   a.q_heads = b->q_heads;
@@ -1131,16 +1314,16 @@ extern "C" gleam_status gleam_prefix_attention(const gleam_kv_pages* kv, const g
   a.scale_log2 = b->scale * kLog2e;
   a.out = static_cast<uint8_t*>(d_out);
   a.lse = d_lse;
-  const uint32_t units = (uint32_t)most_units(shape);
-  const uint64_t waves = (b->n_tokens * b->q_heads + kWaves - 1) / kWaves;
-  const uint32_t joins = (uint32_t)(waves < 2048 ? waves : 2048);
+  // no sequences: join_kernel clears all rows; otherwise the first workgroup may leave the plan
+  uint32_t units = b->n_seq ? (uint32_t)most_units(shape) : 0;
+  if (b->n_seq && units == 0) units = 1;
   hipStream_t s = (hipStream_t)stream;
   if (kv->dtype == GLEAM_FP16) {
-    return kv->head_dim == 64    ? launch_all<Fp16, 64>(a, units, joins, s)
-           : kv->head_dim == 128 ? launch_all<Fp16, 128>(a, units, joins, s)
-                                 : launch_all<Fp16, 256>(a, units, joins, s);
+    return kv->head_dim == 64    ? launch_all<Fp16, 64>(a, units, s)
+           : kv->head_dim == 128 ? launch_all<Fp16, 128>(a, units, s)
+                                 : launch_all<Fp16, 256>(a, units, s);
   }
-  return kv->head_dim == 64    ? launch_all<Bf16, 64>(a, units, joins, s)
-         : kv->head_dim == 128 ? launch_all<Bf16, 128>(a, units, joins, s)
-                               : launch_all<Bf16, 256>(a, units, joins, s);
+  return kv->head_dim == 64    ? launch_all<Bf16, 64>(a, units, s)
+         : kv->head_dim == 128 ? launch_all<Bf16, 128>(a, units, s)
+                               : launch_all<Bf16, 256>(a, units, s);
 }

@@ -33,6 +33,7 @@ struct PlanShape {  // what the host knows
   uint64_t n_tokens, n_seq, n_groups;
   uint32_t kv_heads, ratio;  // ratio: query heads per key head
   uint32_t target;           // units wanted: what fills the GPU
+  uint32_t most_steps;       // of an item, from the widths of the page tables
 };
 
 GLEAM_HD uint64_t div_up(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
@@ -71,13 +72,15 @@ GLEAM_HD Cut cut_steps(uint32_t steps, uint32_t most) {
 // The bounds that the launch and the workspace are sized by, from what the host knows.
 //
 // Units: sum of tiles * kv_heads * chunks, where chunks < steps / chunk_steps + 1, so at most
-// target + kv_heads * tiles. Tiles: an item of n rows has at most n / kFewRows + 1 of them, and
+// target + kv_heads * tiles, and at most kv_heads * tiles * most_steps / kMinFewSteps. Tiles: an item of n rows has at most n / kFewRows + 1 of them, and
 // at most n / kTileRows + 2, and a token's rows are in two items at most, its group's and its
 // sequence's.
 GLEAM_HD uint64_t most_units(const PlanShape& s) {
   const uint64_t rows = 2 * s.n_tokens * s.ratio, items = s.n_groups + s.n_seq;
   const uint64_t few = items + rows / kFewRows, tile = 2 * items + rows / kTileRows;
-  return s.target + s.kv_heads * (few < tile ? few : tile);
+  const uint64_t tiles = s.kv_heads * (few < tile ? few : tile);
+  const uint64_t cuts = tiles * div_up(s.most_steps, kMinFewSteps);
+  return s.target + tiles < cuts ? s.target + tiles : cuts;
 }
 
 // Rows of partial results: an item that is cut, or shares its rows with another, has

@@ -58,7 +58,12 @@ int main() {
     units += (uint64_t)tiles_of(rows) * kvh * c.chunks;
     if (it.partial || c.chunks > 1) parts += rows * kvh * c.chunks;
   }
-  PlanShape s{all, ns, ng, (uint32_t)kvh, (uint32_t)ratio, (uint32_t)target};
+  uint64_t longest[2] = {0, 0};
+  for (const It& it : items) {
+    if (steps_of((uint32_t)it.own) > longest[0]) longest[0] = steps_of((uint32_t)it.own);
+    if (steps_of((uint32_t)it.prefix) > longest[1]) longest[1] = steps_of((uint32_t)it.prefix);
+  }
+  PlanShape s{all, ns, ng, (uint32_t)kvh, (uint32_t)ratio, (uint32_t)target, (uint32_t)(longest[0] + longest[1])};
   printf("%llu %llu %llu %llu\n", (unsigned long long)units, (unsigned long long)most_units(s),
          (unsigned long long)parts, (unsigned long long)most_partials(s));
 }
