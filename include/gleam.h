@@ -701,7 +701,8 @@ gleam_status gleam_kv_append(const gleam_kv_pages* kv, const gleam_append* a, vo
  *   d_lse            nullable float[n_tokens][q_heads]
  *   d_ws             device, 256-byte aligned, >= gleam_prefix_attention_ws_bytes(kv, b)
  * Errors: GLEAM_E_INVALID, GLEAM_E_WORKSPACE, GLEAM_E_UNSUPPORTED (n_tokens * q_heads of 2^31
- * or more, more than 2^20 sequences or groups), GLEAM_E_HIP. gleam_prefix_attention_ws_bytes
+ * or more, more than 2^20 sequences or groups, places of a page 2^26 elements apart or more),
+ * GLEAM_E_HIP. gleam_prefix_attention_ws_bytes
  * returns 0 for arguments the call refuses; it depends on the shapes, not on pointers.
  */
 typedef struct gleam_prefix_batch {

@@ -35,6 +35,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kPlanThreads = 1024;
+constexpr float kRise = 8.f;  // log2
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr uint64_t kMostSeq = 1ull << 20;
 constexpr uint32_t kWideJoin = 4096;   // up to this many rows are joined by a workgroup each
@@ -831,6 +832,13 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
 
   // the wave's rows of a sub-step, from memory to registers and from there to LDS
   u32x4v stage_k[St::kLoads], stage_v[St::kLoads];
+  uint32_t k_off[St::kLoads], v_off[St::kLoads];
+#pragma unroll
+  for (int i = 0; i < St::kLoads; ++i) {
+    const uint32_t r = (i * 64 + lane) / St::kPieces, piece = (i * 64 + lane) % St::kPieces;
+    k_off[i] = r * (uint32_t)a.k_place + piece * 16;
+    v_off[i] = r * (uint32_t)a.v_place + piece * 16;
+  }
   uint32_t stage_flags = 0;  // 1: values were cleared; from bit 8 on how many of the rows exist
   auto stage_load = [&](uint32_t s) {
     const bool shared = s < prefix_subs;
@@ -838,13 +846,20 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
     const uint32_t keys = shared ? it.prefix_keys : it.own_keys;
     const Keys16 t = keys16(a, shared ? prefix_pages : own_pages, key, keys, head);
     stage_flags = (t.n < (uint32_t)St::kRows ? t.n : (uint32_t)St::kRows) << 8;
+    if (t.n >= (uint32_t)St::kRows) {  // no branch in a lane, and addresses that are a base and the lane's offset
 #pragma unroll
-    for (int i = 0; i < St::kLoads; ++i) {
-      const uint32_t r = (i * 64 + lane) / St::kPieces, piece = (i * 64 + lane) % St::kPieces;
-      stage_k[i] = stage_v[i] = (u32x4v)0u;
-      if (r < t.n) {
-        stage_k[i] = *reinterpret_cast<const u32x4v*>(t.k + (int64_t)r * a.k_place + piece * 16);
-        stage_v[i] = *reinterpret_cast<const u32x4v*>(t.v + (int64_t)r * a.v_place + piece * 16);
+      for (int i = 0; i < St::kLoads; ++i) {
+        stage_k[i] = *reinterpret_cast<const u32x4v*>(t.k + k_off[i]);
+        stage_v[i] = *reinterpret_cast<const u32x4v*>(t.v + v_off[i]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < St::kLoads; ++i) {
+        stage_k[i] = stage_v[i] = (u32x4v)0u;
+        if ((i * 64 + lane) / St::kPieces < t.n) {
+          stage_k[i] = *reinterpret_cast<const u32x4v*>(t.k + k_off[i]);
+          stage_v[i] = *reinterpret_cast<const u32x4v*>(t.v + v_off[i]);
+        }
       }
     }
   };
@@ -939,7 +954,9 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
 #pragma unroll
         for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
       top = max_halves(top);
-      if (__any(top > m)) {
+      // m need not be the maximum itself: it follows once some score is kRise above it (of 2^kRise
+      // no 32-bit sum takes harm), which spares most steps the rescaling
+      if (__any((top - m) * scale > kRise || (m == -INFINITY && top > m))) {
         const float m_new = fmaxf(m, top);
         const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - m_new) * scale);
         m = m_new;
@@ -1181,6 +1198,11 @@ gleam_status validate_attention(const gleam_kv_pages* kv, const gleam_prefix_bat
   if (b->q_heads == 0 || b->q_heads % kv->kv_heads != 0 || b->q_heads > 65535) {
     set_error("%s: q_heads must be a multiple of kv_heads, up to 65535", who);
     return GLEAM_E_INVALID;
+  }
+  // places of 16 keys are reached by 32-bit offsets
+  if (kv->k_stride[1] >= 1 << 26 || kv->v_stride[1] >= 1 << 26) {
+    set_error("%s: places of a page 2^26 elements apart or more", who);
+    return GLEAM_E_UNSUPPORTED;
   }
   if (b->n_tokens > (uint64_t)INT32_MAX / b->q_heads) {
     set_error("%s: n_tokens * q_heads of 2^31 or more", who);
