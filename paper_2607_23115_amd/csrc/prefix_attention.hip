@@ -26,6 +26,8 @@
 //           row and transposed within the lane.
 // With few rows this is bound by reading the keys and values once.
 
+#include <type_traits>
+
 #include "kv_pages.h"
 #include "launch_shape.h"
 #include "prefix_plan.h"
@@ -33,7 +35,11 @@
 namespace gleam {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kThreads = 256, kWaves = kThreads / 64;  // of a unit of few rows, and of join_kernel
+// Waves of a workgroup of attend_kernel: as many as the registers of a CU hold (256 a lane, and
+// twice as many for heads of 256).
+template <int D>
+constexpr int kTileWaves = D == 256 ? 4 : 8;
 constexpr int kPlanThreads = 1024;
 constexpr float kRise = 8.f;  // log2
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
@@ -46,14 +52,15 @@ struct Item {
   uint32_t prefix_row, prefix_keys;  // the shared pages' row of the table and how many keys; 0: none
   uint32_t own_row, own_keys;        // the sequence's own
   uint32_t chunks, per;              // chunks and steps of each; 0: no keys at all
-  uint32_t unit_first, part_first;   // the first unit, the first row of partial results
+  uint32_t tile_first, few_first;    // units of full tiles and of few rows before it: its own first
+  uint32_t part_first;               // the first row of partial results
   uint32_t partial;                  // results go to the workspace
-  uint32_t pad[5];
+  uint32_t pad[4];
 };
 
 struct PlanHeader {
-  uint32_t units;
-  uint32_t joins;  // some row needs join_kernel
+  uint32_t tiles, fews;  // units of the two kinds
+  uint32_t joins;        // some row needs join_kernel
 };
 
 struct Ws {  // device addresses within the workspace
@@ -61,7 +68,8 @@ struct Ws {  // device addresses within the workspace
   int32_t* q_first;      // [n_seq + 1] as used: clamped, non-decreasing
   int32_t* group_first;  // [n_groups + 1]
   int32_t* seq_group;    // [n_seq], -1: none
-  uint32_t* unit_first;  // [n_groups + n_seq + 1]
+  uint32_t* tile_first;  // [n_groups + n_seq], of the items
+  uint32_t* few_first;
   Item* items;           // groups, then sequences
   float* part_o;         // [partials][head_dim]
   float* part_ml;        // [partials][2]: m (log2), l
@@ -81,7 +89,7 @@ struct AttendArgs {
   const int32_t* prefix_pages;
   const int32_t* prefix_len;
   uint32_t n_tokens, n_seq, n_groups, own_width, prefix_width;
-  uint32_t q_heads, kv_heads, ratio, page_log2, n_pages, target;
+  uint32_t q_heads, kv_heads, ratio, page_log2, n_pages, target, tile_waves;
   float scale_log2;
   uint8_t* out;
   float* lse;
@@ -101,7 +109,8 @@ Ws ws_at(uint8_t* base, const PlanShape& s, uint32_t head_dim) {
   w.q_first = reinterpret_cast<int32_t*>(take((s.n_seq + 1) * 4));
   w.group_first = reinterpret_cast<int32_t*>(take((s.n_groups + 1) * 4));
   w.seq_group = reinterpret_cast<int32_t*>(take(s.n_seq * 4));
-  w.unit_first = reinterpret_cast<uint32_t*>(take((items + 1) * 4));
+  w.tile_first = reinterpret_cast<uint32_t*>(take(items * 4));
+  w.few_first = reinterpret_cast<uint32_t*>(take(items * 4));
   w.items = reinterpret_cast<Item*>(take(items * sizeof(Item)));
   w.part_o = reinterpret_cast<float*>(take(partials * head_dim * 4));
   w.part_ml = reinterpret_cast<float*>(take(partials * 8));
@@ -218,16 +227,19 @@ __device__ inline uint32_t item_steps(const Item& it) {
   return it.tokens ? steps_of(it.prefix_keys) + steps_of(it.own_keys) : 0;
 }
 
-// Cuts an item, cost being all items'; its units and rows of partial results, as one number (both
-// sums stay below 2^32: most_units, most_partials).
-__device__ inline uint64_t cut_item(const AttendArgs& a, Item& it, uint64_t cost) {
+// What an item takes, once cut (cost: all items'): units of the two kinds, rows of partial results.
+// The sums over all items stay below 2^32 (most_units, most_partials).
+struct Takes {
+  uint32_t tiles, fews, parts;
+};
+__device__ inline Takes cut_item(const AttendArgs& a, Item& it, uint64_t cost) {
   const uint32_t rows = it.tokens * a.ratio;
-  const Cut cut = cut_steps(item_steps(it), chunk_steps(rows, cost, a.target));
+  const Cut cut = cut_steps(item_steps(it), chunk_steps(rows, cost, a.target, a.tile_waves));
   it.chunks = cut.chunks;
   it.per = cut.per;
   if (cut.chunks > 1) it.partial = 1;
-  const uint64_t parts = it.partial ? (uint64_t)it.tokens * a.q_heads * cut.chunks : 0;
-  return (uint64_t)(tiles_of(rows) * a.kv_heads * cut.chunks) << 32 | parts;
+  const uint32_t units = tiles_of(rows, a.tile_waves) * a.kv_heads * cut.chunks;
+  return {few_rows(rows) ? 0 : units, few_rows(rows) ? units : 0, it.partial ? it.tokens * a.q_heads * cut.chunks : 0};
 }
 
 // The plan of a batch of up to 63 items as every wave has it: item i in lane i.
@@ -237,7 +249,7 @@ struct WavePlan {
   Item it;          // of the lane
   int32_t q;        // tidy offset, of the lane
   int32_t group;    // of sequence `lane`
-  uint32_t units, joins;
+  uint32_t tiles, fews, joins;
 };
 
 __device__ WavePlan plan_in_wave(const AttendArgs& a) {
@@ -262,14 +274,16 @@ __device__ WavePlan plan_in_wave(const AttendArgs& a) {
   w.it = make_item(a, lane, of(q), of(g), of(own), of(prefix), of(w.group));
   if (lane >= n_items) w.it = Item{};
   const uint32_t steps = item_steps(w.it);
-  const uint64_t cost = wave_scan(item_cost(w.it.tokens * a.ratio, steps) * a.kv_heads, SumOp());
-  const uint64_t mine = cut_item(a, w.it, __shfl(cost, 63, 64));
-  const uint64_t sum = wave_scan(mine, SumOp());
-  w.it.unit_first = (uint32_t)((sum - mine) >> 32);
-  w.it.part_first = (uint32_t)(sum - mine);
-  w.units = (uint32_t)(__shfl(sum, 63, 64) >> 32);
+  const uint64_t cost = wave_scan(item_cost(w.it.tokens * a.ratio, steps, a.tile_waves) * a.kv_heads, SumOp());
+  const Takes mine = cut_item(a, w.it, __shfl(cost, 63, 64));
+  const uint32_t tiles = wave_scan(mine.tiles, SumOp()), fews = wave_scan(mine.fews, SumOp());
+  w.it.tile_first = tiles - mine.tiles;
+  w.it.few_first = fews - mine.fews;
+  w.it.part_first = wave_scan(mine.parts, SumOp()) - mine.parts;
+  w.tiles = (uint32_t)__builtin_amdgcn_readlane((int)tiles, 63);
+  w.fews = (uint32_t)__builtin_amdgcn_readlane((int)fews, 63);
   const bool empty = lane >= a.n_groups && w.it.tokens && steps == 0;
-  w.joins = __any(empty || (uint32_t)mine != 0) || __shfl(q, 0, 64) > 0 ||
+  w.joins = __any(empty || mine.parts != 0) || __shfl(q, 0, 64) > 0 ||
             __shfl(q, (int)a.n_seq, 64) < (int32_t)a.n_tokens;
   return w;
 }
@@ -284,6 +298,9 @@ __device__ inline void write_plan(const AttendArgs& a, const WavePlan& plan) {
   if (lane == 0) w.head->joins = plan.joins;
 }
 
+// Of a value that is the same in all lanes: kept in a scalar register, branches on it not masked.
+__device__ inline uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+
 // Lane i's item, in all lanes.
 __device__ inline Item item_of_lane(const Item& it, uint32_t i) {
   auto get = [i](uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, (int)i); };
@@ -296,7 +313,8 @@ __device__ inline Item item_of_lane(const Item& it, uint32_t i) {
   r.own_keys = get(it.own_keys);
   r.chunks = get(it.chunks);
   r.per = get(it.per);
-  r.unit_first = get(it.unit_first);
+  r.tile_first = get(it.tile_first);
+  r.few_first = get(it.few_first);
   r.part_first = get(it.part_first);
   r.partial = get(it.partial);
   return r;
@@ -348,7 +366,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a) {
   for (uint32_t i = threadIdx.x; i < n_items; i += blockDim.x) {
     Item it = make_item(a, i, of(q), of(g), of(a.own_len), of(a.prefix_len), group_of);
     const uint32_t steps = item_steps(it);
-    cost += item_cost(it.tokens * a.ratio, steps) * a.kv_heads;
+    cost += item_cost(it.tokens * a.ratio, steps, a.tile_waves) * a.kv_heads;
     if (i >= a.n_groups && it.tokens && steps == 0) joins = 1;
     if (i < blockDim.x) first = it;
     else w.items[i] = it;
@@ -358,7 +376,8 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a) {
   block_scan(cost, lds, &all_cost, SumOp());
 
   // chunks, units and partial rows
-  uint64_t before = 0;
+  Takes before{0, 0, 0};
+  uint32_t* const ldsu = reinterpret_cast<uint32_t*>(lds);
   for (uint32_t i0 = 0; i0 < n_items; i0 += blockDim.x) {
     const uint32_t i = i0 + threadIdx.x;
     Item it = first;
@@ -366,21 +385,25 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a) {
       it = Item{};
       if (i < n_items) it = w.items[i];
     }
-    const uint64_t mine = cut_item(a, it, all_cost);
-    uint64_t total;
-    const uint64_t at = before + block_scan(mine, lds, &total, SumOp()) - mine;
+    const Takes mine = cut_item(a, it, all_cost);
+    Takes total;
+    it.tile_first = before.tiles + block_scan(mine.tiles, ldsu, &total.tiles, SumOp()) - mine.tiles;
+    it.few_first = before.fews + block_scan(mine.fews, ldsu, &total.fews, SumOp()) - mine.fews;
+    it.part_first = before.parts + block_scan(mine.parts, ldsu, &total.parts, SumOp()) - mine.parts;
     if (i < n_items) {
-      it.unit_first = (uint32_t)(at >> 32);
-      it.part_first = (uint32_t)at;
       w.items[i] = it;
-      w.unit_first[i] = it.unit_first;
+      w.tile_first[i] = it.tile_first;
+      w.few_first[i] = it.few_first;
     }
-    joins |= (uint32_t)mine != 0;
-    before += total;
+    joins |= mine.parts != 0;
+    before.tiles += total.tiles;
+    before.fews += total.fews;
+    before.parts += total.parts;
   }
   joins = __syncthreads_or((int)joins);
   if (threadIdx.x == 0) {
-    w.head->units = (uint32_t)(before >> 32);
+    w.head->tiles = before.tiles;
+    w.head->fews = before.fews;
     w.head->joins = joins;
   }
 }
@@ -445,6 +468,14 @@ __device__ inline uint32_t clear_special(uint32_t x) {
   return x & ~((special_bits<T>(x) >> 15) * 0xffffu);
 }
 
+// A number that no cache has a page of.
+constexpr uint32_t kNoPage = ~0u;
+
+// The page of an item's key `key`, of `keys`.
+__device__ inline uint32_t page_at(const AttendArgs& a, const int32_t* pages, uint32_t key, uint32_t keys) {
+  return key < keys ? (uint32_t)pages[key >> a.page_log2] : kNoPage;
+}
+
 // Where the keys from `key` on are, up to the 16 that lie in its page (key a multiple of 8; fewer
 // than 16 are used where it is not one of 16).
 struct Keys16 {
@@ -452,11 +483,9 @@ struct Keys16 {
   const uint8_t* v;
   uint32_t n;  // how many of them exist
 };
-__device__ inline Keys16 keys16(const AttendArgs& a, const int32_t* pages, uint32_t key, uint32_t keys, uint32_t head) {
+__device__ inline Keys16 keys16(const AttendArgs& a, uint32_t page, uint32_t key, uint32_t keys, uint32_t head) {
   Keys16 t{a.k, a.v, 0};
-  if (key >= keys) return t;
-  const uint32_t page = (uint32_t)pages[key >> a.page_log2];
-  if (page >= a.n_pages) return t;
+  if (page >= a.n_pages || key >= keys) return t;
   const uint32_t place = key & ((1u << a.page_log2) - 1);
   t.k = a.k + (int64_t)page * a.k_page + (int64_t)place * a.k_place + (int64_t)head * a.k_head;
   t.v = a.v + (int64_t)page * a.v_page + (int64_t)place * a.v_place + (int64_t)head * a.v_head;
@@ -481,13 +510,27 @@ __device__ inline void add_special(const uint8_t* v, const Add& add) {
   }
 }
 
+// max and sum of a lane's value and that of the lane 32 away, max also of the lane 16 away
+__device__ inline float max_rows(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float max_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float sum_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 // A unit, as its workgroup finds it.
 struct Unit {
   Item it;
   uint32_t head, chunk, tile;
 };
 
-// 16 rows, the waves taking turns at the keys.
+// 16 rows, four waves taking turns at the keys; one barrier, which a workgroup's other four pass too.
 template <class T, int D>
 __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit, char* lds) {
   typedef typename T::scalar scalar;
@@ -505,7 +548,8 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
   const uint32_t rows = it.tokens * a.ratio;
   const Ws& w = a.ws;
 
-  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const uint32_t lane = threadIdx.x & 63, thread = threadIdx.x % kThreads;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane((int)(thread >> 6));
   const uint32_t n = lane & 15, g = lane >> 4;
   const uint32_t row = tile * kFewRows + n;
   const bool row_live = row < rows;
@@ -545,53 +589,92 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
 #pragma unroll
   for (int j = 0; j < kDims; ++j) o[j] = (f32x4)0.f;
 
-  for (uint32_t half = 2 * chunk * it.per + wave; half < end; half += kWaves) {
-    const bool shared = half < prefix_halves;
-    const uint32_t key = 32 * (shared ? half : half - prefix_halves);
-    const uint32_t keys = shared ? it.prefix_keys : it.own_keys;
-    const int32_t* pages = shared ? prefix_pages : own_pages;
-    const Keys16 t[2] = {keys16(a, pages, key, keys, head), keys16(a, pages, key + 16, keys, head)};
+  const uint32_t begin = 2 * chunk * it.per + wave;
+  auto keys_of = [&](uint32_t half) { return half < prefix_halves ? it.prefix_keys : it.own_keys; };
+  auto key_of = [&](uint32_t half) { return 32 * (half < prefix_halves ? half : half - prefix_halves); };
 
-    Pack8 kk[2][kKMfma];
+  // Pages ahead: lane 2 i has that of the first 16 keys of the wave's i-th half from page_half on,
+  // lane 2 i + 1 that of the others. A half's keys wait for no look-up of their own.
+  auto pages_from = [&](uint32_t half) {
+    half += (lane >> 1) * kWaves;
+    if (half >= end) return kNoPage;
+    return page_at(a, half < prefix_halves ? prefix_pages : own_pages, key_of(half) + 16 * (lane & 1), keys_of(half));
+  };
+  uint32_t page_half = begin, pages = pages_from(begin);
+
+  // The keys and values of two halves: those of the next are on their way during the products.
+  u32x4v kk[2][2][kKMfma];
+  uint32_t vv[2][8][kWords], exist[2][2];
+  const uint32_t k_off = n * (uint32_t)a.k_place + g * 16;
+  uint32_t v_off[4];
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+  for (int e = 0; e < 4; ++e) v_off[e] = (4 * g + e) * (uint32_t)a.v_place + n * (kDims * 2);
+  auto load_v = [&](uint32_t (&to)[kWords], const uint8_t* p) {
+    if constexpr (kDims == 4) {
+      const u32x2v x = *reinterpret_cast<const u32x2v*>(p);
+      to[0] = x[0];
+      to[1] = x[1];
+    } else {
 #pragma unroll
-      for (int i = 0; i < kKMfma; ++i) {
-        kk[b][i].u = (u32x4v)0u;
-        if (n < t[b].n)
-          kk[b][i].u = *reinterpret_cast<const u32x4v*>(t[b].k + (int64_t)n * a.k_place + (i * 32 + g * 8) * 2);
+      for (int c = 0; c < kDims / 8; ++c) {
+        const u32x4v x = *reinterpret_cast<const u32x4v*>(p + 16 * c);
+#pragma unroll
+        for (int d = 0; d < 4; ++d) to[4 * c + d] = x[d];
       }
-    uint32_t vv[8][kWords];
+    }
+  };
+  auto load_half = [&](uint32_t half, auto set_) {
+    constexpr int set = decltype(set_)::value;
+    if (half - page_half >= 32 * kWaves) {
+      page_half = half;
+      pages = pages_from(half);
+    }
+    const uint32_t at = (half - page_half) / kWaves * 2;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t r = 4 * g + (e & 3);
-      const bool live = r < t[e >> 2].n;
-      const uint8_t* p = t[e >> 2].v + (int64_t)r * a.v_place + n * (kDims * 2);
-      if constexpr (kDims == 4) {
-        u32x2v x = (u32x2v)0u;
-        if (live) x = *reinterpret_cast<const u32x2v*>(p);
-        vv[e][0] = x[0];
-        vv[e][1] = x[1];
+    for (int b = 0; b < 2; ++b) {
+      const uint32_t page = (uint32_t)__builtin_amdgcn_readlane((int)pages, (int)(at + b));
+      const Keys16 t = keys16(a, page, key_of(half) + 16 * b, keys_of(half), head);
+      exist[set][b] = t.n;
+      if (t.n == 16) {
+#pragma unroll
+        for (int i = 0; i < kKMfma; ++i) kk[set][b][i] = *reinterpret_cast<const u32x4v*>(t.k + k_off + i * 64);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) load_v(vv[set][4 * b + e], t.v + v_off[e]);
       } else {
 #pragma unroll
-        for (int c = 0; c < kDims / 8; ++c) {
-          u32x4v x = (u32x4v)0u;
-          if (live) x = *reinterpret_cast<const u32x4v*>(p + 16 * c);
+        for (int i = 0; i < kKMfma; ++i) {
+          kk[set][b][i] = (u32x4v)0u;
+          if (n < t.n) kk[set][b][i] = *reinterpret_cast<const u32x4v*>(t.k + k_off + i * 64);
+        }
 #pragma unroll
-          for (int d = 0; d < 4; ++d) vv[e][4 * c + d] = x[d];
+        for (int e = 0; e < 4; ++e) {
+#pragma unroll
+          for (int c = 0; c < kWords; ++c) vv[set][4 * b + e][c] = 0;
+          if (4 * g + e < t.n) load_v(vv[set][4 * b + e], t.v + v_off[e]);
         }
       }
     }
+  };
 
+  auto do_half = [&](uint32_t half, auto set_) {
+    constexpr int set = decltype(set_)::value;
+    typedef std::integral_constant<int, 1 - set> Other;
+    if (half + kWaves < end) load_half(half + kWaves, Other());
+    const bool shared = half < prefix_halves;
+    const uint32_t key = key_of(half);
     f32x4 s[2] = {(f32x4)0.f, (f32x4)0.f};
 #pragma unroll
     for (int i = 0; i < kKMfma; ++i) {
-      s[0] = Mfma<T>::run(get(kk[0][i], T()), get(q[i], T()), s[0]);
-      s[1] = Mfma<T>::run(get(kk[1][i], T()), get(q[i], T()), s[1]);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        Pack8 k;
+        k.u = kk[set][b][i];
+        s[b] = Mfma<T>::run(get(k, T()), get(q[i], T()), s[b]);
+      }
     }
     // whether some row of the tile must not see some key of these 32
     const uint32_t least = shared ? it.prefix_keys : own_least;
-    const bool masked = key + 32 > least || t[0].n < 16 || t[1].n < 16;
+    const bool masked = key + 32 > least || exist[set][0] + exist[set][1] < 32;
     const uint32_t seen = shared ? it.prefix_keys : own_seen;
     float x[8], top = -INFINITY;
 #pragma unroll
@@ -599,17 +682,22 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
       x[e] = s[e >> 2][e & 3] * a.scale_log2;
       if (masked) {
         const uint32_t r = 4 * g + (e & 3);
-        if (key + (e >> 2) * 16 + r >= seen || r >= t[e >> 2].n) x[e] = -INFINITY;
+        if (key + (e >> 2) * 16 + r >= seen || r >= exist[set][e >> 2]) x[e] = -INFINITY;
       }
       top = fmaxf(top, x[e]);
     }
-    top = fmaxf(top, __shfl_xor(top, 16, 64));
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
-    const float m_new = fmaxf(m, top);
-    const float m_use = m_new == -INFINITY ? 0.f : m_new;  // nothing seen so far: all exponentials are 0
-    const float alpha = __builtin_amdgcn_exp2f(m - m_use);
-    m = m_new;
-    l *= alpha;
+    top = max_halves(max_rows(top));
+    // m need not be the maximum itself: it follows once some score is kRise above it (of 2^kRise
+    // no 32-bit sum takes harm), which spares most steps the rescaling
+    if (__any(top > m + kRise || (m == -INFINITY && top > m))) {
+      const float m_new = fmaxf(m, top);
+      const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int j = 0; j < kDims; ++j) o[j] *= alpha;
+    }
+    const float m_use = m == -INFINITY ? 0.f : m;  // nothing seen so far: all exponentials are 0
     Pack8 p;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -617,22 +705,18 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
       l += y;
       put(p, e, y, T());
     }
-    if (__any(alpha != 1.f)) {
-#pragma unroll
-      for (int j = 0; j < kDims; ++j) o[j] *= alpha;
-    }
     if (!shared && masked) {
       uint32_t any = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e)
 #pragma unroll
-        for (int c = 0; c < kWords; ++c) any |= special_bits<T>(vv[e][c]);
+        for (int c = 0; c < kWords; ++c) any |= special_bits<T>(vv[set][e][c]);
       if (__any(any != 0)) {
         special = true;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
 #pragma unroll
-          for (int c = 0; c < kWords; ++c) vv[e][c] = clear_special<T>(vv[e][c]);
+          for (int c = 0; c < kWords; ++c) vv[set][e][c] = clear_special<T>(vv[set][e][c]);
       }
     }
 #pragma unroll
@@ -640,19 +724,27 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
       Pack8 lo, hi;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        lo.u[e] = __builtin_amdgcn_perm(vv[2 * e + 1][c], vv[2 * e][c], 0x05040100u);
-        hi.u[e] = __builtin_amdgcn_perm(vv[2 * e + 1][c], vv[2 * e][c], 0x07060302u);
+        lo.u[e] = __builtin_amdgcn_perm(vv[set][2 * e + 1][c], vv[set][2 * e][c], 0x05040100u);
+        hi.u[e] = __builtin_amdgcn_perm(vv[set][2 * e + 1][c], vv[set][2 * e][c], 0x07060302u);
       }
       o[2 * c] = Mfma<T>::run(get(lo, T()), get(p, T()), o[2 * c]);
       o[2 * c + 1] = Mfma<T>::run(get(hi, T()), get(p, T()), o[2 * c + 1]);
     }
+  };
+  typedef std::integral_constant<int, 0> Even;
+  typedef std::integral_constant<int, 1> Odd;
+  if (begin < end) load_half(begin, Even());
+  for (uint32_t half = begin; half < end; half += 2 * kWaves) {
+    do_half(half, Even());
+    if (half + kWaves < end) do_half(half + kWaves, Odd());
   }
   if (special) {  // the same halves again: those that were looked at
-    for (uint32_t half = 2 * chunk * it.per + wave; half < end; half += kWaves) {
+    for (uint32_t half = begin; half < end; half += kWaves) {
       const uint32_t key = 32 * (half - prefix_halves);
       if (half < prefix_halves || key + 32 <= own_least) continue;
       for (uint32_t i = 0; i < 32; ++i) {
-        const Keys16 t = keys16(a, own_pages, key + (i & 16), it.own_keys, head);
+        const uint32_t first = key + (i & 16);
+        const Keys16 t = keys16(a, page_at(a, own_pages, first, it.own_keys), first, it.own_keys, head);
         if ((i & 15) >= t.n || key + i >= own_seen) continue;
         const uint8_t* const v = t.v + (int64_t)(i & 15) * a.v_place;
 #pragma unroll
@@ -678,7 +770,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
     }
   __syncthreads();
   constexpr int kQuads = D / 4;
-  for (int i = threadIdx.x; i < (int)kFewRows * kQuads; i += kThreads) {
+  for (int i = thread; i < (int)kFewRows * kQuads; i += kThreads) {
     const uint32_t rr = i / kQuads, c = i % kQuads, in = tile * kFewRows + rr;
     if (in >= rows) continue;
     float top = -INFINITY;
@@ -714,7 +806,8 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
   }
 }
 
-// 128 rows, 32 a wave, over keys that the workgroup stages in LDS, one sub-step ahead.
+// 32 rows a wave, over keys that the workgroup stages in LDS: a sub-step's keys are loaded into
+// registers three sub-steps ahead, and stored one ahead.
 //
 // Products are v_mfma_f32_32x32x16 in the same orientation: S^T = K Q^T, O^T = V^T P^T, a lane
 // holding one row's scores with keys 8 i + 4 h .. + 3 (h = lane / 32), which again are P's operand
@@ -729,10 +822,10 @@ struct Staged {
   static constexpr int kSubs = kStep / kKeys;           // sub-steps of a step
   static constexpr int kRow = 2 * D;                    // bytes of a row
   static constexpr int kPieces = kRow / 16;             // 16-byte pieces of a row
-  static constexpr int kRows = kKeys / kWaves;          // rows that a wave stages
+  static constexpr int kRows = kKeys / kTileWaves<D>;   // rows that a wave stages
   static constexpr int kLoads = kRows * kPieces / 64;   // 16-byte loads of a lane for them
   static constexpr int kTile = kKeys * kRow;            // bytes of K or V
-  static constexpr int kBytes = 4 * kTile + 2 * kWaves * 4;  // two of each, and flags
+  static constexpr int kBytes = 4 * kTile + 2 * 8;      // two of each, and flags
   static __device__ uint32_t k_at(uint32_t row, uint32_t piece) {
     return row * kRow + ((piece ^ (D == 64 ? (row >> 1) & 7 : row & 15)) << 4);
   }
@@ -767,16 +860,6 @@ __device__ inline u32x2v read_transposed(const char* p) {
   return x.u;
 }
 
-// max and sum of a lane's value and that of the lane 32 away
-__device__ inline float max_halves(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ inline float sum_halves(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
 template <class T, int D>
 __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& unit, char* lds) {
   typedef typename T::scalar scalar;
@@ -784,7 +867,11 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
   constexpr int kKTiles = St::kKeys / 32, kQ = D / 16, kO = D / 32;
   char* const lds_k = lds;
   char* const lds_v = lds + 2 * St::kTile;
-  uint32_t* const lds_flags = reinterpret_cast<uint32_t*>(lds + 4 * St::kTile);
+  uint8_t* const lds_flags = reinterpret_cast<uint8_t*>(lds + 4 * St::kTile);
+  constexpr uint32_t kTileRows = 32 * kTileWaves<D>;
+  // of a wave's staged rows: how many exist, in a byte, 0x80 added where values were cleared
+  constexpr uint32_t kWhole = St::kRows * 0x01010101u, kCleared = 0x80808080u;
+  static_assert(St::kRows == 8, "a quad of keys belongs to one wave's rows");
   const Item& it = unit.it;
   const uint32_t head = unit.head, rows = it.tokens * a.ratio;
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -803,10 +890,10 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
     const int64_t x = behind + r / a.ratio;
     return x < 0 ? 0u : (uint32_t)x;
   };
-  const uint32_t own_seen = seen_by(row), own_least = seen_by(wave_row);
-  const uint32_t own_wave_most = wave_row < rows ? seen_by(wave_row + 31) : 0;
-  const uint32_t own_group_least = seen_by(unit.tile * kTileRows);
-  const uint32_t own_most = seen_by(unit.tile * kTileRows + kTileRows - 1);
+  const uint32_t own_seen = seen_by(row), own_least = uniform(seen_by(wave_row));
+  const uint32_t own_wave_most = uniform(wave_row < rows ? seen_by(wave_row + 31) : 0);
+  const uint32_t own_group_least = uniform(seen_by(unit.tile * kTileRows));
+  const uint32_t own_most = uniform(seen_by(unit.tile * kTileRows + kTileRows - 1));
 
   // Scores are scaled after the product; a scale below zero is taken from the queries' signs, so
   // that the largest score is the largest product's.
@@ -830,8 +917,22 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
   if (end > all_subs) end = all_subs;
   uint32_t sub = St::kSubs * unit.chunk * it.per;
 
-  // the wave's rows of a sub-step, from memory to registers and from there to LDS
-  u32x4v stage_k[St::kLoads], stage_v[St::kLoads];
+  // of the wave's rows of a sub-step the first key, and all keys there are; its page for the 64
+  // sub-steps from page_sub on, one a lane
+  auto keys_of = [&](uint32_t s) { return s < prefix_subs ? it.prefix_keys : it.own_keys; };
+  auto key_of = [&](uint32_t s) {
+    return (s < prefix_subs ? s : s - prefix_subs) * St::kKeys + wave * St::kRows;
+  };
+  auto pages_from = [&](uint32_t s) {
+    s += lane;
+    if (s >= end) return kNoPage;
+    return page_at(a, s < prefix_subs ? prefix_pages : own_pages, key_of(s), keys_of(s));
+  };
+  uint32_t page_sub = sub, pages = pages_from(sub);
+
+  // those rows, from memory to registers and from there to LDS
+  u32x4v stage_k[2][St::kLoads], stage_v[2][St::kLoads];
+  uint32_t stage_flags[2];
   uint32_t k_off[St::kLoads], v_off[St::kLoads];
 #pragma unroll
   for (int i = 0; i < St::kLoads; ++i) {
@@ -839,52 +940,55 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
     k_off[i] = r * (uint32_t)a.k_place + piece * 16;
     v_off[i] = r * (uint32_t)a.v_place + piece * 16;
   }
-  uint32_t stage_flags = 0;  // 1: values were cleared; from bit 8 on how many of the rows exist
-  auto stage_load = [&](uint32_t s) {
-    const bool shared = s < prefix_subs;
-    const uint32_t key = (shared ? s : s - prefix_subs) * St::kKeys + wave * St::kRows;
-    const uint32_t keys = shared ? it.prefix_keys : it.own_keys;
-    const Keys16 t = keys16(a, shared ? prefix_pages : own_pages, key, keys, head);
-    stage_flags = (t.n < (uint32_t)St::kRows ? t.n : (uint32_t)St::kRows) << 8;
+  auto stage_load = [&](uint32_t s, auto set_) {
+    constexpr int set = decltype(set_)::value;
+    if (s - page_sub >= 64) {
+      page_sub = s;
+      pages = pages_from(s);
+    }
+    const uint32_t page = (uint32_t)__builtin_amdgcn_readlane((int)pages, (int)(s - page_sub));
+    const Keys16 t = keys16(a, page, key_of(s), keys_of(s), head);
+    stage_flags[set] = t.n < (uint32_t)St::kRows ? t.n : (uint32_t)St::kRows;
     if (t.n >= (uint32_t)St::kRows) {  // no branch in a lane, and addresses that are a base and the lane's offset
 #pragma unroll
       for (int i = 0; i < St::kLoads; ++i) {
-        stage_k[i] = *reinterpret_cast<const u32x4v*>(t.k + k_off[i]);
-        stage_v[i] = *reinterpret_cast<const u32x4v*>(t.v + v_off[i]);
+        stage_k[set][i] = *reinterpret_cast<const u32x4v*>(t.k + k_off[i]);
+        stage_v[set][i] = *reinterpret_cast<const u32x4v*>(t.v + v_off[i]);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < St::kLoads; ++i) {
-        stage_k[i] = stage_v[i] = (u32x4v)0u;
+        stage_k[set][i] = stage_v[set][i] = (u32x4v)0u;
         if ((i * 64 + lane) / St::kPieces < t.n) {
-          stage_k[i] = *reinterpret_cast<const u32x4v*>(t.k + k_off[i]);
-          stage_v[i] = *reinterpret_cast<const u32x4v*>(t.v + v_off[i]);
+          stage_k[set][i] = *reinterpret_cast<const u32x4v*>(t.k + k_off[i]);
+          stage_v[set][i] = *reinterpret_cast<const u32x4v*>(t.v + v_off[i]);
         }
       }
     }
   };
-  auto stage_store = [&](uint32_t s, uint32_t buf) {
+  auto stage_store = [&](uint32_t s, auto set_) {  // into the buffer of the same number
+    constexpr int set = decltype(set_)::value;
     if (s >= prefix_subs && (s - prefix_subs + 1) * St::kKeys > own_group_least) {
       uint32_t any = 0;
 #pragma unroll
       for (int i = 0; i < St::kLoads; ++i)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) any |= special_bits<T>(stage_v[i][c]);
+        for (int c = 0; c < 4; ++c) any |= special_bits<T>(stage_v[set][i][c]);
       if (__any(any != 0)) {
-        stage_flags |= 1;
+        stage_flags[set] |= 0x80;
 #pragma unroll
         for (int i = 0; i < St::kLoads; ++i)
 #pragma unroll
-          for (int c = 0; c < 4; ++c) stage_v[i][c] = clear_special<T>(stage_v[i][c]);
+          for (int c = 0; c < 4; ++c) stage_v[set][i][c] = clear_special<T>(stage_v[set][i][c]);
       }
     }
 #pragma unroll
     for (int i = 0; i < St::kLoads; ++i) {
       const uint32_t r = wave * St::kRows + (i * 64 + lane) / St::kPieces, piece = (i * 64 + lane) % St::kPieces;
-      *reinterpret_cast<u32x4v*>(lds_k + buf * St::kTile + St::k_at(r, piece)) = stage_k[i];
-      *reinterpret_cast<u32x4v*>(lds_v + buf * St::kTile + St::v_at(r, piece)) = stage_v[i];
+      *reinterpret_cast<u32x4v*>(lds_k + set * St::kTile + St::k_at(r, piece)) = stage_k[set][i];
+      *reinterpret_cast<u32x4v*>(lds_v + set * St::kTile + St::v_at(r, piece)) = stage_v[set][i];
     }
-    if (lane == 0) lds_flags[buf * kWaves + wave] = stage_flags;
+    if (lane == 0) lds_flags[set * 8 + wave] = (uint8_t)stage_flags[set];
   };
 
   bool special = false;
@@ -905,27 +1009,34 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
     }
   }
 
+  typedef std::integral_constant<int, 0> Even;
+  typedef std::integral_constant<int, 1> Odd;
   if (sub < end) {
-    stage_load(sub);
-    stage_store(sub, 0);
+    stage_load(sub, Even());
+    if (sub + 1 < end) stage_load(sub + 1, Odd());
+    stage_store(sub, Even());
+    if (sub + 2 < end) stage_load(sub + 2, Even());
   }
-  __syncthreads();
-  for (uint32_t buf = 0; sub < end; ++sub, buf ^= 1) {
-    const bool more = sub + 1 < end;
-    if (more) stage_load(sub + 1);
+  // One barrier a sub-step: what it stores one ahead is complete at the next one's, and goes to the
+  // buffer that all waves were done with at its own.
+  auto sub_step = [&](auto buf_) {
+    constexpr int buf = decltype(buf_)::value;
+    typedef std::integral_constant<int, 1 - buf> Other;
+    __syncthreads();
+    if (sub + 1 < end) stage_store(sub + 1, Other());
+    if (sub + 3 < end) stage_load(sub + 3, Other());
     const bool shared = sub < prefix_subs;
     const uint32_t key = (shared ? sub : sub - prefix_subs) * St::kKeys;
     if (wave_row < rows && (shared || key < own_wave_most)) {
       const char* const kb = lds_k + buf * St::kTile;
       const char* const vb = lds_v + buf * St::kTile;
-      const u32x4v flags4 = *reinterpret_cast<const u32x4v*>(lds_flags + buf * kWaves);
-      uint32_t exist[4];
+      uint32_t flags[2];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const uint32_t f = (uint32_t)__builtin_amdgcn_readfirstlane((int)flags4[c]);
-        exist[c] = f >> 8;
-        special |= f & 1;
-      }
+      for (int c = 0; c < 2; ++c)
+        flags[c] = c * 4 < kTileWaves<D> ? (uint32_t)__builtin_amdgcn_readfirstlane(
+                                               *reinterpret_cast<const int*>(lds_flags + buf * 8 + 4 * c))
+                                         : kWhole;
+      special |= ((flags[0] | flags[1]) & kCleared) != 0;
       f32x16 s[kKTiles];
 #pragma unroll
       for (int t = 0; t < kKTiles; ++t) {
@@ -937,15 +1048,16 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
           s[t] = Mfma32<T>::run(get(k, T()), get(q[i], T()), s[t]);
         }
       }
-      const bool all_exist = exist[0] + exist[1] + exist[2] + exist[3] == (uint32_t)St::kKeys;
+      const bool all_exist = (flags[0] & ~kCleared) == kWhole && (flags[1] & ~kCleared) == kWhole;
       if (!all_exist || (!shared && key + St::kKeys > own_least)) {
         const uint32_t seen = shared ? it.prefix_keys : own_seen;
 #pragma unroll
         for (int t = 0; t < kKTiles; ++t)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const int in = 32 * t + 8 * (r / 4) + r % 4;  // and 4 h on
-            if (key + in + 4 * h >= seen || in % St::kRows + 4 * h >= exist[in / St::kRows]) s[t][r] = -INFINITY;
+            const int w = 4 * t + r / 4;  // the wave that staged the key
+            const uint32_t in = r % 4 + 4 * h, exist = (flags[w / 4] >> (8 * (w % 4))) & 0x7f;
+            if (key + 8 * w + in >= seen || in >= exist) s[t][r] = -INFINITY;
           }
       }
       float top = s[0][0];
@@ -985,8 +1097,11 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
           o[i] = Mfma32<T>::run(get(v, T()), get(p[kk], T()), o[i]);
         }
     }
-    if (more) stage_store(sub + 1, buf ^ 1);
-    __syncthreads();
+    ++sub;
+  };
+  while (sub < end) {
+    sub_step(Even());
+    if (sub < end) sub_step(Odd());
   }
 
   l = sum_halves(l);
@@ -997,7 +1112,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
     if (first > prefix_subs && (first - prefix_subs) * St::kKeys > key) key = (first - prefix_subs) * St::kKeys;
     const uint32_t to = (end - prefix_subs) * St::kKeys;
     for (; key < to && key < own_seen; ++key) {
-      const Keys16 t = keys16(a, own_pages, key & ~15u, it.own_keys, head);
+      const Keys16 t = keys16(a, page_at(a, own_pages, key & ~15u, it.own_keys), key & ~15u, it.own_keys, head);
       if ((key & 15) >= t.n) continue;
       const uint8_t* const v = t.v + (int64_t)(key & 15) * a.v_place + 8 * h;
 #pragma unroll
@@ -1038,42 +1153,67 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
 }
 
 template <int D>
+constexpr int few_lds() {
+  return kWaves * kFewRows * (D + 4 + 2) * 4;
+}
+template <int D>
 constexpr int lds_bytes() {
-  constexpr int few = kWaves * kFewRows * (D + 4 + 2) * 4, tile = Staged<D>::kBytes;
+  constexpr int few = few_lds<D>() * kTileWaves<D> / kWaves, tile = Staged<D>::kBytes;
   return few > tile ? few : tile;
 }
 
 template <class T, int D>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__(64 * kTileWaves<D>, D == 256 ? 1 : 2) void attend_kernel(AttendArgs a) {
   __shared__ __attribute__((aligned(16))) char lds[lds_bytes<D>()];
   const Ws& w = a.ws;
-  const uint32_t n_items = a.n_groups + a.n_seq;
-  Unit unit;
-  if (n_items <= kWaveItems) {
-    const WavePlan plan = plan_in_wave(a);
+  const uint32_t n_items = a.n_groups + a.n_seq, lane = threadIdx.x & 63;
+  const uint32_t half = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kThreads));
+  // workgroups of full tiles come first, then those that take a unit of few rows for every 4 waves
+  uint32_t tiles, fews;
+  WavePlan plan;
+  const bool in_wave = n_items <= kWaveItems;
+  if (in_wave) {
+    plan = plan_in_wave(a);
     if (blockIdx.x == 0 && threadIdx.x < 64) write_plan(a, plan);
-    if (blockIdx.x >= plan.units) return;
-    const uint32_t lane = threadIdx.x & 63;
-    const uint64_t le = __ballot(lane < n_items && plan.it.unit_first <= blockIdx.x);
-    unit.it = item_of_lane(plan.it, 63 - __clzll((long long)le));
+    tiles = plan.tiles;
+    fews = plan.fews;
   } else {
-    if (blockIdx.x >= w.head->units) return;
-    unit.it = w.items[__builtin_amdgcn_readfirstlane((int)wave_search<uint32_t>(w.unit_first, n_items, blockIdx.x))];
+    tiles = w.head->tiles;
+    fews = w.head->fews;
   }
-  const uint32_t rows = unit.it.tokens * a.ratio;
-  uint32_t u = blockIdx.x - unit.it.unit_first;
-  unit.head = u % a.kv_heads;
-  u /= a.kv_heads;
-  unit.chunk = u % unit.it.chunks;
-  // a prompt's last rows see the most keys: they come first
-  unit.tile = tiles_of(rows) - 1 - u / unit.it.chunks;
-  if (rows <= kMostFew) attend_few<T, D>(a, unit, lds);
+  tiles = uniform(tiles);
+  fews = uniform(fews);
+  const bool few = blockIdx.x >= tiles;
+  uint32_t u = blockIdx.x;
+  if (few) {
+    u = (u - tiles) * (kTileWaves<D> / kWaves) + half;
+    if (u - half >= fews) return;
+  }
+  Unit unit{};
+  if (!few || u < fews) {
+    if (in_wave) {
+      const uint64_t le = __ballot(lane < n_items && (few ? plan.it.few_first : plan.it.tile_first) <= u);
+      unit.it = item_of_lane(plan.it, 63 - __clzll((long long)le));
+    } else {
+      const uint32_t* const first = few ? w.few_first : w.tile_first;
+      const uint32_t at = __builtin_amdgcn_readfirstlane((int)wave_search<uint32_t>(first, n_items, u));
+      unit.it = w.items[at];
+    }
+    u -= few ? unit.it.few_first : unit.it.tile_first;
+    unit.head = u % a.kv_heads;
+    u /= a.kv_heads;
+    unit.chunk = u % unit.it.chunks;
+    // a prompt's last rows see the most keys: they come first
+    unit.tile = tiles_of(unit.it.tokens * a.ratio, kTileWaves<D>) - 1 - u / unit.it.chunks;
+  }
+  unit.it = item_of_lane(unit.it, 0);
+  unit.head = uniform(unit.head);
+  unit.chunk = uniform(unit.chunk);
+  unit.tile = uniform(unit.tile);
+  if (few) attend_few<T, D>(a, unit, lds + half * few_lds<D>());
   else attend_tile<T, D>(a, unit, lds);
 }
 
-// --------------------------------------------------------------------------------------- //
-// join
-// --------------------------------------------------------------------------------------- //
 // D/4 lanes take a piece of a row, 4 dims each. Where there are many rows they join all of its
 // pieces, 64 / (D/4) rows a wave; with few rows (kWide) a workgroup's lanes share the pieces of
 // one. Four pieces are in flight at a time. Bound by reading the pieces, or with few by the time
@@ -1222,10 +1362,11 @@ gleam_status validate_attention(const gleam_kv_pages* kv, const gleam_prefix_bat
   shape->kv_heads = kv->kv_heads;
   shape->ratio = b->q_heads / kv->kv_heads;
   shape->target = 1024;
+  shape->tile_waves = kv->head_dim == 256 ? kTileWaves<256> : kTileWaves<128>;
   const uint64_t most = steps_of((uint32_t)(b->own_width * kv->page_tokens)) +
                         (uint64_t)steps_of((uint32_t)(b->prefix_width * kv->page_tokens));
   shape->most_steps = (uint32_t)most;
-  if (most_units(*shape) > max_workgroups(kThreads) || most_partials(*shape) > UINT32_MAX) {
+  if (most_units(*shape) > max_workgroups(512) || most_partials(*shape) > UINT32_MAX) {
     set_error("%s: more work than one launch holds", who);
     return GLEAM_E_UNSUPPORTED;
   }
@@ -1243,7 +1384,7 @@ gleam_status launch_all(const AttendArgs& a, uint32_t units, hipStream_t stream)
     if ((st = launch_status("plan_kernel")) != GLEAM_OK) return st;
   }
   if (units > 0) {
-    hipLaunchKernelGGL((attend_kernel<T, D>), dim3(units), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((attend_kernel<T, D>), dim3(units), dim3(64 * kTileWaves<D>), 0, stream, a);
     if ((st = launch_status("attend_kernel")) != GLEAM_OK) return st;
   }
   const uint32_t rows = a.n_tokens * a.q_heads;
@@ -1333,6 +1474,7 @@ extern "C" gleam_status gleam_prefix_attention(const gleam_kv_pages* kv, const g
   a.page_log2 = (uint32_t)log2_exact(kv->page_tokens);
   a.n_pages = (uint32_t)kv->n_pages;
   a.target = shape.target;
+  a.tile_waves = shape.tile_waves;
   a.scale_log2 = b->scale * kLog2e;
   a.out = static_cast<uint8_t*>(d_out);
   a.lse = d_lse;
