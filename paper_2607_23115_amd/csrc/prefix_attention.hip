@@ -35,11 +35,7 @@
 namespace gleam {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;  // of a unit of few rows, and of join_kernel
-// Waves of a workgroup of attend_kernel: as many as the registers of a CU hold (256 a lane, and
-// twice as many for heads of 256).
-template <int D>
-constexpr int kTileWaves = D == 256 ? 4 : 8;
+constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kPlanThreads = 1024;
 constexpr float kRise = 8.f;  // log2
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
@@ -89,7 +85,7 @@ struct AttendArgs {
   const int32_t* prefix_pages;
   const int32_t* prefix_len;
   uint32_t n_tokens, n_seq, n_groups, own_width, prefix_width;
-  uint32_t q_heads, kv_heads, ratio, page_log2, n_pages, target, tile_waves;
+  uint32_t q_heads, kv_heads, ratio, page_log2, n_pages, target;
   float scale_log2;
   uint8_t* out;
   float* lse;
@@ -234,11 +230,11 @@ struct Takes {
 };
 __device__ inline Takes cut_item(const AttendArgs& a, Item& it, uint64_t cost) {
   const uint32_t rows = it.tokens * a.ratio;
-  const Cut cut = cut_steps(item_steps(it), chunk_steps(rows, cost, a.target, a.tile_waves));
+  const Cut cut = cut_steps(item_steps(it), chunk_steps(rows, cost, a.target));
   it.chunks = cut.chunks;
   it.per = cut.per;
   if (cut.chunks > 1) it.partial = 1;
-  const uint32_t units = tiles_of(rows, a.tile_waves) * a.kv_heads * cut.chunks;
+  const uint32_t units = tiles_of(rows) * a.kv_heads * cut.chunks;
   return {few_rows(rows) ? 0 : units, few_rows(rows) ? units : 0, it.partial ? it.tokens * a.q_heads * cut.chunks : 0};
 }
 
@@ -274,7 +270,7 @@ __device__ WavePlan plan_in_wave(const AttendArgs& a) {
   w.it = make_item(a, lane, of(q), of(g), of(own), of(prefix), of(w.group));
   if (lane >= n_items) w.it = Item{};
   const uint32_t steps = item_steps(w.it);
-  const uint64_t cost = wave_scan(item_cost(w.it.tokens * a.ratio, steps, a.tile_waves) * a.kv_heads, SumOp());
+  const uint64_t cost = wave_scan(item_cost(w.it.tokens * a.ratio, steps) * a.kv_heads, SumOp());
   const Takes mine = cut_item(a, w.it, __shfl(cost, 63, 64));
   const uint32_t tiles = wave_scan(mine.tiles, SumOp()), fews = wave_scan(mine.fews, SumOp());
   w.it.tile_first = tiles - mine.tiles;
@@ -366,7 +362,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a) {
   for (uint32_t i = threadIdx.x; i < n_items; i += blockDim.x) {
     Item it = make_item(a, i, of(q), of(g), of(a.own_len), of(a.prefix_len), group_of);
     const uint32_t steps = item_steps(it);
-    cost += item_cost(it.tokens * a.ratio, steps, a.tile_waves) * a.kv_heads;
+    cost += item_cost(it.tokens * a.ratio, steps) * a.kv_heads;
     if (i >= a.n_groups && it.tokens && steps == 0) joins = 1;
     if (i < blockDim.x) first = it;
     else w.items[i] = it;
@@ -530,7 +526,7 @@ struct Unit {
   uint32_t head, chunk, tile;
 };
 
-// 16 rows, four waves taking turns at the keys; one barrier, which a workgroup's other four pass too.
+// 16 rows, the waves taking turns at the keys.
 template <class T, int D>
 __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit, char* lds) {
   typedef typename T::scalar scalar;
@@ -548,8 +544,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
   const uint32_t rows = it.tokens * a.ratio;
   const Ws& w = a.ws;
 
-  const uint32_t lane = threadIdx.x & 63, thread = threadIdx.x % kThreads;
-  const uint32_t wave = __builtin_amdgcn_readfirstlane((int)(thread >> 6));
+  const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const uint32_t n = lane & 15, g = lane >> 4;
   const uint32_t row = tile * kFewRows + n;
   const bool row_live = row < rows;
@@ -770,7 +765,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
     }
   __syncthreads();
   constexpr int kQuads = D / 4;
-  for (int i = thread; i < (int)kFewRows * kQuads; i += kThreads) {
+  for (int i = threadIdx.x; i < (int)kFewRows * kQuads; i += kThreads) {
     const uint32_t rr = i / kQuads, c = i % kQuads, in = tile * kFewRows + rr;
     if (in >= rows) continue;
     float top = -INFINITY;
@@ -806,8 +801,9 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
   }
 }
 
-// 32 rows a wave, over keys that the workgroup stages in LDS: a sub-step's keys are loaded into
-// registers three sub-steps ahead, and stored one ahead.
+// 128 rows, 32 a wave, over keys that the workgroup stages in LDS: a sub-step's keys are loaded
+// into registers two sub-steps ahead, and stored one ahead. A SIMD has one wave of each of two
+// workgroups: as these share no barrier, the products of one go on under the other's softmax.
 //
 // Products are v_mfma_f32_32x32x16 in the same orientation: S^T = K Q^T, O^T = V^T P^T, a lane
 // holding one row's scores with keys 8 i + 4 h .. + 3 (h = lane / 32), which again are P's operand
@@ -822,10 +818,10 @@ struct Staged {
   static constexpr int kSubs = kStep / kKeys;           // sub-steps of a step
   static constexpr int kRow = 2 * D;                    // bytes of a row
   static constexpr int kPieces = kRow / 16;             // 16-byte pieces of a row
-  static constexpr int kRows = kKeys / kTileWaves<D>;   // rows that a wave stages
+  static constexpr int kRows = kKeys / kWaves;          // rows that a wave stages
   static constexpr int kLoads = kRows * kPieces / 64;   // 16-byte loads of a lane for them
   static constexpr int kTile = kKeys * kRow;            // bytes of K or V
-  static constexpr int kBytes = 4 * kTile + 2 * 8;      // two of each, and flags
+  static constexpr int kBytes = 4 * kTile + 2 * kWaves; // two of each, and flags
   static __device__ uint32_t k_at(uint32_t row, uint32_t piece) {
     return row * kRow + ((piece ^ (D == 64 ? (row >> 1) & 7 : row & 15)) << 4);
   }
@@ -868,13 +864,11 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
   char* const lds_k = lds;
   char* const lds_v = lds + 2 * St::kTile;
   uint8_t* const lds_flags = reinterpret_cast<uint8_t*>(lds + 4 * St::kTile);
-  constexpr uint32_t kTileRows = 32 * kTileWaves<D>;
   // of a wave's staged rows: how many exist, in a byte, 0x80 added where values were cleared
   constexpr uint32_t kWhole = St::kRows * 0x01010101u, kCleared = 0x80808080u;
-  static_assert(St::kRows == 8, "a quad of keys belongs to one wave's rows");
   const Item& it = unit.it;
   const uint32_t head = unit.head, rows = it.tokens * a.ratio;
-  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const uint32_t n = lane & 31, h = lane >> 5;
   const uint32_t wave_row = unit.tile * kTileRows + 32 * wave;
   const uint32_t row = wave_row + n;
@@ -915,7 +909,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
   const uint32_t all_subs = prefix_subs + (own_most + St::kKeys - 1) / St::kKeys;
   uint32_t end = St::kSubs * (unit.chunk + 1) * it.per;
   if (end > all_subs) end = all_subs;
-  uint32_t sub = St::kSubs * unit.chunk * it.per;
+  const uint32_t first = St::kSubs * unit.chunk * it.per;
 
   // of the wave's rows of a sub-step the first key, and all keys there are; its page for the 64
   // sub-steps from page_sub on, one a lane
@@ -928,11 +922,11 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
     if (s >= end) return kNoPage;
     return page_at(a, s < prefix_subs ? prefix_pages : own_pages, key_of(s), keys_of(s));
   };
-  uint32_t page_sub = sub, pages = pages_from(sub);
+  uint32_t page_sub = first, pages = pages_from(first);
 
   // those rows, from memory to registers and from there to LDS
-  u32x4v stage_k[2][St::kLoads], stage_v[2][St::kLoads];
-  uint32_t stage_flags[2];
+  u32x4v stage_k[St::kLoads], stage_v[St::kLoads];
+  uint32_t stage_flags = 0;
   uint32_t k_off[St::kLoads], v_off[St::kLoads];
 #pragma unroll
   for (int i = 0; i < St::kLoads; ++i) {
@@ -940,55 +934,54 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
     k_off[i] = r * (uint32_t)a.k_place + piece * 16;
     v_off[i] = r * (uint32_t)a.v_place + piece * 16;
   }
-  auto stage_load = [&](uint32_t s, auto set_) {
-    constexpr int set = decltype(set_)::value;
+  auto stage_load = [&](uint32_t s) {
     if (s - page_sub >= 64) {
       page_sub = s;
       pages = pages_from(s);
     }
     const uint32_t page = (uint32_t)__builtin_amdgcn_readlane((int)pages, (int)(s - page_sub));
     const Keys16 t = keys16(a, page, key_of(s), keys_of(s), head);
-    stage_flags[set] = t.n < (uint32_t)St::kRows ? t.n : (uint32_t)St::kRows;
+    stage_flags = t.n < (uint32_t)St::kRows ? t.n : (uint32_t)St::kRows;
     if (t.n >= (uint32_t)St::kRows) {  // no branch in a lane, and addresses that are a base and the lane's offset
 #pragma unroll
       for (int i = 0; i < St::kLoads; ++i) {
-        stage_k[set][i] = *reinterpret_cast<const u32x4v*>(t.k + k_off[i]);
-        stage_v[set][i] = *reinterpret_cast<const u32x4v*>(t.v + v_off[i]);
+        stage_k[i] = *reinterpret_cast<const u32x4v*>(t.k + k_off[i]);
+        stage_v[i] = *reinterpret_cast<const u32x4v*>(t.v + v_off[i]);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < St::kLoads; ++i) {
-        stage_k[set][i] = stage_v[set][i] = (u32x4v)0u;
+        stage_k[i] = stage_v[i] = (u32x4v)0u;
         if ((i * 64 + lane) / St::kPieces < t.n) {
-          stage_k[set][i] = *reinterpret_cast<const u32x4v*>(t.k + k_off[i]);
-          stage_v[set][i] = *reinterpret_cast<const u32x4v*>(t.v + v_off[i]);
+          stage_k[i] = *reinterpret_cast<const u32x4v*>(t.k + k_off[i]);
+          stage_v[i] = *reinterpret_cast<const u32x4v*>(t.v + v_off[i]);
         }
       }
     }
   };
-  auto stage_store = [&](uint32_t s, auto set_) {  // into the buffer of the same number
-    constexpr int set = decltype(set_)::value;
+  auto stage_store = [&](uint32_t s) {
+    const uint32_t buf = (s - first) & 1;
     if (s >= prefix_subs && (s - prefix_subs + 1) * St::kKeys > own_group_least) {
       uint32_t any = 0;
 #pragma unroll
       for (int i = 0; i < St::kLoads; ++i)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) any |= special_bits<T>(stage_v[set][i][c]);
+        for (int c = 0; c < 4; ++c) any |= special_bits<T>(stage_v[i][c]);
       if (__any(any != 0)) {
-        stage_flags[set] |= 0x80;
+        stage_flags |= 0x80;
 #pragma unroll
         for (int i = 0; i < St::kLoads; ++i)
 #pragma unroll
-          for (int c = 0; c < 4; ++c) stage_v[set][i][c] = clear_special<T>(stage_v[set][i][c]);
+          for (int c = 0; c < 4; ++c) stage_v[i][c] = clear_special<T>(stage_v[i][c]);
       }
     }
 #pragma unroll
     for (int i = 0; i < St::kLoads; ++i) {
       const uint32_t r = wave * St::kRows + (i * 64 + lane) / St::kPieces, piece = (i * 64 + lane) % St::kPieces;
-      *reinterpret_cast<u32x4v*>(lds_k + set * St::kTile + St::k_at(r, piece)) = stage_k[set][i];
-      *reinterpret_cast<u32x4v*>(lds_v + set * St::kTile + St::v_at(r, piece)) = stage_v[set][i];
+      *reinterpret_cast<u32x4v*>(lds_k + buf * St::kTile + St::k_at(r, piece)) = stage_k[i];
+      *reinterpret_cast<u32x4v*>(lds_v + buf * St::kTile + St::v_at(r, piece)) = stage_v[i];
     }
-    if (lane == 0) lds_flags[set * 8 + wave] = (uint8_t)stage_flags[set];
+    if (lane == 0) lds_flags[buf * kWaves + wave] = (uint8_t)stage_flags;
   };
 
   bool special = false;
@@ -1009,34 +1002,25 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
     }
   }
 
-  typedef std::integral_constant<int, 0> Even;
-  typedef std::integral_constant<int, 1> Odd;
-  if (sub < end) {
-    stage_load(sub, Even());
-    if (sub + 1 < end) stage_load(sub + 1, Odd());
-    stage_store(sub, Even());
-    if (sub + 2 < end) stage_load(sub + 2, Even());
+  if (first < end) {
+    stage_load(first);
+    stage_store(first);
+    if (first + 1 < end) stage_load(first + 1);
   }
   // One barrier a sub-step: what it stores one ahead is complete at the next one's, and goes to the
   // buffer that all waves were done with at its own.
-  auto sub_step = [&](auto buf_) {
-    constexpr int buf = decltype(buf_)::value;
-    typedef std::integral_constant<int, 1 - buf> Other;
+  for (uint32_t sub = first; sub < end; ++sub) {
+    const uint32_t buf = (sub - first) & 1;
     __syncthreads();
-    if (sub + 1 < end) stage_store(sub + 1, Other());
-    if (sub + 3 < end) stage_load(sub + 3, Other());
+    if (sub + 1 < end) stage_store(sub + 1);
+    if (sub + 2 < end) stage_load(sub + 2);
     const bool shared = sub < prefix_subs;
     const uint32_t key = (shared ? sub : sub - prefix_subs) * St::kKeys;
     if (wave_row < rows && (shared || key < own_wave_most)) {
       const char* const kb = lds_k + buf * St::kTile;
       const char* const vb = lds_v + buf * St::kTile;
-      uint32_t flags[2];
-#pragma unroll
-      for (int c = 0; c < 2; ++c)
-        flags[c] = c * 4 < kTileWaves<D> ? (uint32_t)__builtin_amdgcn_readfirstlane(
-                                               *reinterpret_cast<const int*>(lds_flags + buf * 8 + 4 * c))
-                                         : kWhole;
-      special |= ((flags[0] | flags[1]) & kCleared) != 0;
+      const uint32_t flags = uniform(*reinterpret_cast<const uint32_t*>(lds_flags + buf * kWaves));
+      special |= (flags & kCleared) != 0;
       f32x16 s[kKTiles];
 #pragma unroll
       for (int t = 0; t < kKTiles; ++t) {
@@ -1048,16 +1032,17 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
           s[t] = Mfma32<T>::run(get(k, T()), get(q[i], T()), s[t]);
         }
       }
-      const bool all_exist = (flags[0] & ~kCleared) == kWhole && (flags[1] & ~kCleared) == kWhole;
+      const bool all_exist = (flags & ~kCleared) == kWhole;
       if (!all_exist || (!shared && key + St::kKeys > own_least)) {
         const uint32_t seen = shared ? it.prefix_keys : own_seen;
 #pragma unroll
         for (int t = 0; t < kKTiles; ++t)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const int w = 4 * t + r / 4;  // the wave that staged the key
-            const uint32_t in = r % 4 + 4 * h, exist = (flags[w / 4] >> (8 * (w % 4))) & 0x7f;
-            if (key + 8 * w + in >= seen || in >= exist) s[t][r] = -INFINITY;
+            const int quad = 32 * t + 8 * (r / 4);  // and 4 h on
+            const uint32_t in = quad % St::kRows + r % 4 + 4 * h, w = quad / St::kRows;  // in wave w's rows
+            const uint32_t exist = (flags >> (8 * w)) & 0x7f;
+            if (key + w * St::kRows + in >= seen || in >= exist) s[t][r] = -INFINITY;
           }
       }
       float top = s[0][0];
@@ -1097,18 +1082,12 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
           o[i] = Mfma32<T>::run(get(v, T()), get(p[kk], T()), o[i]);
         }
     }
-    ++sub;
-  };
-  while (sub < end) {
-    sub_step(Even());
-    if (sub < end) sub_step(Odd());
   }
 
   l = sum_halves(l);
   if (!row_live) return;
   if (special) {
     uint32_t key = own_group_least & ~(St::kKeys - 1u);  // the first sub-step that was looked at
-    const uint32_t first = St::kSubs * unit.chunk * it.per;
     if (first > prefix_subs && (first - prefix_subs) * St::kKeys > key) key = (first - prefix_subs) * St::kKeys;
     const uint32_t to = (end - prefix_subs) * St::kKeys;
     for (; key < to && key < own_seen; ++key) {
@@ -1153,22 +1132,17 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
 }
 
 template <int D>
-constexpr int few_lds() {
-  return kWaves * kFewRows * (D + 4 + 2) * 4;
-}
-template <int D>
 constexpr int lds_bytes() {
-  constexpr int few = few_lds<D>() * kTileWaves<D> / kWaves, tile = Staged<D>::kBytes;
+  constexpr int few = kWaves * kFewRows * (D + 4 + 2) * 4, tile = Staged<D>::kBytes;
   return few > tile ? few : tile;
 }
 
 template <class T, int D>
-__global__ __launch_bounds__(64 * kTileWaves<D>, D == 256 ? 1 : 2) void attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(AttendArgs a) {
   __shared__ __attribute__((aligned(16))) char lds[lds_bytes<D>()];
   const Ws& w = a.ws;
   const uint32_t n_items = a.n_groups + a.n_seq, lane = threadIdx.x & 63;
-  const uint32_t half = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kThreads));
-  // workgroups of full tiles come first, then those that take a unit of few rows for every 4 waves
+  // units of full tiles come first
   uint32_t tiles, fews;
   WavePlan plan;
   const bool in_wave = n_items <= kWaveItems;
@@ -1183,34 +1157,29 @@ __global__ __launch_bounds__(64 * kTileWaves<D>, D == 256 ? 1 : 2) void attend_k
   }
   tiles = uniform(tiles);
   fews = uniform(fews);
+  if (blockIdx.x >= tiles + fews) return;
   const bool few = blockIdx.x >= tiles;
-  uint32_t u = blockIdx.x;
-  if (few) {
-    u = (u - tiles) * (kTileWaves<D> / kWaves) + half;
-    if (u - half >= fews) return;
+  uint32_t u = few ? blockIdx.x - tiles : blockIdx.x;
+  Unit unit;
+  if (in_wave) {
+    const uint64_t le = __ballot(lane < n_items && (few ? plan.it.few_first : plan.it.tile_first) <= u);
+    unit.it = item_of_lane(plan.it, 63 - __clzll((long long)le));
+  } else {
+    const uint32_t* const first = few ? w.few_first : w.tile_first;
+    const uint32_t at = uniform(wave_search<uint32_t>(first, n_items, u));
+    unit.it = w.items[at];
   }
-  Unit unit{};
-  if (!few || u < fews) {
-    if (in_wave) {
-      const uint64_t le = __ballot(lane < n_items && (few ? plan.it.few_first : plan.it.tile_first) <= u);
-      unit.it = item_of_lane(plan.it, 63 - __clzll((long long)le));
-    } else {
-      const uint32_t* const first = few ? w.few_first : w.tile_first;
-      const uint32_t at = __builtin_amdgcn_readfirstlane((int)wave_search<uint32_t>(first, n_items, u));
-      unit.it = w.items[at];
-    }
-    u -= few ? unit.it.few_first : unit.it.tile_first;
-    unit.head = u % a.kv_heads;
-    u /= a.kv_heads;
-    unit.chunk = u % unit.it.chunks;
-    // a prompt's last rows see the most keys: they come first
-    unit.tile = tiles_of(unit.it.tokens * a.ratio, kTileWaves<D>) - 1 - u / unit.it.chunks;
-  }
+  u -= few ? unit.it.few_first : unit.it.tile_first;
+  unit.head = u % a.kv_heads;
+  u /= a.kv_heads;
+  unit.chunk = u % unit.it.chunks;
+  // a prompt's last rows see the most keys: they come first
+  unit.tile = tiles_of(unit.it.tokens * a.ratio) - 1 - u / unit.it.chunks;
   unit.it = item_of_lane(unit.it, 0);
   unit.head = uniform(unit.head);
   unit.chunk = uniform(unit.chunk);
   unit.tile = uniform(unit.tile);
-  if (few) attend_few<T, D>(a, unit, lds + half * few_lds<D>());
+  if (few) attend_few<T, D>(a, unit, lds);
   else attend_tile<T, D>(a, unit, lds);
 }
 
@@ -1362,11 +1331,10 @@ gleam_status validate_attention(const gleam_kv_pages* kv, const gleam_prefix_bat
   shape->kv_heads = kv->kv_heads;
   shape->ratio = b->q_heads / kv->kv_heads;
   shape->target = 1024;
-  shape->tile_waves = kv->head_dim == 256 ? kTileWaves<256> : kTileWaves<128>;
   const uint64_t most = steps_of((uint32_t)(b->own_width * kv->page_tokens)) +
                         (uint64_t)steps_of((uint32_t)(b->prefix_width * kv->page_tokens));
   shape->most_steps = (uint32_t)most;
-  if (most_units(*shape) > max_workgroups(512) || most_partials(*shape) > UINT32_MAX) {
+  if (most_units(*shape) > max_workgroups(kThreads) || most_partials(*shape) > UINT32_MAX) {
     set_error("%s: more work than one launch holds", who);
     return GLEAM_E_UNSUPPORTED;
   }
@@ -1384,7 +1352,7 @@ gleam_status launch_all(const AttendArgs& a, uint32_t units, hipStream_t stream)
     if ((st = launch_status("plan_kernel")) != GLEAM_OK) return st;
   }
   if (units > 0) {
-    hipLaunchKernelGGL((attend_kernel<T, D>), dim3(units), dim3(64 * kTileWaves<D>), 0, stream, a);
+    hipLaunchKernelGGL((attend_kernel<T, D>), dim3(units), dim3(kThreads), 0, stream, a);
     if ((st = launch_status("attend_kernel")) != GLEAM_OK) return st;
   }
   const uint32_t rows = a.n_tokens * a.q_heads;
@@ -1474,7 +1442,6 @@ extern "C" gleam_status gleam_prefix_attention(const gleam_kv_pages* kv, const g
   a.page_log2 = (uint32_t)log2_exact(kv->page_tokens);
   a.n_pages = (uint32_t)kv->n_pages;
   a.target = shape.target;
-  a.tile_waves = shape.tile_waves;
   a.scale_log2 = b->scale * kLog2e;
   a.out = static_cast<uint8_t*>(d_out);
   a.lse = d_lse;

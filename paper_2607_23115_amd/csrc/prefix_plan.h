@@ -22,11 +22,11 @@
 namespace gleam {
 
 constexpr uint32_t kStep = 64;        // keys in a step
-constexpr uint32_t kFewRows = 16;     // rows of a tile of the first kind
+constexpr uint32_t kFewRows = 16, kTileRows = 128;  // rows of a tile, of the two kinds
 constexpr uint32_t kMostFew = 32;     // items of up to this many rows take tiles of the first kind
 constexpr uint32_t kJointRows = 128;  // sequences of a group with this many rows on average keep to themselves
 constexpr uint32_t kMinFewSteps = 2;  // steps of the shortest chunk: one round of a workgroup's four waves
-// and of the second kind, whose partial results are 128 KiB a unit (256 rows of 128 dims)
+// and of the second kind, whose partial results are 64 KiB a unit (128 rows of 128 dims)
 constexpr uint32_t kMinTileSteps = 8;
 
 struct PlanShape {  // what the host knows
@@ -34,8 +34,6 @@ struct PlanShape {  // what the host knows
   uint32_t kv_heads, ratio;  // ratio: query heads per key head
   uint32_t target;           // units wanted: what fills the GPU
   uint32_t most_steps;       // of an item, from the widths of the page tables
-  uint32_t tile_waves;       // waves of a workgroup, which takes a tile of 32 rows a wave, or a unit
-                             // of few rows for every 4 waves
 };
 
 GLEAM_HD uint64_t div_up(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
@@ -45,24 +43,19 @@ GLEAM_HD uint32_t steps_of(uint32_t keys) { return (keys + kStep - 1) / kStep; }
 GLEAM_HD bool joint_group(uint64_t rows, uint64_t seqs) { return seqs <= 1 || rows >= kJointRows * seqs; }
 
 GLEAM_HD bool few_rows(uint32_t rows) { return rows <= kMostFew; }
-GLEAM_HD uint32_t tiles_of(uint32_t rows, uint32_t tile_waves) {
-  const uint32_t per = few_rows(rows) ? kFewRows : 32 * tile_waves;
+GLEAM_HD uint32_t tiles_of(uint32_t rows) {
+  const uint32_t per = few_rows(rows) ? kFewRows : kTileRows;
   return (rows + per - 1) / per;
 }
 
-// What an item costs a key head: its tiles' steps, times the quarters of a workgroup that they
-// take (a step of 16 rows is bound by reading its keys and values, a step of a full tile by its
-// products: much the same time).
-GLEAM_HD uint64_t item_cost(uint32_t rows, uint32_t steps, uint32_t tile_waves) {
-  return (uint64_t)tiles_of(rows, tile_waves) * steps * (few_rows(rows) ? 1 : tile_waves / 4);
-}
+// What an item costs a key head: its tiles' steps (a step of 16 rows is bound by reading its
+// keys and values, one of 128 by their products: much the same time).
+GLEAM_HD uint64_t item_cost(uint32_t rows, uint32_t steps) { return (uint64_t)tiles_of(rows) * steps; }
 
 // Steps of a chunk of an item of `rows` rows: no more than `target` chunks of all items' tiles
 // together, apart from each tile's first. `cost`: all items', of all key heads.
-GLEAM_HD uint32_t chunk_steps(uint32_t rows, uint64_t cost, uint32_t target, uint32_t tile_waves) {
-  uint64_t c = div_up(cost, target);
-  if (!few_rows(rows)) c = div_up(c, tile_waves / 4);
-  const uint64_t least = few_rows(rows) ? kMinFewSteps : kMinTileSteps;
+GLEAM_HD uint32_t chunk_steps(uint32_t rows, uint64_t cost, uint32_t target) {
+  const uint64_t c = div_up(cost, target), least = few_rows(rows) ? kMinFewSteps : kMinTileSteps;
   return c < least ? (uint32_t)least : c > 0x7fffffffu ? 0x7fffffffu : (uint32_t)c;
 }
 
@@ -83,11 +76,11 @@ GLEAM_HD Cut cut_steps(uint32_t steps, uint32_t most) {
 //
 // Units: sum of tiles * kv_heads * chunks, where chunks < steps / chunk_steps + 1, so at most
 // target + kv_heads * tiles, and at most kv_heads * tiles * most_steps / kMinFewSteps. Tiles: an
-// item of n rows has at most n / kFewRows + 1 of them, and at most n / (32 tile_waves) + 2, and a
+// item of n rows has at most n / kFewRows + 1 of them, and at most n / kTileRows + 2, and a
 // token's rows are in two items at most, its group's and its sequence's.
 GLEAM_HD uint64_t most_units(const PlanShape& s) {
   const uint64_t rows = 2 * s.n_tokens * s.ratio, items = s.n_groups + s.n_seq;
-  const uint64_t few = items + rows / kFewRows, tile = 2 * items + rows / (32 * s.tile_waves);
+  const uint64_t few = items + rows / kFewRows, tile = 2 * items + rows / kTileRows;
   const uint64_t tiles = s.kv_heads * (few < tile ? few : tile);
   const uint64_t cuts = tiles * div_up(s.most_steps, kMinFewSteps);
   return s.target + tiles < cuts ? s.target + tiles : cuts;
@@ -96,12 +89,11 @@ GLEAM_HD uint64_t most_units(const PlanShape& s) {
 // Rows of partial results: an item that is cut, or shares its rows with another, has
 // rows * kv_heads * chunks. Shared: groups that are not joint have fewer than kJointRows rows a
 // sequence, in two items, for their first chunks. Cut: chunks >= 2 makes chunks <= 2 * steps /
-// chunk_steps, and rows <= 32 tile_waves * tiles, so 2 * 32 tile_waves * target at most (of tiles
-// whose steps cost tile_waves / 4, chunks are as much shorter).
+// chunk_steps, and rows <= kTileRows * tiles, so 2 * kTileRows * target at most.
 GLEAM_HD uint64_t most_partials(const PlanShape& s) {
   const uint64_t rows = s.n_tokens * s.ratio, apart = kJointRows * s.n_seq;
   const uint64_t shared = s.n_groups ? 2 * (rows < apart ? rows : apart) * s.kv_heads : 0;
-  return shared + 2ull * 32 * s.tile_waves * s.target;
+  return shared + 2ull * kTileRows * s.target;
 }
 
 }  // namespace gleam
