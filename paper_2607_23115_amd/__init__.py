@@ -65,27 +65,31 @@ class _Batch(ctypes.Structure):
                 ("block_bytes", ctypes.c_uint32)]
 
 
+def _fields(kinds: dict, layout: str):
+    """ctypes fields from "name:kind name:kind ..."; an array is a field for each place (a
+    Structure takes numbers faster than tuples)."""
+    return [(name, kinds[kind]) for name, kind in (f.split(":") for f in layout.split())]
+
+
+_KINDS = {"p": ctypes.c_void_p, "u8": ctypes.c_uint64, "u4": ctypes.c_uint32, "i8": ctypes.c_int64,
+          "f4": ctypes.c_float}
+
+
 class _KvPages(ctypes.Structure):
-    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_pages", ctypes.c_uint64),
-                ("page_tokens", ctypes.c_uint32), ("kv_heads", ctypes.c_uint32), ("head_dim", ctypes.c_uint32),
-                ("dtype", ctypes.c_uint32), ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3)]
+    _fields_ = _fields(_KINDS, "k:p v:p n_pages:u8 page_tokens:u4 kv_heads:u4 head_dim:u4 dtype:u4 k_page:i8 "
+                               "k_place:i8 k_head:i8 v_page:i8 v_place:i8 v_head:i8")
 
 
 class _Append(ctypes.Structure):
-    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q_out", ctypes.c_void_p),
-                ("slots", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("rotary", ctypes.c_void_p),
-                ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("n_tokens", ctypes.c_uint64),
-                ("rotary_positions", ctypes.c_uint64), ("q_stride", ctypes.c_int64 * 2),
-                ("k_stride", ctypes.c_int64 * 2), ("v_stride", ctypes.c_int64 * 2), ("q_heads", ctypes.c_uint32),
-                ("rot_dim", ctypes.c_uint32), ("interleaved", ctypes.c_uint32), ("eps", ctypes.c_float)]
+    _fields_ = _fields(_KINDS, "q:p k:p v:p q_out:p slots:p positions:p rotary:p q_weight:p k_weight:p n_tokens:u8 "
+                               "rotary_positions:u8 q_token:i8 q_head:i8 k_token:i8 k_head:i8 v_token:i8 v_head:i8 "
+                               "q_heads:u4 rot_dim:u4 interleaved:u4 eps:f4")
 
 
 class _PrefixBatch(ctypes.Structure):
-    _fields_ = [("q", ctypes.c_void_p), ("q_first", ctypes.c_void_p), ("own_pages", ctypes.c_void_p),
-                ("own_len", ctypes.c_void_p), ("group_first", ctypes.c_void_p), ("prefix_pages", ctypes.c_void_p),
-                ("prefix_len", ctypes.c_void_p), ("n_tokens", ctypes.c_uint64), ("n_seq", ctypes.c_uint64),
-                ("n_groups", ctypes.c_uint64), ("own_width", ctypes.c_uint64), ("prefix_width", ctypes.c_uint64),
-                ("q_stride", ctypes.c_int64 * 2), ("q_heads", ctypes.c_uint32), ("scale", ctypes.c_float)]
+    _fields_ = _fields(_KINDS, "q:p q_first:p own_pages:p own_len:p group_first:p prefix_pages:p prefix_len:p "
+                               "n_tokens:u8 n_seq:u8 n_groups:u8 own_width:u8 prefix_width:u8 q_token:i8 q_head:i8 "
+                               "q_heads:u4 scale:f4")
 
 
 def _load() -> ctypes.CDLL:
@@ -839,43 +843,56 @@ def as_u64(t: torch.Tensor) -> np.ndarray:
 # A paged key/value cache
 # --------------------------------------------------------------------------- #
 _KV_TYPES = {torch.float16: 0, torch.bfloat16: 1}  # GLEAM_FP16, GLEAM_BF16
-_I32, _F32 = (torch.int32,), (torch.float32,)
 
 
-def _steps(t: torch.Tensor):
-    """Strides in elements of all dimensions but the last; of a dimension of size 1, which
-    nothing is multiplied by, 0."""
-    return tuple(s if n > 1 else 0 for s, n in zip(t.stride()[:-1], t.shape[:-1]))
+def _flat(t: torch.Tensor | None, name: str, dtype: torch.dtype, dev: int, least: int = 0, optional: bool = False):
+    """Address of a contiguous tensor of the type, on GPU `dev`, of at least `least` elements.
+    (These calls are short: what holds costs one line, the reason of a refusal is _dev's.)"""
+    if t is None and optional:
+        return None
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == dev and t.numel() >= least
+            and t.is_contiguous()):
+        return t.data_ptr()
+    _dev(t, name, (dtype,), least)
+    raise ValueError(f"{name} is on {t.device}, the cache on cuda:{dev}")
 
 
-def _heads(t: torch.Tensor, name: str, like: torch.Tensor, heads: int | None = None):
-    """Check [tokens, heads, head_dim] of the cache's type, whose heads are whole rows."""
+def _heads(t: torch.Tensor, name: str, dtype: torch.dtype, dev: int, d: int):
+    """(address, tokens, heads, strides of both) of [tokens, heads, d] of the cache's type, whose
+    heads are whole rows. The stride of a dimension of size 1 multiplies nothing: 0."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == dev and t.dim() == 3:
+        tokens, heads, last = t.shape
+        a, b, c = t.stride()
+        if last == d and c == 1:
+            return t.data_ptr(), tokens, heads, a if tokens > 1 else 0, b if heads > 1 else 0
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a tensor on the GPU")
-    if t.device != like.device:
-        raise ValueError(f"{name} is on {t.device}, the cache on {like.device}")
-    if t.dtype != like.dtype:
-        raise ValueError(f"{name} must be {like.dtype} as the cache is, not {t.dtype}")
-    if t.dim() != 3 or t.shape[2] != like.shape[3] or (heads is not None and t.shape[1] != heads):
-        raise ValueError(f"{name} must be [tokens, {heads or 'heads'}, {like.shape[3]}], not {list(t.shape)}")
-    if t.stride(2) != 1:
-        raise ValueError(f"{name} must have its last dimension contiguous")
-    return t
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, the cache on cuda:{dev}")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype} as the cache is, not {t.dtype}")
+    if t.dim() != 3 or t.shape[2] != d:
+        raise ValueError(f"{name} must be [tokens, heads, {d}], not {list(t.shape)}")
+    raise ValueError(f"{name} must have its last dimension contiguous")
 
 
 def _kv_struct(k_pages: torch.Tensor, v_pages: torch.Tensor) -> _KvPages:
     for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
-        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        if not isinstance(t, torch.Tensor) or t.get_device() < 0:
             raise ValueError(f"{name} must be a tensor on the GPU")
         if t.dim() != 4 or t.stride(3) != 1:
             raise ValueError(f"{name} must be [pages, page_tokens, kv_heads, head_dim], the last contiguous")
-        if t.dtype not in _KV_TYPES:
-            raise ValueError(f"{name} must be torch.float16 or torch.bfloat16, not {t.dtype}")
-    if k_pages.shape != v_pages.shape or k_pages.dtype != v_pages.dtype or k_pages.device != v_pages.device:
+    dtype = _KV_TYPES.get(k_pages.dtype)
+    if dtype is None:
+        raise ValueError(f"k_pages must be torch.float16 or torch.bfloat16, not {k_pages.dtype}")
+    n, page, heads, d = shape = k_pages.shape
+    if shape != v_pages.shape or k_pages.dtype is not v_pages.dtype or k_pages.get_device() != v_pages.get_device():
         raise ValueError("k_pages and v_pages differ in shape, type or device")
-    n, page, heads, d = k_pages.shape
-    return _KvPages(k_pages.data_ptr(), v_pages.data_ptr(), n, page, heads, d, _KV_TYPES[k_pages.dtype],
-                    _steps(k_pages), _steps(v_pages))
+    a, b, c, _ = k_pages.stride()
+    x, y, z, _ = v_pages.stride()
+    return _KvPages(k_pages.data_ptr(), v_pages.data_ptr(), n, page, heads, d, dtype, a if n > 1 else 0,
+                    b if page > 1 else 0, c if heads > 1 else 0, x if n > 1 else 0, y if page > 1 else 0,
+                    z if heads > 1 else 0)
 
 
 def rotary_table(positions: int, rot_dim: int, base: float = 10000.0, factor: float = 1.0,
@@ -911,43 +928,45 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: 
     -1 to store nothing. rotary: rotary_table()'s, with positions int32. q_weight, k_weight
     [head_dim]: norm each head of q, of k."""
     kv = _kv_struct(k_pages, v_pages)
-    n, heads = k.shape[0] if isinstance(k, torch.Tensor) and k.dim() else 0, k_pages.shape[2]
-    _heads(k, "k", k_pages, heads)
-    _heads(v, "v", k_pages, heads)
-    if v.shape[0] != n:
+    dtype, dev, d = k_pages.dtype, k_pages.get_device(), kv.head_dim
+    k_at, n, heads, k_token, k_head = _heads(k, "k", dtype, dev, d)
+    v_at, v_n, v_heads, v_token, v_head = _heads(v, "v", dtype, dev, d)
+    if n != v_n:
         raise ValueError("k and v differ in tokens")
+    if heads != kv.kv_heads or v_heads != heads:
+        raise ValueError(f"k must be [tokens, {kv.kv_heads}, {d}] and v too, as the cache has so many heads")
+    q_at, q_heads, q_token, q_head = None, 0, 0, 0
     if q is not None:
-        _heads(q, "q", k_pages)
-        if q.shape[0] != n:
+        q_at, q_n, q_heads, q_token, q_head = _heads(q, "q", dtype, dev, d)
+        if q_n != n:
             raise ValueError("q and k differ in tokens")
+        if q_heads == 0:
+            q_at = None
     elif q_out is not None or q_weight is not None:
         raise ValueError("q_out and q_weight need q")
-    _dev(slots, "slots", _U64, n)
-    rot, table = 0, 0
+    slots_at = _flat(slots, "slots", torch.int64, dev, n)
+    table_at, positions_at, rot, table = None, None, 0, 0
     if rotary is not None:
-        _dev(rotary, "rotary", _F32)
-        _dev(positions, "positions", _I32, n)
+        table_at = _flat(rotary, "rotary", torch.float32, dev)
+        positions_at = _flat(positions, "positions", torch.int32, dev, n)
         if rotary.dim() != 2:
             raise ValueError("rotary must be [positions, rot_dim]")
         table, rot = rotary.shape
-    for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        _dev(t, name, (k_pages.dtype,), k_pages.shape[3], optional=True)
-    for t, name in ((slots, "slots"), (rotary, "rotary"), (positions, "positions"), (q_weight, "q_weight"),
-                    (k_weight, "k_weight"), (q_out, "q_out")):
-        if t is not None and t.device != k_pages.device:
-            raise ValueError(f"{name} is on {t.device}, the cache on {k_pages.device}")
+    qw_at = _flat(q_weight, "q_weight", dtype, dev, d, optional=True)
+    kw_at = _flat(k_weight, "k_weight", dtype, dev, d, optional=True)
     with _on_stream(stream, k_pages.device) as hs:
+        out_at = None
         if q is not None:
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            elif _dev(q_out, "q_out", (q.dtype,)).shape != q.shape:
+                q_out = torch.empty((n, q_heads, d), dtype=dtype, device=q.device)
+            out_at = _flat(q_out, "q_out", dtype, dev)
+            if q_out.shape != q.shape:
                 raise ValueError("q_out and q differ in shape")
-        with_q = q is not None and q.shape[1] > 0
-        args = _Append(_ptr(q) if with_q else None, k.data_ptr(), v.data_ptr(), _ptr(q_out) if with_q else None,
-                       slots.data_ptr(), _ptr(positions), _ptr(rotary), _ptr(q_weight), _ptr(k_weight), n, table,
-                       _steps(q) if with_q else (0, 0), _steps(k), _steps(v), q.shape[1] if with_q else 0, rot,
-                       int(interleaved), eps)
-        _check(lib.gleam_kv_append(ctypes.byref(kv), ctypes.byref(args), hs))
+            if q_at is None:
+                out_at = None
+        args = _Append(q_at, k_at, v_at, out_at, slots_at, positions_at, table_at, qw_at, kw_at, n, table, q_token,
+                       q_head, k_token, k_head, v_token, v_head, q_heads, rot, 1 if interleaved else 0, eps)
+        _check(lib.gleam_kv_append(kv, args, hs))
     return q_out
 
 
@@ -966,50 +985,47 @@ def prefix_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
     page tables -1. scale: head_dim ** -0.5 where none is given. ws: a workspace from
     prefix_attention_workspace() of these shapes."""
     kv = _kv_struct(k_pages, v_pages)
-    _heads(q, "q", k_pages)
-    n_seq, n_groups, own_width, prefix_width = own_len.numel(), 0, 0, 0
-    _dev(q_first, "q_first", _I32, n_seq + 1)
-    _dev(own_len, "own_len", _I32)
-    _dev(own_pages, "own_pages", _I32)
+    dtype, dev, d = k_pages.dtype, k_pages.get_device(), kv.head_dim
+    q_at, tokens, heads, q_token, q_head = _heads(q, "q", dtype, dev, d)
+    i32 = torch.int32
+    len_at = _flat(own_len, "own_len", i32, dev)
+    n_seq = own_len.numel()
+    first_at = _flat(q_first, "q_first", i32, dev, n_seq + 1)
+    pages_at = _flat(own_pages, "own_pages", i32, dev)
     if own_pages.dim() != 2 or own_pages.shape[0] != n_seq:
         raise ValueError(f"own_pages must be [{n_seq}, pages], not {list(own_pages.shape)}")
-    own_width = own_pages.shape[1]
+    n_groups, prefix_width, group_at, prefix_at, prefix_len_at = 0, 0, None, None, None
     if group_first is not None or prefix_pages is not None or prefix_len is not None:
-        _dev(prefix_len, "prefix_len", _I32)
+        prefix_len_at = _flat(prefix_len, "prefix_len", i32, dev)
         n_groups = prefix_len.numel()
-        _dev(group_first, "group_first", _I32, n_groups + 1)
-        _dev(prefix_pages, "prefix_pages", _I32)
+        group_at = _flat(group_first, "group_first", i32, dev, n_groups + 1)
+        prefix_at = _flat(prefix_pages, "prefix_pages", i32, dev)
         if prefix_pages.dim() != 2 or prefix_pages.shape[0] != n_groups:
             raise ValueError(f"prefix_pages must be [{n_groups}, pages], not {list(prefix_pages.shape)}")
         prefix_width = prefix_pages.shape[1]
-    for t, name in ((q_first, "q_first"), (own_pages, "own_pages"), (own_len, "own_len"), (lse, "lse"), (ws, "ws"),
-                    (group_first, "group_first"), (prefix_pages, "prefix_pages"), (prefix_len, "prefix_len"),
-                    (out, "out")):
-        if t is not None and t.device != k_pages.device:
-            raise ValueError(f"{name} is on {t.device}, the cache on {k_pages.device}")
-    tokens, heads, d = q.shape
-    b = _PrefixBatch(q.data_ptr(), q_first.data_ptr(), own_pages.data_ptr(), own_len.data_ptr(), _ptr(group_first),
-                     _ptr(prefix_pages), _ptr(prefix_len), tokens, n_seq, n_groups, own_width, prefix_width,
-                     _steps(q), heads, d ** -0.5 if scale is None else scale)
-    with _on_stream(stream, k_pages.device) as hs:
+    b = _PrefixBatch(q_at, first_at, pages_at, len_at, group_at, prefix_at, prefix_len_at, tokens, n_seq, n_groups,
+                     own_pages.shape[1], prefix_width, q_token, q_head, heads, d ** -0.5 if scale is None else scale)
+    device = k_pages.device
+    with _on_stream(stream, device) as hs:
         if out is None:
-            out = torch.empty((tokens, heads, d), dtype=q.dtype, device=q.device)
-        elif _dev(out, "out", (q.dtype,)).shape != q.shape:
+            out = torch.empty((tokens, heads, d), dtype=dtype, device=device)
+        out_at = _flat(out, "out", dtype, dev)
+        if out.shape != q.shape:
             raise ValueError("out and q differ in shape")
         if lse is None and want_lse:
-            lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device)
-        elif lse is not None and _dev(lse, "lse", _F32).shape != q.shape[:2]:
+            lse = torch.empty((tokens, heads), dtype=torch.float32, device=device)
+        lse_at = _flat(lse, "lse", torch.float32, dev, optional=True)
+        if lse is not None and lse.shape != q.shape[:2]:
             raise ValueError("lse must be [tokens, q_heads]")
         if ws is None:
-            ws = torch.empty(_attention_ws(kv, b), dtype=torch.uint8, device=q.device)
-        _dev(ws, "ws", _U8)
-        _check(lib.gleam_prefix_attention(ctypes.byref(kv), ctypes.byref(b), out.data_ptr(), _ptr(lse),
-                                          ws.data_ptr(), ws.numel(), hs))
+            ws = torch.empty(_attention_ws(kv, b), dtype=torch.uint8, device=device)
+        ws_at = _flat(ws, "ws", torch.uint8, dev)
+        _check(lib.gleam_prefix_attention(kv, b, out_at, lse_at, ws_at, ws.numel(), hs))
     return out, lse
 
 
 def _attention_ws(kv: _KvPages, b: _PrefixBatch) -> int:
-    n = int(lib.gleam_prefix_attention_ws_bytes(ctypes.byref(kv), ctypes.byref(b)))
+    n = lib.gleam_prefix_attention_ws_bytes(kv, b)
     if n == 0:
         raise GleamError(E_INVALID, lib.gleam_last_error().decode())
     return n

@@ -14,25 +14,30 @@ import paper_2607_23115_amd as g
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
-def kv(**kw):
-    s = g._KvPages(256, 256, 4, 16, 2, 64, 0, (2048, 128, 64), (2048, 128, 64))
+def put(s, **kw):
+    """Sets fields; "k_stride" and its like are all strides of k, in their order."""
     for n, x in kw.items():
-        setattr(s, n, x)
+        if n.endswith("_stride"):
+            names = [f for f, _ in s._fields_ if f in (n[0] + "_page", n[0] + "_place", n[0] + "_token", n[0] + "_head")]
+            assert len(names) == len(x)
+            put(s, **dict(zip(names, x)))
+        else:
+            setattr(s, n, x)
     return s
 
 
+def kv(**kw):
+    return put(g._KvPages(256, 256, 4, 16, 2, 64, 0, 2048, 128, 64, 2048, 128, 64), **kw)
+
+
 def append(cache=None, **kw):
-    a = g._Append(256, 256, 256, 256, 256, 256, 256, None, None, 4, 10, (128, 64), (128, 64), (128, 64), 2, 64, 0, 1e-6)
-    for n, x in kw.items():
-        setattr(a, n, x)
+    a = put(g._Append(256, 256, 256, 256, 256, 256, 256, None, None, 4, 10, 128, 64, 128, 64, 128, 64, 2, 64, 0, 1e-6),
+            **kw)
     return g.lib.gleam_kv_append(ctypes.byref(cache if cache is not None else kv()), ctypes.byref(a), None)
 
 
 def batch(**kw):
-    b = g._PrefixBatch(256, 256, 256, 256, 256, 256, 256, 4, 2, 1, 3, 3, (128, 64), 4, 1.0)
-    for n, x in kw.items():
-        setattr(b, n, x)
-    return b
+    return put(g._PrefixBatch(256, 256, 256, 256, 256, 256, 256, 4, 2, 1, 3, 3, 128, 64, 4, 1.0), **kw)
 
 
 def attend(cache=None, out=256, ws=256, ws_bytes=1 << 40, **kw):
@@ -110,18 +115,21 @@ def test_rotary_tables_that_are_refused():
 def test_structures_match_the_header(tmp_path):
     cc = shutil.which("gcc")
     assert cc, "gcc not found"
-    fields = {"gleam_kv_pages": (g._KvPages, ["n_pages", "page_tokens", "dtype", "k_stride", "v_stride"]),
-              "gleam_append": (g._Append, ["n_tokens", "rotary_positions", "q_stride", "v_stride", "q_heads", "eps"]),
-              "gleam_prefix_batch": (g._PrefixBatch, ["n_tokens", "prefix_width", "q_stride", "q_heads", "scale"])}
+    fields = {"gleam_kv_pages": (g._KvPages, ["n_pages", "page_tokens", "dtype", "k_stride k_page",
+                                              "v_stride v_page"]),
+              "gleam_append": (g._Append, ["n_tokens", "rotary_positions", "q_stride q_token", "v_stride v_token",
+                                           "q_heads", "eps"]),
+              "gleam_prefix_batch": (g._PrefixBatch, ["n_tokens", "prefix_width", "q_stride q_token", "q_heads",
+                                                      "scale"])}
     lines = [f'printf("%zu\\n", sizeof({s}));' for s in fields]
-    lines += [f'printf("%zu\\n", offsetof({s}, {f}));' for s, (_, fs) in fields.items() for f in fs]
+    lines += [f'printf("%zu\\n", offsetof({s}, {f.split()[0]}));' for s, (_, fs) in fields.items() for f in fs]
     src = tmp_path / "layout.c"
     src.write_text('#include <stddef.h>\n#include <stdio.h>\n#include "gleam.h"\nint main(void) {' + "".join(lines) +
                    "return 0;}\n")
     subprocess.run([cc, "-I", os.path.join(ROOT, "include"), str(src), "-o", str(tmp_path / "layout")], check=True)
     got = [int(x) for x in subprocess.run([str(tmp_path / "layout")], capture_output=True, text=True).stdout.split()]
     want = [ctypes.sizeof(t) for t, _ in fields.values()]
-    want += [getattr(t, f).offset for t, fs in fields.values() for f in fs]
+    want += [getattr(t, f.split()[-1]).offset for t, fs in fields.values() for f in fs]
     assert got == want
 
 
