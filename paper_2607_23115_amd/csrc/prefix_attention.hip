@@ -40,7 +40,7 @@ constexpr int kPlanThreads = 1024;
 constexpr float kRise = 8.f;  // log2
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr uint64_t kMostSeq = 1ull << 20;
-constexpr uint32_t kWideJoin = 4096;   // up to this many rows are joined by a workgroup each
+constexpr uint32_t kWideJoin = 256;    // up to this many rows are joined by a workgroup each
 constexpr uint32_t kMostJoins = 2048;  // workgroups of the others: those that the GPU holds at once
 
 struct Item {
@@ -85,7 +85,7 @@ struct AttendArgs {
   const int32_t* prefix_pages;
   const int32_t* prefix_len;
   uint32_t n_tokens, n_seq, n_groups, own_width, prefix_width;
-  uint32_t q_heads, kv_heads, ratio, page_log2, n_pages, target;
+  uint32_t q_heads, kv_heads, ratio, page_log2, n_pages, target, head_dim;
   float scale_log2;
   uint8_t* out;
   float* lse;
@@ -223,14 +223,25 @@ __device__ inline uint32_t item_steps(const Item& it) {
   return it.tokens ? steps_of(it.prefix_keys) + steps_of(it.own_keys) : 0;
 }
 
+// What the items of the two kinds cost together.
+struct Costs {
+  uint64_t tiles, fews;
+};
+__device__ inline Costs item_costs(const AttendArgs& a, const Item& it) {
+  const uint32_t rows = it.tokens * a.ratio;
+  const uint64_t cost = item_cost(rows, item_steps(it)) * a.kv_heads;
+  return few_rows(rows) ? Costs{0, cost} : Costs{cost, 0};
+}
+
 // What an item takes, once cut (cost: all items'): units of the two kinds, rows of partial results.
 // The sums over all items stay below 2^32 (most_units, most_partials).
 struct Takes {
   uint32_t tiles, fews, parts;
 };
-__device__ inline Takes cut_item(const AttendArgs& a, Item& it, uint64_t cost) {
+__device__ inline Takes cut_item(const AttendArgs& a, Item& it, const Costs& cost) {
   const uint32_t rows = it.tokens * a.ratio;
-  const Cut cut = cut_steps(item_steps(it), chunk_steps(rows, cost, a.target));
+  const Cut cut = cut_steps(item_steps(it), chunk_steps(rows, few_rows(rows) ? cost.fews : cost.tiles, a.target,
+                                                    a.head_dim));
   it.chunks = cut.chunks;
   it.per = cut.per;
   if (cut.chunks > 1) it.partial = 1;
@@ -269,16 +280,17 @@ __device__ WavePlan plan_in_wave(const AttendArgs& a) {
   auto of = [](int32_t v) { return [v](uint32_t i) { return __shfl(v, (int)i, 64); }; };
   w.it = make_item(a, lane, of(q), of(g), of(own), of(prefix), of(w.group));
   if (lane >= n_items) w.it = Item{};
-  const uint32_t steps = item_steps(w.it);
-  const uint64_t cost = wave_scan(item_cost(w.it.tokens * a.ratio, steps) * a.kv_heads, SumOp());
-  const Takes mine = cut_item(a, w.it, __shfl(cost, 63, 64));
+  Costs cost = item_costs(a, w.it);
+  cost.tiles = __shfl(wave_scan(cost.tiles, SumOp()), 63, 64);
+  cost.fews = __shfl(wave_scan(cost.fews, SumOp()), 63, 64);
+  const Takes mine = cut_item(a, w.it, cost);
   const uint32_t tiles = wave_scan(mine.tiles, SumOp()), fews = wave_scan(mine.fews, SumOp());
   w.it.tile_first = tiles - mine.tiles;
   w.it.few_first = fews - mine.fews;
   w.it.part_first = wave_scan(mine.parts, SumOp()) - mine.parts;
   w.tiles = (uint32_t)__builtin_amdgcn_readlane((int)tiles, 63);
   w.fews = (uint32_t)__builtin_amdgcn_readlane((int)fews, 63);
-  const bool empty = lane >= a.n_groups && w.it.tokens && steps == 0;
+  const bool empty = lane >= a.n_groups && w.it.tokens && item_steps(w.it) == 0;
   w.joins = __any(empty || mine.parts != 0) || __shfl(q, 0, 64) > 0 ||
             __shfl(q, (int)a.n_seq, 64) < (int32_t)a.n_tokens;
   return w;
@@ -356,20 +368,22 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a) {
   auto of = [](const int32_t* v) { return [v](uint32_t i) { return v[i]; }; };
 
   // the items without their cuts, and the cost of all
-  uint64_t cost = 0;
+  Costs cost{0, 0};
   uint32_t joins = q[0] > 0 || q[a.n_seq] < (int32_t)a.n_tokens;
   Item first{};  // of the thread; those of later rounds go through the workspace
   for (uint32_t i = threadIdx.x; i < n_items; i += blockDim.x) {
     Item it = make_item(a, i, of(q), of(g), of(a.own_len), of(a.prefix_len), group_of);
-    const uint32_t steps = item_steps(it);
-    cost += item_cost(it.tokens * a.ratio, steps) * a.kv_heads;
-    if (i >= a.n_groups && it.tokens && steps == 0) joins = 1;
+    const Costs c = item_costs(a, it);
+    cost.tiles += c.tiles;
+    cost.fews += c.fews;
+    if (i >= a.n_groups && it.tokens && item_steps(it) == 0) joins = 1;
     if (i < blockDim.x) first = it;
     else w.items[i] = it;
     if (a.n_groups && i >= a.n_groups) w.seq_group[i - a.n_groups] = group_of(i - a.n_groups);
   }
-  uint64_t all_cost;
-  block_scan(cost, lds, &all_cost, SumOp());
+  Costs all_cost;
+  block_scan(cost.tiles, lds, &all_cost.tiles, SumOp());
+  block_scan(cost.fews, lds, &all_cost.fews, SumOp());
 
   // chunks, units and partial rows
   Takes before{0, 0, 0};
@@ -1330,7 +1344,8 @@ gleam_status validate_attention(const gleam_kv_pages* kv, const gleam_prefix_bat
   shape->n_groups = b->n_groups;
   shape->kv_heads = kv->kv_heads;
   shape->ratio = b->q_heads / kv->kv_heads;
-  shape->target = 1024;
+  shape->target = 256;
+  shape->head_dim = kv->head_dim;
   const uint64_t most = steps_of((uint32_t)(b->own_width * kv->page_tokens)) +
                         (uint64_t)steps_of((uint32_t)(b->prefix_width * kv->page_tokens));
   shape->most_steps = (uint32_t)most;
@@ -1442,6 +1457,7 @@ extern "C" gleam_status gleam_prefix_attention(const gleam_kv_pages* kv, const g
   a.page_log2 = (uint32_t)log2_exact(kv->page_tokens);
   a.n_pages = (uint32_t)kv->n_pages;
   a.target = shape.target;
+  a.head_dim = kv->head_dim;
   a.scale_log2 = b->scale * kLog2e;
   a.out = static_cast<uint8_t*>(d_out);
   a.lse = d_lse;

@@ -23,17 +23,21 @@ namespace gleam {
 
 constexpr uint32_t kStep = 64;        // keys in a step
 constexpr uint32_t kFewRows = 16, kTileRows = 128;  // rows of a tile, of the two kinds
-constexpr uint32_t kMostFew = 32;     // items of up to this many rows take tiles of the first kind
+constexpr uint32_t kMostFew = 64;     // items of up to this many rows take tiles of the first kind
 constexpr uint32_t kJointRows = 128;  // sequences of a group with this many rows on average keep to themselves
-constexpr uint32_t kMinFewSteps = 2;  // steps of the shortest chunk: one round of a workgroup's four waves
-// and of the second kind, whose partial results are 64 KiB a unit (128 rows of 128 dims)
-constexpr uint32_t kMinTileSteps = 8;
+// Steps of the shortest chunks: one round of a workgroup's four waves; and of the second kind, whose
+// partial results are 512 bytes a dim and unit, 256 keys of 128 dims, or as many bytes of others
+// (64 rows behind 2,000 keys of 128 dims take 31 us with 4 steps, 35 with 8; 12 groups of 16 behind
+// up to 4,096 of 64 dims 37 and 34).
+constexpr uint32_t kMinFewSteps = 2;
+GLEAM_HD uint32_t min_tile_steps(uint32_t head_dim) { return 512 / head_dim; }
 
 struct PlanShape {  // what the host knows
   uint64_t n_tokens, n_seq, n_groups;
   uint32_t kv_heads, ratio;  // ratio: query heads per key head
-  uint32_t target;           // units wanted: what fills the GPU
+  uint32_t target;           // units of each kind wanted: what the GPU holds at once
   uint32_t most_steps;       // of an item, from the widths of the page tables
+  uint32_t head_dim;
 };
 
 GLEAM_HD uint64_t div_up(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
@@ -48,14 +52,13 @@ GLEAM_HD uint32_t tiles_of(uint32_t rows) {
   return (rows + per - 1) / per;
 }
 
-// What an item costs a key head: its tiles' steps (a step of 16 rows is bound by reading its
-// keys and values, one of 128 by their products: much the same time).
+// What an item costs a key head: its tiles' steps.
 GLEAM_HD uint64_t item_cost(uint32_t rows, uint32_t steps) { return (uint64_t)tiles_of(rows) * steps; }
 
-// Steps of a chunk of an item of `rows` rows: no more than `target` chunks of all items' tiles
-// together, apart from each tile's first. `cost`: all items', of all key heads.
-GLEAM_HD uint32_t chunk_steps(uint32_t rows, uint64_t cost, uint32_t target) {
-  const uint64_t c = div_up(cost, target), least = few_rows(rows) ? kMinFewSteps : kMinTileSteps;
+// Steps of a chunk of an item of `rows` rows: no more than `target` chunks of all tiles of a kind
+// together, apart from each tile's first. `cost`: of all items of the kind, all key heads.
+GLEAM_HD uint32_t chunk_steps(uint32_t rows, uint64_t cost, uint32_t target, uint32_t head_dim) {
+  const uint64_t c = div_up(cost, target), least = few_rows(rows) ? kMinFewSteps : min_tile_steps(head_dim);
   return c < least ? (uint32_t)least : c > 0x7fffffffu ? 0x7fffffffu : (uint32_t)c;
 }
 
@@ -75,25 +78,27 @@ GLEAM_HD Cut cut_steps(uint32_t steps, uint32_t most) {
 // The bounds that the launch and the workspace are sized by, from what the host knows.
 //
 // Units: sum of tiles * kv_heads * chunks, where chunks < steps / chunk_steps + 1, so at most
-// target + kv_heads * tiles, and at most kv_heads * tiles * most_steps / kMinFewSteps. Tiles: an
-// item of n rows has at most n / kFewRows + 1 of them, and at most n / kTileRows + 2, and a
-// token's rows are in two items at most, its group's and its sequence's.
+// 2 * target (one for each kind) + kv_heads * tiles, and at most kv_heads * tiles * most_steps /
+// kMinFewSteps. Tiles: an item of n rows has at most n / kFewRows + 1 of them, and at most
+// n / kTileRows + kMostFew / kFewRows, and a token's rows are in two items at most, its group's
+// and its sequence's.
 GLEAM_HD uint64_t most_units(const PlanShape& s) {
   const uint64_t rows = 2 * s.n_tokens * s.ratio, items = s.n_groups + s.n_seq;
-  const uint64_t few = items + rows / kFewRows, tile = 2 * items + rows / kTileRows;
+  const uint64_t few = items + rows / kFewRows, tile = kMostFew / kFewRows * items + rows / kTileRows;
   const uint64_t tiles = s.kv_heads * (few < tile ? few : tile);
   const uint64_t cuts = tiles * div_up(s.most_steps, kMinFewSteps);
-  return s.target + tiles < cuts ? s.target + tiles : cuts;
+  return 2 * s.target + tiles < cuts ? 2 * s.target + tiles : cuts;
 }
 
 // Rows of partial results: an item that is cut, or shares its rows with another, has
 // rows * kv_heads * chunks. Shared: groups that are not joint have fewer than kJointRows rows a
 // sequence, in two items, for their first chunks. Cut: chunks >= 2 makes chunks <= 2 * steps /
-// chunk_steps, and rows <= kTileRows * tiles, so 2 * kTileRows * target at most.
+// chunk_steps, and rows <= kTileRows (kFewRows) * tiles, so 2 * (kTileRows + kFewRows) * target at
+// most.
 GLEAM_HD uint64_t most_partials(const PlanShape& s) {
   const uint64_t rows = s.n_tokens * s.ratio, apart = kJointRows * s.n_seq;
   const uint64_t shared = s.n_groups ? 2 * (rows < apart ? rows : apart) * s.kv_heads : 0;
-  return shared + 2ull * kTileRows * s.target;
+  return shared + 2ull * (kTileRows + kFewRows) * s.target;
 }
 
 }  // namespace gleam

@@ -12,7 +12,7 @@ import pytest
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 CSRC = os.path.join(ROOT, "paper_2607_23115_amd", "csrc")
 
-# reads: kv_heads ratio target n_seq n_groups, then per sequence tokens own, then per group
+# reads: head_dim kv_heads ratio target n_seq n_groups, then per sequence tokens own, then per group
 # sequences prefix (groups cover the first sequences in order)
 BODY = r"""
 #include <cstdio>
@@ -21,8 +21,8 @@ BODY = r"""
 using namespace gleam;
 struct It { uint64_t tokens, prefix, own; bool partial; };
 int main() {
-  unsigned long long kvh, ratio, target, ns, ng;
-  if (scanf("%llu %llu %llu %llu %llu", &kvh, &ratio, &target, &ns, &ng) != 5) return 2;
+  unsigned long long dim, kvh, ratio, target, ns, ng;
+  if (scanf("%llu %llu %llu %llu %llu %llu", &dim, &kvh, &ratio, &target, &ns, &ng) != 6) return 2;
   std::vector<It> items(ng + ns);
   uint64_t all = 0;
   for (uint64_t s = 0; s < ns; ++s) {
@@ -45,14 +45,14 @@ int main() {
     }
     at += n;
   }
-  uint64_t cost = 0;
+  uint64_t cost[2] = {0, 0};
   for (const It& it : items)
-    if (it.tokens) cost += item_cost((uint32_t)(it.tokens * ratio), steps_of((uint32_t)it.prefix) + steps_of((uint32_t)it.own)) * kvh;
+    if (it.tokens) cost[few_rows((uint32_t)(it.tokens * ratio))] += item_cost((uint32_t)(it.tokens * ratio), steps_of((uint32_t)it.prefix) + steps_of((uint32_t)it.own)) * kvh;
   uint64_t units = 0, parts = 0;
   for (const It& it : items) {
     const uint32_t rows = (uint32_t)(it.tokens * ratio);
     const uint32_t steps = it.tokens ? steps_of((uint32_t)it.prefix) + steps_of((uint32_t)it.own) : 0;
-    const Cut c = cut_steps(steps, chunk_steps(rows, cost, (uint32_t)target));
+    const Cut c = cut_steps(steps, chunk_steps(rows, cost[few_rows(rows)], (uint32_t)target, (uint32_t)dim));
     if ((steps == 0) != (c.chunks == 0)) return 3;
     if (steps && ((uint64_t)c.chunks * c.per < steps || (uint64_t)(c.chunks - 1) * c.per >= steps)) return 4;
     units += (uint64_t)tiles_of(rows) * kvh * c.chunks;
@@ -63,7 +63,7 @@ int main() {
     if (steps_of((uint32_t)it.own) > longest[0]) longest[0] = steps_of((uint32_t)it.own);
     if (steps_of((uint32_t)it.prefix) > longest[1]) longest[1] = steps_of((uint32_t)it.prefix);
   }
-  PlanShape s{all, ns, ng, (uint32_t)kvh, (uint32_t)ratio, (uint32_t)target, (uint32_t)(longest[0] + longest[1])};
+  PlanShape s{all, ns, ng, (uint32_t)kvh, (uint32_t)ratio, (uint32_t)target, (uint32_t)(longest[0] + longest[1]), (uint32_t)dim};
   printf("%llu %llu %llu %llu\n", (unsigned long long)units, (unsigned long long)most_units(s),
          (unsigned long long)parts, (unsigned long long)most_partials(s));
 }
@@ -79,8 +79,8 @@ def plan(tmp_path_factory):
     subprocess.run([cxx, "-std=c++17", "-Wall", "-Werror", "-O1", "-I", CSRC, str(d / "plan.cpp"), "-o",
                     str(d / "plan")], check=True)
 
-    def run(kv_heads, ratio, target, seqs, groups):
-        text = " ".join(map(str, [kv_heads, ratio, target, len(seqs), len(groups)] + [x for s in seqs for x in s] +
+    def run(kv_heads, ratio, target, seqs, groups, dim=128):
+        text = " ".join(map(str, [dim, kv_heads, ratio, target, len(seqs), len(groups)] + [x for s in seqs for x in s] +
                             [x for g in groups for x in g]))
         p = subprocess.run([str(d / "plan")], input=text, capture_output=True, text=True)
         assert p.returncode == 0, (p.returncode, text[:200])
@@ -105,7 +105,7 @@ def test_bounds_hold(plan, seed):
             groups.append((n, size(rng, 1 << 18)))
             left -= n
         units, most_units, parts, most_parts = plan(rng.choice([1, 2, 5, 8, 32]), rng.choice([1, 3, 4, 8, 32]),
-                                                    rng.choice([256, 1024, 2048]), seqs, groups)
+                                                    rng.choice([256, 1024, 2048]), seqs, groups, rng.choice([64, 128, 256]))
         assert units <= most_units and parts <= most_parts, (seed, seqs[:5], groups[:5])
 
 
