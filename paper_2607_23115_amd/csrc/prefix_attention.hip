@@ -153,21 +153,28 @@ __device__ V wave_scan(V v, Op op) {
   return v;
 }
 
-// The same over the workgroup; every thread calls it. `total` gets the last value.
-template <class V, class Op>
-__device__ V block_scan(V v, V* lds, V* total, Op op) {
+// The same over the workgroup, of kN values at once (two barriers); every thread calls it. `total`
+// gets the last values.
+template <int kN, class V, class Op>
+__device__ void block_scan(V (&v)[kN], V (&total)[kN], V (*lds)[kN], Op op) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  v = wave_scan(v, op);
-  if (lane == 63) lds[wave] = v;
-  __syncthreads();
-  V all = lds[0];
-  for (int w = 1; w < (int)(blockDim.x >> 6); ++w) {
-    if (w == wave) v = op(all, v);
-    all = op(all, lds[w]);
+#pragma unroll
+  for (int i = 0; i < kN; ++i) v[i] = wave_scan(v[i], op);
+  if (lane == 63) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) lds[wave][i] = v[i];
   }
-  *total = all;
   __syncthreads();
-  return v;
+#pragma unroll
+  for (int i = 0; i < kN; ++i) {
+    V all = lds[0][i];
+    for (int w = 1; w < (int)(blockDim.x >> 6); ++w) {
+      if (w == wave) v[i] = op(all, v[i]);
+      all = op(all, lds[w][i]);
+    }
+    total[i] = all;
+  }
+  __syncthreads();
 }
 
 __device__ inline int32_t clamp_to(int32_t v, int32_t most) { return v < 0 ? 0 : v > most ? most : v; }
@@ -331,29 +338,34 @@ __device__ inline Item item_of_lane(const Item& it, uint32_t i) {
 // Offsets of up to this many sequences and groups are kept in LDS, of more in the workspace.
 constexpr uint32_t kPlanLds = 4096;
 
-// src[0..n] as non-decreasing values within [0, most], into dst and out (which may be one).
-__device__ void tidy_offsets(const int32_t* src, int32_t* dst, int32_t* out, uint32_t n, int32_t most, int32_t* lds) {
-  int32_t carry = 0;
-  for (uint32_t i0 = 0; i0 <= n; i0 += blockDim.x) {
-    const uint32_t i = i0 + threadIdx.x;
-    int32_t v = clamp_to(i <= n ? src[i] : 0, most), total;
-    v = block_scan(v, lds, &total, MaxOp());
-    v = v > carry ? v : carry;
-    if (i <= n) dst[i] = out[i] = v;
-    carry = carry > total ? carry : total;
-  }
-}
-
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a) {
-  __shared__ uint64_t lds[kPlanThreads / 64];
+  __shared__ uint64_t lds_costs[kPlanThreads / 64][2];
+  __shared__ uint32_t lds_takes[kPlanThreads / 64][4];
+  __shared__ int32_t lds_tidy[kPlanThreads / 64][2];
   __shared__ int32_t lds_q[kPlanLds + 1], lds_g[kPlanLds + 1];
-  int32_t* lds32 = reinterpret_cast<int32_t*>(lds);
   const Ws& w = a.ws;
-  const uint32_t n_items = a.n_groups + a.n_seq;
+  const uint32_t n_items = a.n_groups + a.n_seq, threads = blockDim.x;
   int32_t* const q = a.n_seq <= kPlanLds ? lds_q : w.q_first;
   int32_t* const g = a.n_groups <= kPlanLds ? lds_g : w.group_first;
-  tidy_offsets(a.q_first, q, w.q_first, a.n_seq, (int32_t)a.n_tokens, lds32);
-  if (a.n_groups) tidy_offsets(a.group_first, g, w.group_first, a.n_groups, (int32_t)a.n_seq, lds32);
+
+  // the offsets as non-decreasing values in their ranges
+  const uint32_t offsets = a.n_groups > a.n_seq ? a.n_groups : a.n_seq;
+  int32_t carry[2] = {0, 0};
+  for (uint32_t i0 = 0; i0 <= offsets; i0 += threads) {
+    const uint32_t i = i0 + threadIdx.x;
+    const bool has_g = a.n_groups && i <= a.n_groups;
+    int32_t v[2] = {clamp_to(i <= a.n_seq ? a.q_first[i] : 0, (int32_t)a.n_tokens),
+                    clamp_to(has_g ? a.group_first[i] : 0, (int32_t)a.n_seq)};
+    int32_t total[2];
+    block_scan(v, total, lds_tidy, MaxOp());
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      v[c] = v[c] > carry[c] ? v[c] : carry[c];
+      carry[c] = carry[c] > total[c] ? carry[c] : total[c];
+    }
+    if (i <= a.n_seq) w.q_first[i] = q[i] = v[0];
+    if (has_g) g[i] = v[1];
+  }
   __syncthreads();
   auto group_of = [&](uint32_t s) {
     if ((int32_t)s < g[0] || (int32_t)s >= g[a.n_groups]) return -1;
@@ -368,53 +380,49 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a) {
   auto of = [](const int32_t* v) { return [v](uint32_t i) { return v[i]; }; };
 
   // the items without their cuts, and the cost of all
-  Costs cost{0, 0};
+  uint64_t costs[2] = {0, 0}, all_costs[2];
   uint32_t joins = q[0] > 0 || q[a.n_seq] < (int32_t)a.n_tokens;
   Item first{};  // of the thread; those of later rounds go through the workspace
-  for (uint32_t i = threadIdx.x; i < n_items; i += blockDim.x) {
+  for (uint32_t i = threadIdx.x; i < n_items; i += threads) {
     Item it = make_item(a, i, of(q), of(g), of(a.own_len), of(a.prefix_len), group_of);
     const Costs c = item_costs(a, it);
-    cost.tiles += c.tiles;
-    cost.fews += c.fews;
+    costs[0] += c.tiles;
+    costs[1] += c.fews;
     if (i >= a.n_groups && it.tokens && item_steps(it) == 0) joins = 1;
-    if (i < blockDim.x) first = it;
+    if (i < threads) first = it;
     else w.items[i] = it;
     if (a.n_groups && i >= a.n_groups) w.seq_group[i - a.n_groups] = group_of(i - a.n_groups);
   }
-  Costs all_cost;
-  block_scan(cost.tiles, lds, &all_cost.tiles, SumOp());
-  block_scan(cost.fews, lds, &all_cost.fews, SumOp());
+  block_scan(costs, all_costs, lds_costs, SumOp());
 
   // chunks, units and partial rows
-  Takes before{0, 0, 0};
-  uint32_t* const ldsu = reinterpret_cast<uint32_t*>(lds);
-  for (uint32_t i0 = 0; i0 < n_items; i0 += blockDim.x) {
+  uint32_t before[4] = {0, 0, 0, 0};
+  for (uint32_t i0 = 0; i0 < n_items; i0 += threads) {
     const uint32_t i = i0 + threadIdx.x;
     Item it = first;
     if (i0 > 0) {
       it = Item{};
       if (i < n_items) it = w.items[i];
     }
-    const Takes mine = cut_item(a, it, all_cost);
-    Takes total;
-    it.tile_first = before.tiles + block_scan(mine.tiles, ldsu, &total.tiles, SumOp()) - mine.tiles;
-    it.few_first = before.fews + block_scan(mine.fews, ldsu, &total.fews, SumOp()) - mine.fews;
-    it.part_first = before.parts + block_scan(mine.parts, ldsu, &total.parts, SumOp()) - mine.parts;
+    const Takes mine = cut_item(a, it, Costs{all_costs[0], all_costs[1]});
+    uint32_t sum[4] = {mine.tiles, mine.fews, mine.parts, joins | (mine.parts != 0)}, total[4];
+    joins = 0;
+    block_scan(sum, total, lds_takes, SumOp());
+    it.tile_first = before[0] + sum[0] - mine.tiles;
+    it.few_first = before[1] + sum[1] - mine.fews;
+    it.part_first = before[2] + sum[2] - mine.parts;
     if (i < n_items) {
       w.items[i] = it;
       w.tile_first[i] = it.tile_first;
       w.few_first[i] = it.few_first;
     }
-    joins |= mine.parts != 0;
-    before.tiles += total.tiles;
-    before.fews += total.fews;
-    before.parts += total.parts;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) before[c] += total[c];
   }
-  joins = __syncthreads_or((int)joins);
   if (threadIdx.x == 0) {
-    w.head->tiles = before.tiles;
-    w.head->fews = before.fews;
-    w.head->joins = joins;
+    w.head->tiles = before[0];
+    w.head->fews = before[1];
+    w.head->joins = before[3];
   }
 }
 
@@ -1179,9 +1187,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(Atte
     const uint64_t le = __ballot(lane < n_items && (few ? plan.it.few_first : plan.it.tile_first) <= u);
     unit.it = item_of_lane(plan.it, 63 - __clzll((long long)le));
   } else {
-    const uint32_t* const first = few ? w.few_first : w.tile_first;
-    const uint32_t at = uniform(wave_search<uint32_t>(first, n_items, u));
-    unit.it = w.items[at];
+    unit.it = w.items[uniform(wave_search<uint32_t>(few ? w.few_first : w.tile_first, n_items, u))];
   }
   u -= few ? unit.it.few_first : unit.it.tile_first;
   unit.head = u % a.kv_heads;
@@ -1349,7 +1355,7 @@ gleam_status validate_attention(const gleam_kv_pages* kv, const gleam_prefix_bat
   const uint64_t most = steps_of((uint32_t)(b->own_width * kv->page_tokens)) +
                         (uint64_t)steps_of((uint32_t)(b->prefix_width * kv->page_tokens));
   shape->most_steps = (uint32_t)most;
-  if (most_units(*shape) > max_workgroups(kThreads) || most_partials(*shape) > UINT32_MAX) {
+  if (most_units_any_width(*shape) > max_workgroups(kThreads) || most_partials(*shape) > UINT32_MAX) {
     set_error("%s: more work than one launch holds", who);
     return GLEAM_E_UNSUPPORTED;
   }
@@ -1361,8 +1367,8 @@ gleam_status launch_all(const AttendArgs& a, uint32_t units, hipStream_t stream)
   gleam_status st;
   const uint32_t items = a.n_groups + a.n_seq;
   if (items > kWaveItems && a.n_seq > 0) {
-    // as few threads as hold the items: a barrier of 16 waves takes longer than one of 4
-    const uint32_t threads = items <= 256 ? 256 : kPlanThreads;
+    // as few threads as hold the offsets: a barrier of 16 waves takes longer than one of 3
+    const uint32_t threads = items < kPlanThreads ? (items + 64) / 64 * 64 : kPlanThreads;
     hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(threads), 0, stream, a);
     if ((st = launch_status("plan_kernel")) != GLEAM_OK) return st;
   }

@@ -82,12 +82,15 @@ GLEAM_HD Cut cut_steps(uint32_t steps, uint32_t most) {
 // kMinFewSteps. Tiles: an item of n rows has at most n / kFewRows + 1 of them, and at most
 // n / kTileRows + kMostFew / kFewRows, and a token's rows are in two items at most, its group's
 // and its sequence's.
-GLEAM_HD uint64_t most_units(const PlanShape& s) {
+GLEAM_HD uint64_t most_first_units(const PlanShape& s) {  // kv_heads * tiles
   const uint64_t rows = 2 * s.n_tokens * s.ratio, items = s.n_groups + s.n_seq;
   const uint64_t few = items + rows / kFewRows, tile = kMostFew / kFewRows * items + rows / kTileRows;
-  const uint64_t tiles = s.kv_heads * (few < tile ? few : tile);
-  const uint64_t cuts = tiles * div_up(s.most_steps, kMinFewSteps);
-  return 2 * s.target + tiles < cuts ? 2 * s.target + tiles : cuts;
+  return s.kv_heads * (few < tile ? few : tile);
+}
+GLEAM_HD uint64_t most_units_any_width(const PlanShape& s) { return 2ull * s.target + most_first_units(s); }
+GLEAM_HD uint64_t most_units(const PlanShape& s) {
+  const uint64_t cuts = most_first_units(s) * div_up(s.most_steps, kMinFewSteps), any = most_units_any_width(s);
+  return cuts < any ? cuts : any;
 }
 
 // Rows of partial results: an item that is cut, or shares its rows with another, has
