@@ -179,8 +179,9 @@ __device__ void block_scan(V (&v)[kN], V (&total)[kN], V (*lds)[kN], Op op) {
 
 __device__ inline int32_t clamp_to(int32_t v, int32_t most) { return v < 0 ? 0 : v > most ? most : v; }
 
-__device__ inline uint32_t clamp_keys(int32_t n, uint32_t width, uint32_t page_log2) {
-  return (uint32_t)clamp_to(n, (int32_t)(width << page_log2));
+// How many keys a length means: none in a cache without pages.
+__device__ inline uint32_t clamp_keys(const AttendArgs& a, int32_t n, uint32_t width) {
+  return a.n_pages ? (uint32_t)clamp_to(n, (int32_t)(width << a.page_log2)) : 0;
 }
 
 // Item i without its cut. q(i), g(i): the offsets, already tidy; own(s), prefix(g): lengths as
@@ -191,7 +192,7 @@ __device__ Item make_item(const AttendArgs& a, uint32_t i, const Q& q, const G& 
   const bool is_group = i < a.n_groups;
   const uint32_t s = is_group || i >= a.n_groups + a.n_seq ? 0 : i - a.n_groups;
   const uint32_t t0 = (uint32_t)q(s), t1 = (uint32_t)q(s + 1);
-  const uint32_t own_keys = clamp_keys(own(s), a.own_width, a.page_log2);
+  const uint32_t own_keys = clamp_keys(a, own(s), a.own_width);
   uint32_t shared = 0, g0 = 0, g1 = 0, row = 0;  // the group's prefix
   if (a.n_groups) {
     const int32_t of_seq = group_of(s), in = is_group ? (int32_t)i : of_seq;
@@ -199,7 +200,7 @@ __device__ Item make_item(const AttendArgs& a, uint32_t i, const Q& q, const G& 
     const uint32_t s0 = (uint32_t)g(row), s1 = (uint32_t)g(row + 1);
     g0 = (uint32_t)q(s0);
     g1 = (uint32_t)q(s1);
-    const uint32_t keys = clamp_keys(prefix(row), a.prefix_width, a.page_log2);
+    const uint32_t keys = clamp_keys(a, prefix(row), a.prefix_width);
     if (in >= 0) shared = keys;
     // keys that the group's item has, and the sequence's has not
     if (joint_group((uint64_t)(g1 - g0) * a.ratio, s1 - s0) == is_group) {
@@ -509,6 +510,14 @@ __device__ inline Keys16 keys16(const AttendArgs& a, uint32_t page, uint32_t key
   t.v = a.v + (int64_t)page * a.v_page + (int64_t)place * a.v_place + (int64_t)head * a.v_head;
   t.n = keys - key < 16 ? keys - key : 16;
   return t;
+}
+
+// 16 bytes at a base that is the same in all lanes and the lane's own offset, added by the load.
+__device__ inline u32x4v load_at(const uint8_t* base, uint32_t offset) {
+  uint64_t x = reinterpret_cast<uint64_t>(base);
+  asm("" : "+s"(x));  // kept apart from the offset
+  typedef const __attribute__((address_space(1))) uint8_t* Global;
+  return *reinterpret_cast<const __attribute__((address_space(1))) u32x4v*>(reinterpret_cast<Global>(x) + offset);
 }
 
 // Calls add(i, value) for kN values, with 0 in the place of finite ones.
@@ -932,6 +941,9 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
   uint32_t end = St::kSubs * (unit.chunk + 1) * it.per;
   if (end > all_subs) end = all_subs;
   const uint32_t first = St::kSubs * unit.chunk * it.per;
+  // after wave_end the wave's rows see nothing (rows that do not exist, from the start): it only stages
+  uint32_t wave_end = wave_row < rows ? prefix_subs + (own_wave_most + St::kKeys - 1) / St::kKeys : first;
+  if (wave_end > end) wave_end = end;
 
   // of the wave's rows of a sub-step the first key, and all keys there are; its page for the 64
   // sub-steps from page_sub on, one a lane
@@ -946,16 +958,16 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
   };
   uint32_t page_sub = first, pages = pages_from(first);
 
-  // those rows, from memory to registers and from there to LDS
+  // Those rows, from memory to registers and from there to LDS. All of them are loaded, whether keys
+  // or not: they lie in one page, and in the cache's first where there is no page (without keys
+  // there are no sub-steps, without pages no keys). Keys that are none are masked, and the values
+  // in their place set to 0.
+  constexpr uint32_t kLoadRows = 64 / St::kPieces;  // rows of one load
+  const uint32_t piece = lane % St::kPieces, load_row = lane / St::kPieces;
+  const uint32_t k_off = load_row * (uint32_t)a.k_place + piece * 16;
+  const uint32_t v_off = load_row * (uint32_t)a.v_place + piece * 16;
   u32x4v stage_k[St::kLoads], stage_v[St::kLoads];
   uint32_t stage_flags = 0;
-  uint32_t k_off[St::kLoads], v_off[St::kLoads];
-#pragma unroll
-  for (int i = 0; i < St::kLoads; ++i) {
-    const uint32_t r = (i * 64 + lane) / St::kPieces, piece = (i * 64 + lane) % St::kPieces;
-    k_off[i] = r * (uint32_t)a.k_place + piece * 16;
-    v_off[i] = r * (uint32_t)a.v_place + piece * 16;
-  }
   auto stage_load = [&](uint32_t s) {
     if (s - page_sub >= 64) {
       page_sub = s;
@@ -964,25 +976,17 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
     const uint32_t page = (uint32_t)__builtin_amdgcn_readlane((int)pages, (int)(s - page_sub));
     const Keys16 t = keys16(a, page, key_of(s), keys_of(s), head);
     stage_flags = t.n < (uint32_t)St::kRows ? t.n : (uint32_t)St::kRows;
-    if (t.n >= (uint32_t)St::kRows) {  // no branch in a lane, and addresses that are a base and the lane's offset
 #pragma unroll
-      for (int i = 0; i < St::kLoads; ++i) {
-        stage_k[i] = *reinterpret_cast<const u32x4v*>(t.k + k_off[i]);
-        stage_v[i] = *reinterpret_cast<const u32x4v*>(t.v + v_off[i]);
-      }
-    } else {
+    for (int i = 0; i < St::kLoads; ++i) stage_k[i] = load_at(t.k + i * kLoadRows * a.k_place, k_off);
 #pragma unroll
-      for (int i = 0; i < St::kLoads; ++i) {
-        stage_k[i] = stage_v[i] = (u32x4v)0u;
-        if ((i * 64 + lane) / St::kPieces < t.n) {
-          stage_k[i] = *reinterpret_cast<const u32x4v*>(t.k + k_off[i]);
-          stage_v[i] = *reinterpret_cast<const u32x4v*>(t.v + v_off[i]);
-        }
-      }
-    }
+    for (int i = 0; i < St::kLoads; ++i) stage_v[i] = load_at(t.v + i * kLoadRows * a.v_place, v_off);
   };
-  auto stage_store = [&](uint32_t s) {
-    const uint32_t buf = (s - first) & 1;
+  auto stage_tidy = [&](uint32_t s) {
+    if (stage_flags < (uint32_t)St::kRows) {
+#pragma unroll
+      for (int i = 0; i < St::kLoads; ++i)
+        if (i * kLoadRows + load_row >= stage_flags) stage_v[i] = (u32x4v)0u;
+    }
     if (s >= prefix_subs && (s - prefix_subs + 1) * St::kKeys > own_group_least) {
       uint32_t any = 0;
 #pragma unroll
@@ -997,9 +1001,12 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
           for (int c = 0; c < 4; ++c) stage_v[i][c] = clear_special<T>(stage_v[i][c]);
       }
     }
+  };
+  auto stage_store = [&](uint32_t s) {
+    const uint32_t buf = (s - first) & 1;
 #pragma unroll
     for (int i = 0; i < St::kLoads; ++i) {
-      const uint32_t r = wave * St::kRows + (i * 64 + lane) / St::kPieces, piece = (i * 64 + lane) % St::kPieces;
+      const uint32_t r = wave * St::kRows + i * kLoadRows + load_row;
       *reinterpret_cast<u32x4v*>(lds_k + buf * St::kTile + St::k_at(r, piece)) = stage_k[i];
       *reinterpret_cast<u32x4v*>(lds_v + buf * St::kTile + St::v_at(r, piece)) = stage_v[i];
     }
@@ -1014,18 +1021,12 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
 
   // where the lane reads: K rows and pieces, V quads of keys and dims
   const uint32_t k_lane = St::k_at(n, h);
-  uint32_t v_lane[kO];
-  {
-    const uint32_t quad = (lane & 15) >> 2, half = (lane >> 4) & 1;
-#pragma unroll
-    for (int i = 0; i < kO; ++i) {
-      const uint32_t r = 4 * h + quad;
-      v_lane[i] = r * St::kRow + (((2 * i + half) ^ St::v_swizzle(r)) << 5) + (lane & 3) * 8;
-    }
-  }
+  const uint32_t v_row = 4 * h + ((lane & 15) >> 2);
+  const uint32_t v_lane = v_row * St::kRow + ((((lane >> 4) & 1) ^ St::v_swizzle(v_row)) << 5) + (lane & 3) * 8;
 
   if (first < end) {
     stage_load(first);
+    stage_tidy(first);
     stage_store(first);
     if (first + 1 < end) stage_load(first + 1);
   }
@@ -1034,11 +1035,14 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
   for (uint32_t sub = first; sub < end; ++sub) {
     const uint32_t buf = (sub - first) & 1;
     __syncthreads();
-    if (sub + 1 < end) stage_store(sub + 1);
+    if (sub + 1 < end) {
+      stage_tidy(sub + 1);
+      stage_store(sub + 1);
+    }
     if (sub + 2 < end) stage_load(sub + 2);
-    const bool shared = sub < prefix_subs;
-    const uint32_t key = (shared ? sub : sub - prefix_subs) * St::kKeys;
-    if (wave_row < rows && (shared || key < own_wave_most)) {
+    if (sub < wave_end) {
+      const bool shared = sub < prefix_subs;
+      const uint32_t key = (shared ? sub : sub - prefix_subs) * St::kKeys;
       const char* const kb = lds_k + buf * St::kTile;
       const char* const vb = lds_v + buf * St::kTile;
       const uint32_t flags = uniform(*reinterpret_cast<const uint32_t*>(lds_flags + buf * kWaves));
@@ -1098,8 +1102,8 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
 #pragma unroll
         for (int i = 0; i < kO; ++i) {
           Pack8 v;
-          const u32x2v x = read_transposed(vb + kk * 16 * St::kRow + v_lane[i]);
-          const u32x2v y = read_transposed(vb + (kk * 16 + 8) * St::kRow + v_lane[i]);
+          const u32x2v x = read_transposed(vb + kk * 16 * St::kRow + (v_lane ^ (i << 6)));
+          const u32x2v y = read_transposed(vb + (kk * 16 + 8) * St::kRow + (v_lane ^ (i << 6)));
           v.u = (u32x4v){x[0], x[1], y[0], y[1]};
           o[i] = Mfma32<T>::run(get(v, T()), get(p[kk], T()), o[i]);
         }
