@@ -40,6 +40,7 @@ constexpr int kPlanThreads = 1024;
 constexpr float kRise = 8.f;  // log2
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr uint64_t kMostSeq = 1ull << 20;
+constexpr uint64_t kPassing = 128ull << 20;  // bytes of an item's keys and values
 constexpr uint32_t kWideJoin = 256;    // up to this many rows are joined by a workgroup each
 constexpr uint32_t kMostJoins = 2048;  // workgroups of the others: those that the GPU holds at once
 
@@ -512,12 +513,15 @@ __device__ inline Keys16 keys16(const AttendArgs& a, uint32_t page, uint32_t key
   return t;
 }
 
-// 16 bytes at a base that is the same in all lanes and the lane's own offset, added by the load.
-__device__ inline u32x4v load_at(const uint8_t* base, uint32_t offset) {
+// What is at a base that is the same in all lanes and the lane's own offset, added by the load;
+// kOnce: what nobody reads again soon is not kept in the caches.
+template <class V, bool kOnce = false>
+__device__ inline V load_at(const uint8_t* base, uint32_t offset) {
   uint64_t x = reinterpret_cast<uint64_t>(base);
   asm("" : "+s"(x));  // kept apart from the offset
   typedef const __attribute__((address_space(1))) uint8_t* Global;
-  return *reinterpret_cast<const __attribute__((address_space(1))) u32x4v*>(reinterpret_cast<Global>(x) + offset);
+  const auto* p = reinterpret_cast<const __attribute__((address_space(1))) V*>(reinterpret_cast<Global>(x) + offset);
+  return kOnce ? __builtin_nontemporal_load(p) : *p;
 }
 
 // Calls add(i, value) for kN values, with 0 in the place of finite ones.
@@ -628,27 +632,37 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
   };
   uint32_t page_half = begin, pages = pages_from(begin);
 
-  // The keys and values of two halves: those of the next are on their way during the products.
+  // The keys and values of two halves: those of the next are on their way during the products. All
+  // places of 16 are loaded, whether keys or not: they lie in one page, and in the cache's first
+  // where there is no page (without pages there are no keys, without keys no halves). Keys that are
+  // none are masked, and the values in their place set to 0.
   u32x4v kk[2][2][kKMfma];
   uint32_t vv[2][8][kWords], exist[2][2];
   const uint32_t k_off = n * (uint32_t)a.k_place + g * 16;
   uint32_t v_off[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) v_off[e] = (4 * g + e) * (uint32_t)a.v_place + n * (kDims * 2);
-  auto load_v = [&](uint32_t (&to)[kWords], const uint8_t* p) {
-    if constexpr (kDims == 4) {
-      const u32x2v x = *reinterpret_cast<const u32x2v*>(p);
-      to[0] = x[0];
-      to[1] = x[1];
-    } else {
+  auto load_tile = [&](const Keys16& t, auto set_, int b, auto once_) {
+    constexpr int set = decltype(set_)::value;
+    constexpr bool kOnce = decltype(once_)::value;
 #pragma unroll
-      for (int c = 0; c < kDims / 8; ++c) {
-        const u32x4v x = *reinterpret_cast<const u32x4v*>(p + 16 * c);
+    for (int i = 0; i < kKMfma; ++i) kk[set][b][i] = load_at<u32x4v, kOnce>(t.k + i * 64, k_off);
 #pragma unroll
-        for (int d = 0; d < 4; ++d) to[4 * c + d] = x[d];
+    for (int e = 0; e < 4; ++e) {
+      typedef std::conditional_t<kDims == 4, u32x2v, u32x4v> Part;
+      constexpr int kPart = sizeof(Part) / 4;
+#pragma unroll
+      for (int c = 0; c < kWords / kPart; ++c) {
+        const Part x = load_at<Part, kOnce>(t.v + 4 * kPart * c, v_off[e]);
+#pragma unroll
+        for (int d = 0; d < kPart; ++d) vv[set][4 * b + e][kPart * c + d] = x[d];
       }
     }
   };
+  // Keys and values that one tile reads, and that are too many for the caches to have at the next
+  // call, are not kept there (one token of 8 key heads: behind 131,072 keys 90 us, 102 where they
+  // are; behind 32,768 31.0 and 30.5).
+  const bool once = rows <= kFewRows && ((uint64_t)it.prefix_keys + it.own_keys) * a.kv_heads * (4 * D) >= kPassing;
   auto load_half = [&](uint32_t half, auto set_) {
     constexpr int set = decltype(set_)::value;
     if (half - page_half >= 32 * kWaves) {
@@ -661,23 +675,12 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
       const uint32_t page = (uint32_t)__builtin_amdgcn_readlane((int)pages, (int)(at + b));
       const Keys16 t = keys16(a, page, key_of(half) + 16 * b, keys_of(half), head);
       exist[set][b] = t.n;
-      if (t.n == 16) {
-#pragma unroll
-        for (int i = 0; i < kKMfma; ++i) kk[set][b][i] = *reinterpret_cast<const u32x4v*>(t.k + k_off + i * 64);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) load_v(vv[set][4 * b + e], t.v + v_off[e]);
+      if (once) {
+        asm volatile("");  // the two kinds of loads are not to be merged into one
+        load_tile(t, set_, b, std::true_type());
+        asm volatile("");
       } else {
-#pragma unroll
-        for (int i = 0; i < kKMfma; ++i) {
-          kk[set][b][i] = (u32x4v)0u;
-          if (n < t.n) kk[set][b][i] = *reinterpret_cast<const u32x4v*>(t.k + k_off + i * 64);
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-#pragma unroll
-          for (int c = 0; c < kWords; ++c) vv[set][4 * b + e][c] = 0;
-          if (4 * g + e < t.n) load_v(vv[set][4 * b + e], t.v + v_off[e]);
-        }
+        load_tile(t, set_, b, std::false_type());
       }
     }
   };
@@ -730,6 +733,13 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
       const float y = __builtin_amdgcn_exp2f(x[e] - m_use);
       l += y;
       put(p, e, y, T());
+    }
+    if (exist[set][0] + exist[set][1] < 32) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int c = 0; c < kWords; ++c)
+          if (4 * g + (e & 3) >= exist[set][e >> 2]) vv[set][e][c] = 0;
     }
     if (!shared && masked) {
       uint32_t any = 0;
@@ -977,9 +987,9 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
     const Keys16 t = keys16(a, page, key_of(s), keys_of(s), head);
     stage_flags = t.n < (uint32_t)St::kRows ? t.n : (uint32_t)St::kRows;
 #pragma unroll
-    for (int i = 0; i < St::kLoads; ++i) stage_k[i] = load_at(t.k + i * kLoadRows * a.k_place, k_off);
+    for (int i = 0; i < St::kLoads; ++i) stage_k[i] = load_at<u32x4v>(t.k + i * kLoadRows * a.k_place, k_off);
 #pragma unroll
-    for (int i = 0; i < St::kLoads; ++i) stage_v[i] = load_at(t.v + i * kLoadRows * a.v_place, v_off);
+    for (int i = 0; i < St::kLoads; ++i) stage_v[i] = load_at<u32x4v>(t.v + i * kLoadRows * a.v_place, v_off);
   };
   auto stage_tidy = [&](uint32_t s) {
     if (stage_flags < (uint32_t)St::kRows) {
