@@ -930,10 +930,11 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
   const uint32_t own_group_least = uniform(seen_by(unit.tile * kTileRows));
   const uint32_t own_most = uniform(seen_by(unit.tile * kTileRows + kTileRows - 1));
 
-  // Scores are scaled after the product; a scale below zero is taken from the queries' signs, so
-  // that the largest score is the largest product's.
-  const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;
-  const float scale = fabsf(a.scale_log2);
+  // Scores are scaled after the product, and masked ones are minus infinity before it: a scale below
+  // zero is taken from the queries' signs, so that the largest score is the largest product's, and
+  // one of zero is taken as queries of zero.
+  const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u, keep = a.scale_log2 == 0.f ? 0u : ~0u;
+  const float scale = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);
   Pack8 q[kQ];
 #pragma unroll
   for (int i = 0; i < kQ; ++i) {
@@ -941,7 +942,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
     if (row_live)
       q[i].u = *reinterpret_cast<const u32x4v*>(a.q + (int64_t)token * a.q_token + (int64_t)q_head * a.q_head +
                                                 (i * 16 + h * 8) * 2);
-    q[i].u ^= flip;
+    q[i].u = (q[i].u ^ flip) & keep;
   }
 
   const int32_t* const prefix_pages = a.prefix_pages + (uint64_t)it.prefix_row * a.prefix_width;

@@ -181,6 +181,13 @@ def test_scale_and_strided_queries():
     c.check()
 
 
+def test_a_scale_of_zero_takes_the_mean_of_what_is_seen():
+    for n, own, prefix in ((1, 70, 40), (100, 130, 75), (150, 100, 0)):
+        c = Case([n, 1], [own, 3], [(0, 2, prefix)], 4, 2, 64, 16, BF16)
+        c.scale = 0.0
+        c.check()
+
+
 def test_later_keys_and_values_may_be_anything():
     """Keys and values of a sequence's later tokens hold NaN and infinities: earlier tokens of
     the same call do not see them, later ones do."""
