@@ -752,6 +752,122 @@ def transfer_path(args, g, torch, threads):
     print(json.dumps(out), flush=True)
 
 
+def serve_path(args, g, torch):
+    """One attention layer of a serving loop on the paged key/value cache: 64 users of the 7B
+    decoder (32 heads of 128, fp16) behind one system prompt of 2,048 tokens. The prompts are
+    identified in blocks of 1,024 tokens (gleam_detect): a held block's value is the first of its
+    pages. The users' own prompt tokens go in by one kv_append and are answered by one
+    prefix_attention; a timed step is the next token of every user through both calls.
+    Queries, keys and values are synthetic N(0, 1)."""
+    users, system, block, page, heads, d = 64, 2048, 1024, 64, 32, 128
+    K, total, dt = args.steps, args.warmup + args.steps, torch.float16
+    rng = np.random.default_rng(2607)
+    gen = torch.Generator(device="cuda").manual_seed(2607)
+    own = rng.integers(1, 300, users)
+    prompts = [rng.integers(0, 32000, system, dtype=np.int32)]
+    prompts += [np.concatenate([prompts[0], rng.integers(0, 32000, n, dtype=np.int32)]) for n in own]
+
+    def batch_of(rows):
+        lens = np.array([4 * r.size for r in rows])
+        offs = np.concatenate([[0], np.cumsum(lens)[:-1]])
+        return g.Batch.from_arena(torch.from_numpy(np.concatenate(rows).view(np.uint8)).to("cuda"), offs, lens,
+                                  4 * block)
+
+    def dev(x, dtype=torch.int32):
+        return torch.from_numpy(np.ascontiguousarray(x)).to("cuda", dtype)
+
+    def product(tokens):  # stands for the layer's product: queries, keys and values side by side
+        x = torch.randn(tokens, 3 * heads, d, generator=gen, device="cuda").to(dt)
+        return x[:, :heads], x[:, heads:2 * heads], x[:, 2 * heads:]
+
+    shared = system // page
+    each = [-(-(int(n) + total) // page) for n in own]
+    pool = [torch.zeros(shared + sum(each), heads, page, d, dtype=dt, device="cuda").transpose(1, 2) for _ in range(2)]
+    rotary = g.rotary_table(system + 300 + total, d)
+    # the system prompt was served before: its keys and values lie in the first pages
+    q, k, v = product(system)
+    g.kv_append(k, v, *pool, torch.arange(system, device="cuda"), positions=dev(np.arange(system)), rotary=rotary)
+    table = g.Cache(1 << 10)
+    table.insert(g.fp_chunks(batch_of(prompts[:1])), dev(np.arange(0, shared, block // page), torch.int64))
+
+    # the users' prompts: leading blocks that are held need no work
+    prompt_batch = batch_of(prompts[1:])
+    found = g.detect(prompt_batch, table)
+    status, ref = found.status.cpu().numpy(), g.as_u64(found.ref)
+    first = np.concatenate([[0], np.cumsum([-(-p.size // block) for p in prompts[1:]])])
+    for i in range(users):
+        lead = slice(first[i], first[i] + system // block)
+        if not (status[lead] == g.HIT_CACHE).all() or not np.array_equal(ref[lead], np.arange(0, shared, block // page)):
+            raise SystemExit("a prompt's shared blocks were not found")
+    group_first, prefix_pages, prefix_len = dev([0, users]), dev(np.arange(shared)[None]), dev([system])
+    own_rows = np.full((users, max(each)), -1, np.int32)
+    at = shared
+    for i, n in enumerate(each):
+        own_rows[i, :n] = np.arange(at, at + n)
+        at += n
+    own_pages = dev(own_rows)
+
+    def places(user, j):  # of own token j
+        return own_rows[user, j // page].astype(np.int64) * page + j % page
+
+    q, k, v = product(int(own.sum()))
+    user, j = np.repeat(np.arange(users), own), np.concatenate([np.arange(n) for n in own])
+    q = g.kv_append(k, v, *pool, dev(places(user, j), torch.int64), q=q, positions=dev(system + j), rotary=rotary)
+    g.prefix_attention(q, *pool, dev(np.concatenate([[0], np.cumsum(own)])), own_pages, dev(own),
+                       group_first, prefix_pages, prefix_len)
+
+    everyone = np.arange(users)
+    q_first = dev(np.arange(users + 1))
+    rows = [product(users) for _ in range(total)]
+    slots = [dev(places(everyone, own + t), torch.int64) for t in range(total)]
+    positions = [dev(system + own + t) for t in range(total)]
+    lens = [dev(own + t + 1) for t in range(total)]
+    out = torch.empty(users, heads, d, dtype=dt, device="cuda")
+    ws = g.prefix_attention_workspace(*pool, users, heads, users, 1)
+
+    def step(t):
+        q, k, v = rows[t]
+        q = g.kv_append(k, v, *pool, slots[t], q=q, positions=positions[t], rotary=rotary)
+        g.prefix_attention(q, *pool, q_first, own_pages, lens[t], group_first, prefix_pages, prefix_len, out=out, ws=ws)
+        return q
+
+    for t in range(args.warmup):
+        step(t)
+    torch.cuda.synchronize()
+    t0 = time.perf_counter()
+    for t in range(args.warmup, total):
+        q = step(t)
+    torch.cuda.synchronize()
+    ms = (time.perf_counter() - t0) / K * 1e3
+    # the last step's answers in 64 bits, from what the pages hold
+    worst = 0.0
+    for i in (0, users // 2, users - 1):
+        rows_of = torch.cat([prefix_pages[0], own_pages[i, :each[i]]]).long()
+        kk, vv = (x[rows_of].reshape(-1, heads, d)[:system + int(own[i]) + total].double() for x in pool)
+        p = torch.softmax((q[i].double()[None] * kk).sum(-1) * d ** -0.5, 0)
+        worst = max(worst, float(((p[..., None] * vv).sum(0) - out[i].double()).abs().max()))
+    # one rounding of each exponential and of the answer, values N(0, 1) up to 6
+    if not worst <= 6 * 2.0 ** -10:
+        raise SystemExit(f"answers differ from those in 64 bits by {worst}")
+    held = system + int(own.sum()) + users * (args.warmup + (K + 1) / 2)
+    moved = int(held * heads * d * 4 + users * heads * d * (6 + 4 + 4))
+    out = {"metric": "tokens/s through one attention layer's paged cache (append and attention), 64 users behind "
+                     "2,048 shared tokens, 1 MI355X",
+           "value": round(users / (ms * 1e-3), 1), "unit": "tokens/s", "n_gpus": 1, "steps": K, "warmup": args.warmup,
+           "ms_per_step": round(ms, 4), "higher_is_better": True, "scaling": "weak", "vs_baseline": None,
+           "dtype": "fp16", "data": "synthetic",
+           "config": {"workload": "next token of 64 users, 32 heads of 128, pages of 64, 1 to 299 prompt tokens of "
+                                  "their own", "users": users, "shared_tokens": system,
+                      "own_tokens": int(own.sum()), "check": "answers of three users against 64-bit attention",
+                      "worst_difference": worst},
+           "roofline": {"bound": "hbm", "kernel": "append_kernel, attend_kernel, join_kernel",
+                        "achieved": round(moved / (ms * 1e-3) / 1e9, 1), "peak": HBM_PEAK_GBS, "unit": "GB/s",
+                        "frac": round(moved / (ms * 1e-3) / 1e9 / HBM_PEAK_GBS, 4), "traffic": None,
+                        "algorithmic_bytes": moved},
+           "cpu_baseline": None}
+    print(json.dumps(out), flush=True)
+
+
 WORKLOADS = {"decoder7b": build_decoder7b, "random16": build_random16, "small_copies": build_small_copies,
              "resnet50": build_resnet50, "large_bf16": build_large_bf16}
 
@@ -1001,11 +1117,12 @@ def main():
     ap.add_argument("--cpu-budget-gb", type=float, default=20.0)
     ap.add_argument("--copy-calibration", action="store_true")
     ap.add_argument("--path", default="detect", choices=["detect", "identify", "md5prefix", "lifecycle", "transfer", "remap",
-                                                          "first_writes"],
+                                                          "first_writes", "serve"],
                     help="detect: fingerprint+lookup+compact (default); identify: free-time weight "
                          "identification (block and leaf level); md5prefix: the paper's MD5-of-first-1024-bits "
                          "identifier and its exposure; lifecycle: evict/export/erase; transfer: send plan, "
-                         "packing and restore; remap: the address-remap map; first_writes: the first-write rule")
+                         "packing and restore; remap: the address-remap map; first_writes: the first-write rule; "
+                         "serve: decoding steps on the paged key/value cache")
     ap.add_argument("--no-settle", action="store_true",
                     help="skip the untimed streaming reads that bring the engine clock to its steady "
                          "state before the warm-up")
@@ -1052,6 +1169,9 @@ def main():
     threads = host_threads()
     if args.path == "first_writes":
         first_writes_path(args, g, torch)
+        return
+    if args.path == "serve":
+        serve_path(args, g, torch)
         return
     if args.path == "lifecycle":
         lifecycle_path(args, g, torch)
