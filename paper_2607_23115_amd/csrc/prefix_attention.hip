@@ -24,7 +24,9 @@
 //           brings makes its own scores, once exponentiated, P's operand as they are. As V's
 //           operand a lane holds those 8 keys' dims (lane % 16) * D/16 .. + D/16, loaded row by
 //           row and transposed within the lane.
-// With few rows this is bound by reading the keys and values once.
+// With few rows this is bound by reading the keys and values once: one token of 32 heads behind
+// 131,071 keys of 8 heads of 128 takes 84 us (6.4 TB/s; a plain read reaches 7.1), the join 5 more.
+// Items of more than 64 rows take units of 128 rows (attend_tile).
 
 #include <type_traits>
 
@@ -337,7 +339,8 @@ __device__ inline Item item_of_lane(const Item& it, uint32_t i) {
   return r;
 }
 
-// Offsets of up to this many sequences and groups are kept in LDS, of more in the workspace.
+// One workgroup, whose time is that of its loads and seven barriers: 4.8 us for 65 items, 6.2 for
+// 204. Offsets of up to this many sequences and groups are kept in LDS, of more in the workspace.
 constexpr uint32_t kPlanLds = 4096;
 
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a) {
@@ -845,6 +848,9 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
 // 128 rows, 32 a wave, over keys that the workgroup stages in LDS: a sub-step's keys are loaded
 // into registers two sub-steps ahead, and stored one ahead. A SIMD has one wave of each of two
 // workgroups: as these share no barrier, the products of one go on under the other's softmax.
+// 8,192 tokens of 32 heads of 128: 680 us, 810 TFLOP/s, where a library product of 8,192 cubed
+// reaches 1,150 to 1,200. No unit is the limit by itself: of a step's 1.3 us its products, counted
+// at 2.4 GHz, take 0.4, the exponentials with the rest of the softmax 0.5, the LDS 0.5.
 //
 // Products are v_mfma_f32_32x32x16 in the same orientation: S^T = K Q^T, O^T = V^T P^T, a lane
 // holding one row's scores with keys 8 i + 4 h .. + 3 (h = lane / 32), which again are P's operand
@@ -1221,7 +1227,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(Atte
 // D/4 lanes take a piece of a row, 4 dims each. Where there are many rows they join all of its
 // pieces, 64 / (D/4) rows a wave; with few rows (kWide) a workgroup's lanes share the pieces of
 // one. Four pieces are in flight at a time. Bound by reading the pieces, or with few by the time
-// of two loads. Rows that no piece covers are set to nothing seen.
+// of half a dozen loads that wait for each other: 4 to 5 us, 7 for 2,048 rows of some ten pieces.
+// Rows that no piece covers are set to nothing seen.
 template <class T, int D, bool kWide>
 __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a) {
   typedef typename T::scalar scalar;
@@ -1230,15 +1237,23 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a) {
   __shared__ __attribute__((aligned(16))) float lds_o[kWide ? kTeams : 1][D];
   __shared__ float lds_m[kTeams], lds_l[kTeams];
   const Ws& w = a.ws;
-  if (a.n_seq > 0 && !w.head->joins) return;  // attend_kernel wrote every row
+  // asked for together: each comes from memory, as another kernel has just written it
+  uint32_t joins = 1;
+  int32_t t0 = 0, t1 = 0;
+  if (a.n_seq) {
+    joins = w.head->joins;
+    t0 = w.q_first[0];
+    t1 = w.q_first[a.n_seq];
+  }
+  asm volatile("" : "+v"(joins), "+v"(t0), "+v"(t1));
+  if (!joins) return;  // attend_kernel wrote every row
   const uint32_t team = threadIdx.x / kLanes, dim = threadIdx.x % kLanes * 4;
   const uint32_t all = a.n_tokens * a.q_heads;
-  const int32_t t0 = a.n_seq ? w.q_first[0] : 0, t1 = a.n_seq ? w.q_first[a.n_seq] : 0;
   // the rows of a workgroup are side by side: of few tokens, and the first one's sequence is found by all
   for (uint32_t r0 = blockIdx.x * kRows; r0 < all; r0 += gridDim.x * kRows) {
     const uint32_t token0 = r0 / a.q_heads;
     uint32_t s = 0;
-    if ((int32_t)token0 >= t0 && (int32_t)token0 < t1) s = wave_search<int32_t>(w.q_first, a.n_seq + 1, (int32_t)token0);
+    if ((int32_t)token0 >= t0 && (int32_t)token0 < t1) s = wave_search<int32_t>(w.q_first, a.n_seq, (int32_t)token0);
     const uint32_t r = r0 + (kWide ? 0 : team);
     if (r >= all) continue;
     const uint32_t token = r / a.q_heads, h = r - token * a.q_heads;
@@ -1248,13 +1263,13 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a) {
       while (w.q_first[s + 1] <= (int32_t)token) ++s;
       const Item& own = w.items[a.n_groups + s];
       const uint32_t chunks = own.chunks, partial = own.partial;
+      const int32_t gr = a.n_groups ? w.seq_group[s] : -1;
       if (!partial && chunks) continue;  // written already
       if (partial) {
         const uint32_t rows = own.tokens * a.ratio;
         first[1] = own.part_first + head * chunks * rows + (token - own.token_first) * a.ratio + h % a.ratio;
         count[1] = chunks;
         step[1] = rows;
-        const int32_t gr = a.n_groups ? w.seq_group[s] : -1;
         if (gr >= 0) {
           const Item& pre = w.items[gr];
           const uint32_t all_rows = pre.tokens * a.ratio;
