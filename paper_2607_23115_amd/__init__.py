@@ -876,6 +876,12 @@ def _heads(t: torch.Tensor, name: str, dtype: torch.dtype, dev: int, d: int):
     raise ValueError(f"{name} must have its last dimension contiguous")
 
 
+def _empty_heads(t: torch.Tensor) -> torch.Tensor:
+    """A contiguous tensor like t (what a call makes itself needs no checks; empty_like is the
+    quickest way to one: 1.3 us, torch.empty 1.8)."""
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+
+
 def _kv_struct(k_pages: torch.Tensor, v_pages: torch.Tensor) -> _KvPages:
     for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
         if not isinstance(t, torch.Tensor) or t.get_device() < 0:
@@ -958,10 +964,12 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: 
         out_at = None
         if q is not None:
             if q_out is None:
-                q_out = torch.empty((n, q_heads, d), dtype=dtype, device=q.device)
-            out_at = _flat(q_out, "q_out", dtype, dev)
-            if q_out.shape != q.shape:
-                raise ValueError("q_out and q differ in shape")
+                q_out = _empty_heads(q)
+                out_at = q_out.data_ptr()
+            else:
+                out_at = _flat(q_out, "q_out", dtype, dev)
+                if q_out.shape != q.shape:
+                    raise ValueError("q_out and q differ in shape")
             if q_at is None:
                 out_at = None
         args = _Append(q_at, k_at, v_at, out_at, slots_at, positions_at, table_at, qw_at, kw_at, n, table, q_token,
@@ -1008,19 +1016,27 @@ def prefix_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
     device = k_pages.device
     with _on_stream(stream, device) as hs:
         if out is None:
-            out = torch.empty((tokens, heads, d), dtype=dtype, device=device)
-        out_at = _flat(out, "out", dtype, dev)
-        if out.shape != q.shape:
-            raise ValueError("out and q differ in shape")
-        if lse is None and want_lse:
-            lse = torch.empty((tokens, heads), dtype=torch.float32, device=device)
-        lse_at = _flat(lse, "lse", torch.float32, dev, optional=True)
-        if lse is not None and lse.shape != q.shape[:2]:
-            raise ValueError("lse must be [tokens, q_heads]")
+            out = _empty_heads(q)
+            out_at = out.data_ptr()
+        else:
+            out_at = _flat(out, "out", dtype, dev)
+            if out.shape != q.shape:
+                raise ValueError("out and q differ in shape")
+        lse_at = None
+        if lse is not None:
+            lse_at = _flat(lse, "lse", torch.float32, dev)
+            if lse.shape != q.shape[:2]:
+                raise ValueError("lse must be [tokens, q_heads]")
+        elif want_lse:
+            lse = q.new_empty((tokens, heads), dtype=torch.float32)
+            lse_at = lse.data_ptr()
         if ws is None:
-            ws = torch.empty(_attention_ws(kv, b), dtype=torch.uint8, device=device)
-        ws_at = _flat(ws, "ws", torch.uint8, dev)
-        _check(lib.gleam_prefix_attention(kv, b, out_at, lse_at, ws_at, ws.numel(), hs))
+            ws_bytes = _attention_ws(kv, b)
+            ws = q.new_empty(ws_bytes, dtype=torch.uint8)
+            ws_at = ws.data_ptr()
+        else:
+            ws_at, ws_bytes = _flat(ws, "ws", torch.uint8, dev), ws.numel()
+        _check(lib.gleam_prefix_attention(kv, b, out_at, lse_at, ws_at, ws_bytes, hs))
     return out, lse
 
 
