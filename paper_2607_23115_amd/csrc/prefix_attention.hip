@@ -625,6 +625,9 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
   const uint32_t begin = 2 * chunk * it.per + wave;
   auto keys_of = [&](uint32_t half) { return half < prefix_halves ? it.prefix_keys : it.own_keys; };
   auto key_of = [&](uint32_t half) { return 32 * (half < prefix_halves ? half : half - prefix_halves); };
+  // whose infinite and NaN values are taken out and added at the end: a half with an own key that some
+  // row of the tile must not see (keys that do not exist are no reason, their values are set to 0)
+  auto looked_at = [&](uint32_t half) { return half >= prefix_halves && key_of(half) + 32 > own_least; };
 
   // Pages ahead: lane 2 i has that of the first 16 keys of the wave's i-th half from page_half on,
   // lane 2 i + 1 that of the others. A half's keys wait for no look-up of their own.
@@ -744,7 +747,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
         for (int c = 0; c < kWords; ++c)
           if (4 * g + (e & 3) >= exist[set][e >> 2]) vv[set][e][c] = 0;
     }
-    if (!shared && masked) {
+    if (looked_at(half)) {
       uint32_t any = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e)
@@ -779,8 +782,8 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
   }
   if (special) {  // the same halves again: those that were looked at
     for (uint32_t half = begin; half < end; half += kWaves) {
-      const uint32_t key = 32 * (half - prefix_halves);
-      if (half < prefix_halves || key + 32 <= own_least) continue;
+      if (!looked_at(half)) continue;
+      const uint32_t key = key_of(half);
       for (uint32_t i = 0; i < 32; ++i) {
         const uint32_t first = key + (i & 16);
         const Keys16 t = keys16(a, page_at(a, own_pages, first, it.own_keys), first, it.own_keys, head);

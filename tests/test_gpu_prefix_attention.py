@@ -340,3 +340,18 @@ def test_refusals():
     refused("out and q differ", out=lambda a: a["q"][:1].clone())
     refused("lse must be", lse=lambda a: torch.empty(2, 3, device="cuda"))
     refused("contiguous", out=lambda a: a["q"].transpose(0, 1).contiguous().transpose(0, 1))
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("n", [1, 5, 16, 32, 40])
+def test_infinities_beside_a_page_that_is_missing(n, dtype):
+    """Of 32 keys that are looked up together one page of 16 is missing; what the other one holds
+    reaches the rows that see it, infinities and NaN included."""
+    c = Case([n], [140], [], 4, 2, 64, 16, dtype, seed=n)
+    pages = c.own_pages[0].clone()
+    c.vp[pages[3], 2, 0, 3] = math.inf     # key 50, behind a missing page
+    c.vp[pages[3], 12, 1, 9] = math.nan
+    c.vp[pages[4], 0, 1, 20] = -math.inf   # key 64, before one
+    c.vp[pages[8], 11, 0, 33] = math.inf   # the last key
+    c.own_pages[0, 2], c.own_pages[0, 5] = -1, c.kp.shape[0]
+    c.check()
