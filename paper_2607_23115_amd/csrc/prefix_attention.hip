@@ -941,8 +941,8 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
 
   // Scores are scaled after the product, and masked ones are minus infinity before it: a scale below
   // zero is taken from the queries' signs, so that the largest score is the largest product's, and
-  // one of zero is taken as queries of zero.
-  const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u, keep = a.scale_log2 == 0.f ? 0u : ~0u;
+  // one of zero is taken as queries of zero, NaN where the query is infinite or NaN.
+  const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;
   const float scale = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);
   Pack8 q[kQ];
 #pragma unroll
@@ -951,7 +951,11 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
     if (row_live)
       q[i].u = *reinterpret_cast<const u32x4v*>(a.q + (int64_t)token * a.q_token + (int64_t)q_head * a.q_head +
                                                 (i * 16 + h * 8) * 2);
-    q[i].u = (q[i].u ^ flip) & keep;
+    q[i].u ^= flip;
+    if (a.scale_log2 == 0.f) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) q[i].u[c] = (special_bits<T>(q[i].u[c]) >> 15) * 0x7fffu;
+    }
   }
 
   const int32_t* const prefix_pages = a.prefix_pages + (uint64_t)it.prefix_row * a.prefix_width;

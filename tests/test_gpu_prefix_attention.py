@@ -355,3 +355,12 @@ def test_infinities_beside_a_page_that_is_missing(n, dtype):
     c.vp[pages[8], 11, 0, 33] = math.inf   # the last key
     c.own_pages[0, 2], c.own_pages[0, 5] = -1, c.kp.shape[0]
     c.check()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("n", [1, 100])
+def test_a_scale_of_zero_keeps_queries_that_are_not_finite(n, dtype):
+    c = Case([n, 2], [130, 3], [(0, 2, 40)], 4, 2, 64, 16, dtype)
+    c.q[0, 1, 5], c.q[n // 2, 2, 63] = math.nan, math.inf
+    c.scale = 0.0
+    c.check()
