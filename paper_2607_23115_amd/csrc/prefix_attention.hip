@@ -942,7 +942,6 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
   // Scores are scaled after the product, and masked ones are minus infinity before it: a scale below
   // zero is taken from the queries' signs, so that the largest score is the largest product's, and
   // one of zero is taken as queries of zero, NaN where the query is infinite or NaN.
-  const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;
   const float scale = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);
   Pack8 q[kQ];
 #pragma unroll
@@ -951,11 +950,6 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
     if (row_live)
       q[i].u = *reinterpret_cast<const u32x4v*>(a.q + (int64_t)token * a.q_token + (int64_t)q_head * a.q_head +
                                                 (i * 16 + h * 8) * 2);
-    q[i].u ^= flip;
-    if (a.scale_log2 == 0.f) {
-#pragma unroll
-      for (int c = 0; c < 4; ++c) q[i].u[c] = (special_bits<T>(q[i].u[c]) >> 15) * 0x7fffu;
-    }
   }
 
   const int32_t* const prefix_pages = a.prefix_pages + (uint64_t)it.prefix_row * a.prefix_width;
@@ -1053,6 +1047,16 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
     stage_tidy(first);
     stage_store(first);
     if (first + 1 < end) stage_load(first + 1);
+  }
+  // the queries as the scale wants them: here, where they have arrived
+  const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+  for (int i = 0; i < kQ; ++i) q[i].u ^= flip;
+  if (a.scale_log2 == 0.f) {
+#pragma unroll
+    for (int i = 0; i < kQ; ++i)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) q[i].u[c] = (special_bits<T>(q[i].u[c]) >> 15) * 0x7fffu;
   }
   // One barrier a sub-step: what it stores one ahead is complete at the next one's, and goes to the
   // buffer that all waves were done with at its own.
