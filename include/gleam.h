@@ -687,8 +687,10 @@ gleam_status gleam_kv_append(const gleam_kv_pages* kv, const gleam_append* a, vo
  * each token and query head (q_heads / kv_heads of them share a key head, in order):
  *   score = scale * q.k,  out = sum exp(score) v / sum exp(score),  lse = log sum exp(score)
  * Scores, maxima, sums and outputs are kept in 32 bits, exp(score - max) is rounded to dtype
- * for its product with v, and the output once more. A row that sees nothing gets out = 0 and
- * lse = -infinity. What a row may not see does not reach it, whatever it holds (NaN too).
+ * for its product with v (the matrix units take no wider one; in fp16 what is below 2^-32 is 0,
+ * so that an infinite value behind it gives NaN), and the output once more. A row that sees
+ * nothing gets out = 0 and lse = -infinity. What a row may not see does not reach it, whatever it
+ * holds (NaN too).
  *
  * Everything with a d_ is device memory and is read when the kernels run, so a captured call
  * follows changed lengths and pages. Lengths are taken as at least 0 and at most what the

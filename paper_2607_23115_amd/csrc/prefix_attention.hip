@@ -40,6 +40,11 @@ namespace {
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kPlanThreads = 1024;
 constexpr float kRise = 8.f;  // log2
+// The exponentials' reference is 2^up below the score that it follows: 16 bits of fp16 hold them from
+// 2^-25 on, and without it the many small ones of a long history would be in a row's sum, but not in its
+// output (a key and 65,536 others 2^25 below it: 0.2% of the output). They go up to 2^15 that way. bf16
+// reaches down to 2^-133, and its values so far up that their sums need the room.
+template <class T> constexpr float kUp = std::is_same_v<T, Fp16> ? 7.f : 0.f;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr uint64_t kMostSeq = 1ull << 20;
 constexpr uint64_t kPassing = 128ull << 20;  // bytes of an item's keys and values
@@ -558,6 +563,28 @@ __device__ inline float sum_halves(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// A sum that small terms are added to for long: `lost` gathers what each addition rounds off.
+struct Sum {
+  float sum = 0.f, lost = 0.f;
+  __device__ void add(float x) {
+    const float t = sum + x;
+    lost += x - (t - sum);
+    sum = t;
+  }
+  __device__ void scale(float f) {
+    sum *= f;
+    lost *= f;
+  }
+  __device__ float value() const { return sum + lost; }
+};
+
+// The sum of kN values, in pairs.
+template <int kN>
+__device__ inline float sum_of(const float* x) {
+  if constexpr (kN == 1) return x[0];
+  else return sum_of<kN / 2>(x) + sum_of<kN / 2>(x + kN / 2);
+}
+
 // A unit, as its workgroup finds it.
 struct Unit {
   Item it;
@@ -617,7 +644,8 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
   if (end > all_halves) end = all_halves;
 
   bool special = false;
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY;
+  Sum l_sum;
   f32x4 o[kDims];
 #pragma unroll
   for (int j = 0; j < kDims; ++j) o[j] = (f32x4)0.f;
@@ -722,13 +750,13 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
       top = fmaxf(top, x[e]);
     }
     top = max_halves(max_rows(top));
-    // m need not be the maximum itself: it follows once some score is kRise above it (of 2^kRise
-    // no 32-bit sum takes harm), which spares most steps the rescaling
-    if (__any(top > m + kRise || (m == -INFINITY && top > m))) {
-      const float m_new = fmaxf(m, top);
+    // m need not follow the maximum at once: it does when some score is kRise above its last one (of
+    // 2^kRise no 32-bit sum takes harm), which spares most steps the rescaling
+    if (__any(top > m + (kUp<T> + kRise) || (m == -INFINITY && top > m))) {
+      const float m_new = fmaxf(m, top - kUp<T>);
       const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
       m = m_new;
-      l *= alpha;
+      l_sum.scale(alpha);
 #pragma unroll
       for (int j = 0; j < kDims; ++j) o[j] *= alpha;
     }
@@ -736,10 +764,10 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
     Pack8 p;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float y = __builtin_amdgcn_exp2f(x[e] - m_use);
-      l += y;
-      put(p, e, y, T());
+      x[e] = __builtin_amdgcn_exp2f(x[e] - m_use);
+      put(p, e, x[e], T());
     }
+    l_sum.add(sum_of<8>(x));
     if (exist[set][0] + exist[set][1] < 32) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
@@ -797,6 +825,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
   }
 
   // the four waves' results, joined through LDS
+  float l = l_sum.value();
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
   if (g == 0) {
@@ -1032,7 +1061,8 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
   };
 
   bool special = false;
-  float m = -INFINITY, l = 0.f;  // m: of the products, not yet scaled
+  float m = -INFINITY;  // of the products, not yet scaled, without kUp
+  Sum l_sum;
   f32x16 o[kO];
 #pragma unroll
   for (int i = 0; i < kO; ++i) o[i] = (f32x16)0.f;
@@ -1105,26 +1135,27 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
 #pragma unroll
         for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
       top = max_halves(top);
-      // m need not be the maximum itself: it follows once some score is kRise above it (of 2^kRise
-      // no 32-bit sum takes harm), which spares most steps the rescaling
+      // m need not be the maximum itself: it follows once some score is kRise above it (as above)
       if (__any((top - m) * scale > kRise || (m == -INFINITY && top > m))) {
         const float m_new = fmaxf(m, top);
         const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - m_new) * scale);
         m = m_new;
-        l *= alpha;
+        l_sum.scale(alpha);
 #pragma unroll
         for (int i = 0; i < kO; ++i) o[i] *= alpha;
       }
-      const float bias = m == -INFINITY ? 0.f : -m * scale;  // nothing seen so far: all exponentials are 0
+      const float bias = m == -INFINITY ? 0.f : kUp<T> - m * scale;  // nothing seen so far: all exponentials are 0
       Pack8 p[kKTiles * 2];
+      float step = 0.f;
 #pragma unroll
       for (int t = 0; t < kKTiles; ++t)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const float y = __builtin_amdgcn_exp2f(fmaf(s[t][r], scale, bias));
-          l += y;
+          step += y;
           put(p[2 * t + r / 8], r % 8, y, T());
         }
+      l_sum.add(step);
 #pragma unroll
       for (int kk = 0; kk < 2 * kKTiles; ++kk)
 #pragma unroll
@@ -1138,7 +1169,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
     }
   }
 
-  l = sum_halves(l);
+  const float l = sum_halves(l_sum.value());
   if (!row_live) return;
   if (special) {
     uint32_t key = own_group_least & ~(St::kKeys - 1u);  // the first sub-step that was looked at
@@ -1155,7 +1186,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
           add_special<T, 4>(v + (32 * i + 2 * r) * 2, [&](int c, float x) { o[i][r + c] += x; });
     }
   }
-  const float top = m == -INFINITY ? -INFINITY : m * scale;
+  const float top = m == -INFINITY ? -INFINITY : m * scale - kUp<T>;
   if (it.partial) {
     const uint64_t at_row = it.part_first + ((uint64_t)head * it.chunks + unit.chunk) * rows + row;
     float* const to = a.ws.part_o + at_row * D + 4 * h;

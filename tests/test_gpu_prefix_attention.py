@@ -364,3 +364,30 @@ def test_a_scale_of_zero_keeps_queries_that_are_not_finite(n, dtype):
     c.q[0, 1, 5], c.q[n // 2, 2, 63] = math.nan, math.inf
     c.scale = 0.0
     c.check()
+
+
+@pytest.mark.parametrize("n", [1, 40, 70])
+def test_many_small_weights_of_fp16(n):
+    """Each wave meets keys that outweigh every other one by 2^25.2, and tens of thousands of those,
+    whose exponentials relative to the largest score are below what fp16 holds. The bound: a rounding
+    of the output and one of the large exponentials, 2^-11 each; the small ones' half spacing, 2^-32 of
+    the sum's largest term, of which there are four; 2^-16 for 32-bit arithmetic."""
+    heads, d, page, keys = 256, 64, 4096, 1 << 18
+    lead, rest = 17.5, math.exp(-17.5)
+    k = torch.zeros(2, page, heads, d, dtype=F16)
+    v = torch.ones(2, page, heads, d, dtype=F16)
+    k[0, 0:128:32, :, 0], v[0, 0:128:32] = lead, -1.0
+    table = torch.ones(1, keys // page, dtype=torch.int32)
+    table[0, 0] = 0
+    q = torch.zeros(n, heads, d, dtype=F16)
+    q[:, :, 0] = 1.0
+    say("prefix_attention small weights", n)
+    out, lse = g.prefix_attention(q.cuda(), k.cuda(), v.cuda(), i32([0, n]).cuda(), table.cuda(), i32([keys]).cuda(),
+                                  scale=1.0, want_lse=True)
+    torch.cuda.synchronize()
+    seen = torch.arange(keys - n + 1, keys + 1, dtype=torch.float64)
+    total = 4 + (seen - 4) * rest
+    want = ((seen - 4) * rest - 4) / total
+    off = float((out.cpu().double() - want[:, None, None]).abs().max())
+    assert off <= 2.0 ** -10 + keys / 4 * 2.0 ** -32 + 2.0 ** -16
+    assert float((lse.cpu().double() - lead - total.log()[:, None]).abs().max()) <= 2.0 ** -18 * 40
