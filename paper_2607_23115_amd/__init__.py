@@ -876,6 +876,22 @@ def _heads(t: torch.Tensor, name: str, dtype: torch.dtype, dev: int, d: int):
     raise ValueError(f"{name} must have its last dimension contiguous")
 
 
+# Forward mode's level, -1 outside it. Not part of torch's public interface: without it every call
+# asks its tensors.
+_forward = torch.autograd.forward_ad if hasattr(torch.autograd.forward_ad, "_current_level") else None
+
+
+def _no_gradient(call: str, **tensors: torch.Tensor | None) -> None:
+    """These calls have no gradient: where torch would record one, or carries a tangent along, the
+    result would silently lack it. (The callers ask for requires_grad and the level themselves,
+    0.2 us; a call of this takes 0.6.)"""
+    for name, t in tensors.items():
+        if t is not None and (t.requires_grad and torch.is_grad_enabled() or
+                              torch.autograd.forward_ad.unpack_dual(t).tangent is not None):
+            raise ValueError(f"{name} requires a gradient, {call} has none: call it under torch.no_grad(), or with "
+                             f"detached tensors")
+
+
 def _empty_heads(t: torch.Tensor) -> torch.Tensor:
     """A contiguous tensor like t (what a call makes itself needs no checks; empty_like is the
     quickest way to one: 1.3 us, torch.empty 1.8)."""
@@ -932,7 +948,8 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: 
     one product's output, say). k_pages, v_pages: [pages, page_tokens, kv_heads, head_dim], any
     order in memory of the first three. slots int64: page * page_tokens + place of each token,
     -1 to store nothing. rotary: rotary_table()'s, with positions int32. q_weight, k_weight
-    [head_dim]: norm each head of q, of k."""
+    [head_dim]: norm each head of q, of k. There is no gradient: tensors that require one are
+    refused while torch records them."""
     kv = _kv_struct(k_pages, v_pages)
     dtype, dev, d = k_pages.dtype, k_pages.get_device(), kv.head_dim
     k_at, n, heads, k_token, k_head = _heads(k, "k", dtype, dev, d)
@@ -972,6 +989,12 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: 
                     raise ValueError("q_out and q differ in shape")
             if q_at is None:
                 out_at = None
+        if (k.requires_grad or v.requires_grad or k_pages.requires_grad or v_pages.requires_grad
+                or q is not None and (q.requires_grad or q_out.requires_grad)
+                or rotary is not None and rotary.requires_grad or q_weight is not None and q_weight.requires_grad
+                or k_weight is not None and k_weight.requires_grad or not _forward or _forward._current_level >= 0):
+            _no_gradient("kv_append", k=k, v=v, k_pages=k_pages, v_pages=v_pages, q=q, q_out=q_out, rotary=rotary,
+                         q_weight=q_weight, k_weight=k_weight)
         args = _Append(q_at, k_at, v_at, out_at, slots_at, positions_at, table_at, qw_at, kw_at, n, table, q_token,
                        q_head, k_token, k_head, v_token, v_head, q_heads, rot, 1 if interleaved else 0, eps)
         _check(lib.gleam_kv_append(kv, args, hs))
@@ -991,7 +1014,8 @@ def prefix_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
     group_first[g] to group_first[g + 1] also see all prefix_len[g] keys in prefix_pages[g],
     which are read once for the group. All of these are int32 on the GPU, unused places of the
     page tables -1. scale: head_dim ** -0.5 where none is given. ws: a workspace from
-    prefix_attention_workspace() of these shapes."""
+    prefix_attention_workspace() of these shapes. There is no gradient: tensors that require one
+    are refused while torch records them."""
     kv = _kv_struct(k_pages, v_pages)
     dtype, dev, d = k_pages.dtype, k_pages.get_device(), kv.head_dim
     q_at, tokens, heads, q_token, q_head = _heads(q, "q", dtype, dev, d)
@@ -1036,6 +1060,9 @@ def prefix_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
             ws_at = ws.data_ptr()
         else:
             ws_at, ws_bytes = _flat(ws, "ws", torch.uint8, dev), ws.numel()
+        if (q.requires_grad or k_pages.requires_grad or v_pages.requires_grad or out.requires_grad
+                or lse is not None and lse.requires_grad or not _forward or _forward._current_level >= 0):
+            _no_gradient("prefix_attention", q=q, k_pages=k_pages, v_pages=v_pages, out=out, lse=lse)
         _check(lib.gleam_prefix_attention(kv, b, out_at, lse_at, ws_at, ws_bytes, hs))
     return out, lse
 

@@ -237,3 +237,27 @@ def test_refusals():
                 {"rot_dim": 64, "factor": math.nan}, {"rot_dim": 64, "slow": 2.0, "fast": 2.0}):
         with pytest.raises(g.GleamError):
             g.rotary_table(8, **bad)
+
+
+def test_gradients_are_refused_and_not_dropped():
+    f = torch.float16
+    a = {"k": torch.zeros(4, 2, 64), "v": torch.zeros(4, 2, 64), "q": torch.zeros(4, 2, 64),
+         "k_pages": torch.zeros(3, 16, 2, 64), "v_pages": torch.zeros(3, 16, 2, 64), "q_weight": torch.ones(64),
+         "k_weight": torch.ones(64)}
+    a = {n: t.to(f).cuda() for n, t in a.items()}
+    a.update(slots=torch.arange(4, device="cuda"), positions=torch.arange(4, dtype=torch.int32, device="cuda"),
+             rotary=g.rotary_table(4, 64))
+    say("kv_append gradients")
+    for name in ("k", "v", "q", "k_pages", "v_pages", "q_weight", "k_weight", "rotary"):
+        b = {**a, name: a[name].clone().requires_grad_()}
+        with pytest.raises(ValueError, match=name + " requires a gradient"):
+            g.kv_append(**b)
+        with torch.no_grad():
+            assert not g.kv_append(**b).requires_grad
+        with torch.autograd.forward_ad.dual_level():
+            b[name] = torch.autograd.forward_ad.make_dual(a[name], torch.ones_like(a[name]))
+            with pytest.raises(ValueError, match=name + " requires a gradient"):
+                g.kv_append(**b)
+    refused("q_out requires a gradient", q=lambda a: a["k"], q_out=lambda a: a["k"].clone().requires_grad_())
+    with torch.inference_mode():
+        g.kv_append(**a)

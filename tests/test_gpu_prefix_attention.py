@@ -391,3 +391,20 @@ def test_many_small_weights_of_fp16(n):
     off = float((out.cpu().double() - want[:, None, None]).abs().max())
     assert off <= 2.0 ** -10 + keys / 4 * 2.0 ** -32 + 2.0 ** -16
     assert float((lse.cpu().double() - lead - total.log()[:, None]).abs().max()) <= 2.0 ** -18 * 40
+
+
+def test_gradients_are_refused_and_not_dropped():
+    c = Case([1, 1], [5, 6], [(0, 2, 7)], 4, 2, 64, 16, F16)
+    a = {**c.arguments(), "out": torch.zeros(2, 4, 64, dtype=F16, device="cuda"),
+         "lse": torch.zeros(2, 4, device="cuda")}
+    say("prefix_attention gradients")
+    for name in ("q", "k_pages", "v_pages", "out", "lse"):
+        b = {**a, name: a[name].clone().requires_grad_()}
+        with pytest.raises(ValueError, match=name + " requires a gradient"):
+            g.prefix_attention(**b)
+        with torch.no_grad():
+            g.prefix_attention(**b)
+    with torch.autograd.forward_ad.dual_level():
+        b = {**a, "q": torch.autograd.forward_ad.make_dual(a["q"], torch.ones_like(a["q"]))}
+        with pytest.raises(ValueError, match="q requires a gradient"):
+            g.prefix_attention(**b)
