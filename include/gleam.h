@@ -648,7 +648,9 @@ gleam_status gleam_rotary_table(float* d_table, uint64_t positions, uint32_t rot
  *                                                table's for d_positions[t]
  * d_slots[t] = page * page_tokens + place is where the token's keys and values go; a slot that
  * is not in the cache (-1 for padding) stores nothing, its query is rotated all the same. Two
- * tokens with one slot leave either's keys. A position outside the table gives NaN.
+ * tokens with one slot leave a mixture of both. A position outside the table gives NaN. The
+ * cache's places must not overlap: by size, each stride (of a dimension of more than one) is at
+ * least what the smaller ones span.
  *   q, k, v          device, token and head strides in elements (multiples of 8), 16-byte aligned
  *   d_q, d_q_out     nullable together; d_q_out is [n_tokens][q_heads][head_dim] and may be d_q
  *                    itself where that is contiguous

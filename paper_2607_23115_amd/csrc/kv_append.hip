@@ -13,6 +13,8 @@
 // and sines once. 16,384 tokens of 32 and 8 heads of 128: 83 us, 4.9 TB/s (a copy of as many bytes
 // 78 us); one token 2.8 us.
 
+#include <algorithm>
+
 #include "kv_pages.h"
 #include "launch_shape.h"
 
@@ -74,6 +76,24 @@ gleam_status validate_kv(const gleam_kv_pages* kv, const char* who) {
 }
 
 namespace {
+
+// Whether no element belongs to two places: each stride is at least what the smaller ones span.
+// (Places that interleave without meeting, of strides that none of the usual orders has, are not
+// told from those that overlap.)
+bool places_apart(const gleam_kv_pages& kv, const int64_t stride[3]) {
+  struct Dim {
+    int64_t stride;
+    uint64_t count;
+  } dim[3] = {{stride[0], kv.n_pages}, {stride[1], kv.page_tokens}, {stride[2], kv.kv_heads}};
+  std::sort(dim, dim + 3, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
+  unsigned __int128 span = kv.head_dim;
+  for (const Dim& d : dim) {
+    if (d.count < 2) continue;
+    if ((uint64_t)d.stride < span) return false;
+    span += (unsigned __int128)d.stride * (d.count - 1);
+  }
+  return true;
+}
 
 constexpr int kAppendThreads = 256, kAppendWaves = kAppendThreads / 64;
 
@@ -311,8 +331,7 @@ extern "C" gleam_status gleam_kv_append(const gleam_kv_pages* kv, const gleam_ap
   // a place that two heads or two tokens share would take whichever is stored last
   const int64_t* const strides[2] = {kv->k_stride, kv->v_stride};
   for (const int64_t* s : strides) {
-    if ((kv->n_pages > 1 && s[0] < (int64_t)kv->head_dim) || s[1] < (int64_t)kv->head_dim ||
-        (kv->kv_heads > 1 && s[2] < (int64_t)kv->head_dim)) {
+    if (!places_apart(*kv, s)) {
       set_error("%s: pages, places and heads of the cache overlap", who);
       return GLEAM_E_INVALID;
     }

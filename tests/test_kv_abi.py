@@ -141,3 +141,24 @@ def test_the_binding_refuses_host_tensors():
         g.prefix_attention(x[0, :4], x, x, None, None, None)
     with pytest.raises(ValueError, match="CUDA device"):
         g.rotary_table(4, 64, device="cpu")
+
+
+def test_appends_into_places_that_overlap_by_their_strides_together_are_refused():
+    # each stride holds a head by itself
+    for bad in ((2048, 64, 64),       # head 1 of a place is head 0 of the next
+                (2048, 64, 512),      # head 1 starts within head 0's places
+                (1024, 128, 64),      # a page's second half is the next page
+                (64, 128, 64), (1984, 128, 64), (128, 256, 64)):
+        assert append(kv(k_stride=bad)) == g.E_INVALID, bad
+        assert append(kv(v_stride=bad)) == g.E_INVALID, bad
+        assert b"overlap" in g.lib.gleam_last_error()
+
+
+@pytest.mark.parametrize("good", [(2048, 128, 64), (2048, 64, 1024), (4096, 256, 64), (64, 512, 256), (128, 512, 64),
+                                  (1 << 40, 1 << 20, 64), ((1 << 62) - 8, 128, 64)])
+def test_orders_of_pages_places_and_heads_that_do_not_overlap_are_taken(good):
+    # what the next check refuses, so that nothing is launched
+    assert append(kv(k_stride=good, v_stride=good), n_tokens=1 << 31) == g.E_UNSUPPORTED
+    # strides of dimensions of one multiply nothing
+    one = put(kv(k_stride=(0, 64, 0), v_stride=(8, 64, 8)), n_pages=1, kv_heads=1)
+    assert append(one, n_tokens=1 << 31) == g.E_UNSUPPORTED
