@@ -975,6 +975,9 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: 
         if rotary.dim() != 2:
             raise ValueError("rotary must be [positions, rot_dim]")
         table, rot = rotary.shape
+        # a table without positions has no address, and every position is outside it: none of it is
+        # read, but the call would take a null table as no rotation
+        table_at = table_at or k_at
     qw_at = _flat(q_weight, "q_weight", dtype, dev, d, optional=True)
     kw_at = _flat(k_weight, "k_weight", dtype, dev, d, optional=True)
     with _on_stream(stream, k_pages.device) as hs:

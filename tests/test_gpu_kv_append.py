@@ -261,3 +261,16 @@ def test_gradients_are_refused_and_not_dropped():
     refused("q_out requires a gradient", q=lambda a: a["k"], q_out=lambda a: a["k"].clone().requires_grad_())
     with torch.inference_mode():
         g.kv_append(**a)
+
+
+def test_a_table_without_positions_gives_nan():
+    say("kv_append empty table")
+    k = torch.ones(3, 2, 64, dtype=torch.float16, device="cuda")
+    kp, vp = (torch.zeros(1, 16, 2, 64, dtype=torch.float16, device="cuda") for _ in range(2))
+    positions = torch.tensor([0, 5, -1], dtype=torch.int32, device="cuda")
+    got = g.kv_append(k, k, kp, vp, torch.arange(3, device="cuda"), q=k, positions=positions,
+                      rotary=g.rotary_table(0, 32))
+    for x in (got, kp[0, :3]):
+        assert torch.isnan(x[..., :32]).all() and (x[..., 32:] == 1).all()
+    refused("rot_dim", rotary=lambda a: g.rotary_table(0, 24), positions=lambda a: a["slots"].int())
+    refused("rot_dim", rotary=lambda a: torch.empty(0, 0, device="cuda"), positions=lambda a: a["slots"].int())
