@@ -755,10 +755,12 @@ def transfer_path(args, g, torch, threads):
 def serve_path(args, g, torch):
     """One attention layer of a serving loop on the paged key/value cache: 64 users of the 7B
     decoder (32 heads of 128, fp16) behind one system prompt of 2,048 tokens. The prompts are
-    identified in blocks of 1,024 tokens (gleam_detect): a held block's value is the first of its
-    pages. The users' own prompt tokens go in by one kv_append and are answered by one
-    prefix_attention; a timed step is the next token of every user through both calls.
-    Queries, keys and values are synthetic N(0, 1)."""
+    identified in blocks of 1,024 tokens, each with all that comes before it (gleam_detect of their
+    digests' lists): a held block's value is the first of its pages. Another prompt that was served
+    holds the system prompt's second block behind another first one, in other pages. The users' own
+    prompt tokens go in by one kv_append and are answered by one prefix_attention; a timed step is
+    the next token of every user through both calls. Queries, keys and values are synthetic
+    N(0, 1)."""
     users, system, block, page, heads, d = 64, 2048, 1024, 64, 32, 128
     K, total, dt = args.steps, args.warmup + args.steps, torch.float16
     rng = np.random.default_rng(2607)
@@ -773,6 +775,10 @@ def serve_path(args, g, torch):
         return g.Batch.from_arena(torch.from_numpy(np.concatenate(rows).view(np.uint8)).to("cuda"), offs, lens,
                                   4 * block)
 
+    def beginnings(rows):
+        b = batch_of(rows)
+        return g.Batch.prefixes(b, g.fp_chunks(b))
+
     def dev(x, dtype=torch.int32):
         return torch.from_numpy(np.ascontiguousarray(x)).to("cuda", dtype)
 
@@ -782,17 +788,22 @@ def serve_path(args, g, torch):
 
     shared = system // page
     each = [-(-(int(n) + total) // page) for n in own]
-    pool = [torch.zeros(shared + sum(each), heads, page, d, dtype=dt, device="cuda").transpose(1, 2) for _ in range(2)]
+    pool = [torch.zeros(2 * shared + sum(each), heads, page, d, dtype=dt, device="cuda").transpose(1, 2)
+            for _ in range(2)]
     rotary = g.rotary_table(system + 300 + total, d)
-    # the system prompt was served before: its keys and values lie in the first pages
-    q, k, v = product(system)
-    g.kv_append(k, v, *pool, torch.arange(system, device="cuda"), positions=dev(np.arange(system)), rotary=rotary)
+    # the system prompt was served before: its keys and values lie in the first pages. The other one's
+    # lie in the last: it starts differently, and goes on with the system prompt's second block.
     table = g.Cache(1 << 10)
-    table.insert(g.fp_chunks(batch_of(prompts[:1])), dev(np.arange(0, shared, block // page), torch.int64))
+    other = np.concatenate([rng.integers(0, 32000, block, dtype=np.int32), prompts[0][block:]])
+    for prompt, first_page in ((other, shared + sum(each)), (prompts[0], 0)):
+        q, k, v = product(system)
+        g.kv_append(k, v, *pool, torch.arange(system, device="cuda") + first_page * page,
+                    positions=dev(np.arange(system)), rotary=rotary)
+        table.insert(g.fp_chunks(beginnings([prompt])),
+                     dev(first_page + np.arange(0, shared, block // page), torch.int64))
 
     # the users' prompts: leading blocks that are held need no work
-    prompt_batch = batch_of(prompts[1:])
-    found = g.detect(prompt_batch, table)
+    found = g.detect(beginnings(prompts[1:]), table)
     status, ref = found.status.cpu().numpy(), g.as_u64(found.ref)
     first = np.concatenate([[0], np.cumsum([-(-p.size // block) for p in prompts[1:]])])
     for i in range(users):

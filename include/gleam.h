@@ -599,9 +599,15 @@ gleam_status gleam_remap_export(const gleam_remap* m, uint64_t* d_start, uint64_
                                 uint64_t* d_count, void* stream);
 
 /*
- * A paged key/value cache. Identifiers of blocks of prompt tokens (gleam_cache_lookup, whose
- * values may be page numbers) say which pages already hold a prompt's keys and values; the
- * calls below fill such pages and read them. They are for serving: nothing here has a gradient.
+ * A paged key/value cache. Identifiers of prompts' beginnings (gleam_cache_lookup, whose values
+ * may be page numbers) say which pages already hold a prompt's keys and values; the calls below
+ * fill such pages and read them. They are for serving: nothing here has a gradient.
+ *
+ * Keys and values depend on every token before their own, a block's digest on that block's bytes
+ * alone: the same block behind another one has other keys and values. What identifies a block's
+ * pages is the digest of its prompt's list of block digests up to and with its own:
+ * gleam_fp_chunks of the prompts, then of a batch whose payloads are those lists, u64[j + 1] from
+ * &d_block_digest[blk_first[s]] on for block j of prompt s.
  *
  * Keys and values live in n_pages pages of page_tokens places each. Place i of page p holds
  * head_dim elements of head h at element offset p * stride[0] + i * stride[1] + h * stride[2]

@@ -284,6 +284,15 @@ def geometry(seg_len, block_bytes: int) -> np.ndarray:
     return first
 
 
+def _digest_lists(first: np.ndarray) -> tuple[np.ndarray, np.ndarray]:
+    """Byte offset and length, among the digests of a batch with geometry first[S+1], of the list
+    of each block's payload's digests up to and with its own."""
+    first = first.astype(np.int64)
+    start = np.repeat(first[:-1], np.diff(first))
+    at = 8 * start
+    return at.astype(np.uint64), (8 * (np.arange(start.size) + 1) - at).astype(np.uint64)
+
+
 class Batch:
     """A batch of payloads in device memory: addresses, lengths and block geometry."""
 
@@ -334,6 +343,22 @@ class Batch:
         addr = [t.data_ptr() for t in tensors]
         lens = [t.numel() * t.element_size() for t in tensors]
         return cls(addr, lens, block_bytes, dev, keepalive=list(tensors))
+
+    @classmethod
+    def prefixes(cls, batch: "Batch", digests: torch.Tensor) -> "Batch":
+        """One payload and block for each block of `batch`: its payload's block digests up to and
+        with its own, out of `digests` (fp_chunks(batch)'s, not copied). fp_chunks() and detect()
+        of this batch identify each block together with all that comes before it in its payload,
+        as a prompt's cached keys and values have to be: they depend on every token before
+        theirs, a block's own digest on its bytes alone."""
+        _dev(digests, "digests", _U64, batch.n_blocks)
+        if digests.device != batch.d_first.device:
+            raise ValueError(f"digests are on {digests.device}, the batch on {batch.d_first.device}")
+        at, lens = _digest_lists(batch.host_first)
+        block = LEAF_BYTES
+        while block < int(lens.max(initial=0)):
+            block *= 2
+        return cls(at + np.uint64(digests.data_ptr()), lens, block, digests.device, keepalive=digests)
 
     @property
     def leaves_per_block(self) -> int:
