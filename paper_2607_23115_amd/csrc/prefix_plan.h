@@ -81,9 +81,9 @@ GLEAM_HD Cut cut_steps(uint32_t steps, uint32_t most) {
 // 2 * target (one for each kind) + kv_heads * tiles, and at most kv_heads * tiles * most_steps /
 // kMinFewSteps. Tiles: an item of n rows has at most n / kFewRows + 1 of them, and at most
 // n / kTileRows + kMostFew / kFewRows, and a token's rows are in two items at most, its group's
-// and its sequence's.
+// (if there are groups) and its sequence's.
 GLEAM_HD uint64_t most_first_units(const PlanShape& s) {  // kv_heads * tiles
-  const uint64_t rows = 2 * s.n_tokens * s.ratio, items = s.n_groups + s.n_seq;
+  const uint64_t rows = (s.n_groups ? 2 : 1) * s.n_tokens * s.ratio, items = s.n_groups + s.n_seq;
   const uint64_t few = items + rows / kFewRows, tile = kMostFew / kFewRows * items + rows / kTileRows;
   return s.kv_heads * (few < tile ? few : tile);
 }
@@ -96,12 +96,15 @@ GLEAM_HD uint64_t most_units(const PlanShape& s) {
 // Rows of partial results: an item that is cut, or shares its rows with another, has
 // rows * kv_heads * chunks. Shared: groups that are not joint have fewer than kJointRows rows a
 // sequence, in two items, for their first chunks. Cut: chunks >= 2 makes chunks <= 2 * steps /
-// chunk_steps, and rows <= kTileRows (kFewRows) * tiles, so 2 * (kTileRows + kFewRows) * target at
-// most.
+// chunk_steps, and an item's rows <= the rows of a tile * tiles, so 2 * target of the rows of a
+// tile at most for each kind. A tile has no more rows than all tokens have, and of the second kind
+// there is none where those are few.
 GLEAM_HD uint64_t most_partials(const PlanShape& s) {
   const uint64_t rows = s.n_tokens * s.ratio, apart = kJointRows * s.n_seq;
   const uint64_t shared = s.n_groups ? 2 * (rows < apart ? rows : apart) * s.kv_heads : 0;
-  return shared + 2ull * (kTileRows + kFewRows) * s.target;
+  const uint64_t few = rows < kFewRows ? rows : kFewRows;
+  const uint64_t tile = rows <= kMostFew ? 0 : rows < kTileRows ? rows : kTileRows;
+  return shared + 2 * (few + tile) * s.target;
 }
 
 }  // namespace gleam

@@ -162,3 +162,13 @@ def test_orders_of_pages_places_and_heads_that_do_not_overlap_are_taken(good):
     # strides of dimensions of one multiply nothing
     one = put(kv(k_stride=(0, 64, 0), v_stride=(8, 64, 8)), n_pages=1, kv_heads=1)
     assert append(one, n_tokens=1 << 31) == g.E_UNSUPPORTED
+
+
+def test_small_batches_ask_for_small_workspaces():
+    """A unit leaves no more rows of partial results than the batch has, of 256 units twice over."""
+    for d in (64, 128, 256):
+        cache = kv(head_dim=d, kv_heads=8, k_stride=(16 * 8 * d, d, 16 * d), v_stride=(16 * 8 * d, d, 16 * d))
+        for tokens, q_heads in ((1, 8), (1, 32), (3, 16)):
+            need = g.lib.gleam_prefix_attention_ws_bytes(ctypes.byref(cache), ctypes.byref(
+                batch(n_tokens=tokens, n_seq=1, n_groups=0, q_heads=q_heads, own_width=1 << 14)))
+            assert 0 < need <= 2 * 256 * (tokens * q_heads // 8) * (4 * d + 8) + 4096

@@ -114,3 +114,21 @@ def test_edges(plan):
     assert plan(8, 4, 1024, [(1, 0)], [(1, 0)])[0] == 0
     units, most, _, _ = plan(1, 1, 1024, [(1, 2**31 - 1)], [])
     assert 512 <= units <= 1025 <= most + 1
+
+
+def test_a_launch_without_groups_has_a_units_room_once(plan):
+    units, most, parts, most_parts = plan(32, 1, 256, [(8192, 8192)], [])
+    assert units <= most <= 2 * 256 + 32 * (64 + 4) and parts <= most_parts
+
+
+@pytest.mark.parametrize("seed", range(20))
+def test_bounds_hold_for_few_rows(plan, seed):
+    """Where tiles are not full the bounds are closest."""
+    rng = random.Random(1000 + seed)
+    for _ in range(20):
+        seqs = [(rng.choice([0, 1, 1, 2, 17, 64]), size(rng, 1 << 17)) for _ in range(rng.choice([1, 1, 2, 5]))]
+        n = rng.randint(0, len(seqs))
+        units, most_units, parts, most_parts = plan(rng.choice([1, 2, 8]), rng.choice([1, 1, 2, 4, 5]), 256, seqs,
+                                                    [(n, size(rng, 1 << 17))] if rng.random() < 0.6 else [],
+                                                    rng.choice([64, 128, 256]))
+        assert units <= most_units and parts <= most_parts, (seed, seqs, n)
