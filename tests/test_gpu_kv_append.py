@@ -274,3 +274,12 @@ def test_a_table_without_positions_gives_nan():
         assert torch.isnan(x[..., :32]).all() and (x[..., 32:] == 1).all()
     refused("rot_dim", rotary=lambda a: g.rotary_table(0, 24), positions=lambda a: a["slots"].int())
     refused("rot_dim", rotary=lambda a: torch.empty(0, 0, device="cuda"), positions=lambda a: a["slots"].int())
+
+
+def test_a_cache_without_pages():
+    say("kv_append without pages")
+    none = torch.empty(0, 16, 2, 64, dtype=torch.float16, device="cuda")
+    k = torch.randn(3, 2, 64, device="cuda").to(torch.float16)
+    got = g.kv_append(k, k, none, none, torch.tensor([0, 5, -1], device="cuda"), q=k)
+    torch.cuda.synchronize()
+    assert torch.equal(got, k)

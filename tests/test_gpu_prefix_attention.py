@@ -408,3 +408,63 @@ def test_gradients_are_refused_and_not_dropped():
         b = {**a, "q": torch.autograd.forward_ad.make_dual(a["q"], torch.ones_like(a["q"]))}
         with pytest.raises(ValueError, match="q requires a gradient"):
             g.prefix_attention(**b)
+
+
+def test_thousands_of_sequences_and_groups():
+    """Above 4,096 sequences and groups the plan keeps their offsets in the workspace, and with more
+    rows than 2,048 workgroups join at once those go on to others."""
+    gen = torch.Generator().manual_seed(11)
+    groups, at = [], 0
+    while len(groups) < 4200:
+        end = at + 1 + (len(groups) % 7 == 0)
+        groups.append((at, end, len(groups) % 23))
+        at = end
+    n_seq = at + 50
+    own = torch.randint(0, 20, (n_seq,), generator=gen).tolist()
+    n = torch.randint(0, 3, (n_seq,), generator=gen).tolist()
+    c = Case(n, own, groups, 2, 1, 256, 16, F16)
+    assert n_seq > 4096 and c.q.shape[0] * 2 > 2048 * 4  # 4 rows of 256 dims a workgroup
+    c.check()
+
+
+@pytest.mark.parametrize("n_seq,groups", [(62, 1), (64, 1), (65, 0), (200, 12), (1000, 23), (1023, 0), (1024, 1)])
+def test_batches_on_both_sides_of_a_plan_of_their_own(n_seq, groups):
+    gen = torch.Generator().manual_seed(n_seq)
+    own = torch.randint(0, 90, (n_seq,), generator=gen).tolist()
+    n = [1 + (i % 11 == 3) for i in range(n_seq)]
+    n[5], own[5] = 70, 150
+    first = [n_seq * i // max(groups, 1) for i in range(groups + 1)]
+    Case(n, own, [(a, b, 17 + 40 * i) for i, (a, b) in enumerate(zip(first, first[1:]))], 4, 2, 64, 16, BF16,
+         seed=n_seq).check()
+
+
+@pytest.mark.parametrize("d,hkv", [(64, 64), (128, 32), (256, 16)])
+def test_histories_that_are_not_kept_in_the_caches(d, hkv):
+    """Of 128 MiB and a little, its end ragged and a page missing; three of the heads."""
+    page, own = 16, 8203
+    say("prefix_attention long history", d, hkv, own)
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    pages = -(-own // page)
+    kp, vp = (torch.randn(pages, hkv, page, d, generator=gen, device="cuda").to(BF16).transpose(1, 2) for _ in range(2))
+    table = torch.randperm(pages, generator=gen, device="cuda").to(torch.int32)[None]
+    table[0, 100] = -1
+    q = torch.randn(1, hkv, d, generator=gen, device="cuda").to(BF16)
+    first, length = i32([0, 1]), i32([own])
+    assert own * hkv * 4 * d >= 128 << 20
+    out, lse = g.prefix_attention(q, kp, vp, first.cuda(), table, length.cuda(), want_lse=True)
+    torch.cuda.synchronize()
+    for h in (0, hkv // 2 + 1, hkv - 1):
+        o, l, o_tol, l_tol = R.attention(q[:, h:h + 1].cpu(), kp[:, :, h:h + 1].cpu(), vp[:, :, h:h + 1].cpu(), first,
+                                         table.cpu(), length)
+        R.near(lse[:, h:h + 1], l, l_tol, "lse")
+        R.near(out[:, h:h + 1], o, o_tol, "out")
+
+
+def test_a_cache_without_pages():
+    say("prefix_attention without pages")
+    none = torch.empty(0, 16, 2, 64, dtype=F16, device="cuda")
+    q = torch.randn(3, 4, 64, device="cuda").to(F16)
+    out, lse = g.prefix_attention(q, none, none, i32([0, 2, 3]).cuda(), i32([[0], [5]]).cuda(), i32([7, 1]).cuda(),
+                                  i32([0, 2]).cuda(), i32([[0]]).cuda(), i32([9]).cuda(), want_lse=True)
+    torch.cuda.synchronize()
+    assert (out == 0).all() and (lse == -math.inf).all()
