@@ -10,8 +10,8 @@
 // head, 16 dimensions each, so that both members of 8 pairs are in one lane (no exchange for the
 // rotation; the norm's sum takes log2(head_dim / 16) exchanges) and every access is 16 bytes. A
 // lane rotates the same pairs of every head, so a wave that keeps to one token loads its cosines
-// and sines once. 16,384 tokens of 32 and 8 heads of 128: 83 us, 4.9 TB/s (a copy of as many bytes
-// 78 us); one token 2.8 us.
+// and sines once. 16,384 tokens of 32 and 8 heads of 128: 84 us, 4.9 TB/s (a copy of as many bytes
+// 78 us); one token 2.6 us.
 
 #include <algorithm>
 

@@ -25,7 +25,8 @@
 //           operand a lane holds those 8 keys' dims (lane % 16) * D/16 .. + D/16, loaded row by
 //           row and transposed within the lane.
 // With few rows this is bound by reading the keys and values once: one token of 32 heads behind
-// 131,071 keys of 8 heads of 128 takes 84 us (6.4 TB/s; a plain read reaches 7.1), the join 5 more.
+// 131,071 keys of 8 heads of 128 takes 85 us (6.3 TB/s; a plain read reaches 7.1), the join 5 more. 64
+// sequences of 8,192 keys, nothing shared, take 366 us, 5.9 TB/s.
 // Items of more than 64 rows take units of 128 rows (attend_tile).
 
 #include <type_traits>
@@ -50,6 +51,10 @@ constexpr uint64_t kMostSeq = 1ull << 20;
 constexpr uint64_t kPassing = 128ull << 20;  // bytes of an item's keys and values
 constexpr uint32_t kWideJoin = 256;    // up to this many rows are joined by a workgroup each
 constexpr uint32_t kMostJoins = 2048;  // workgroups of the others: those that the GPU holds at once
+// Units wanted of each kind: one a CU, chosen by measurement. A CU holds two (of heads of 256 one), but
+// with 512 an item is cut into twice the pieces: 1.6% slower over twelve cases and fourteen drawn ones, 128
+// sequences behind 8,192 keys 70 us for 58.
+constexpr uint32_t kUnits = 256;
 
 struct Item {
   uint32_t token_first, tokens;  // rows: tokens * ratio
@@ -344,7 +349,7 @@ __device__ inline Item item_of_lane(const Item& it, uint32_t i) {
   return r;
 }
 
-// One workgroup, whose time is that of its loads and seven barriers: 4.8 us for 65 items, 6.2 for
+// One workgroup, whose time is that of its loads and seven barriers: 4.3 us for 65 items, 6.2 for
 // 204. Offsets of up to this many sequences and groups are kept in LDS, of more in the workspace.
 constexpr uint32_t kPlanLds = 4096;
 
@@ -693,9 +698,9 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
       }
     }
   };
-  // Keys and values that one tile reads, and that are too many for the caches to have at the next
-  // call, are not kept there (one token of 8 key heads: behind 131,072 keys 90 us, 102 where they
-  // are; behind 32,768 31.0 and 30.5).
+  // An item's keys and values that one tile reads, and that are too many for the caches to have at the
+  // next call, are not kept there (one token of 8 key heads: behind 131,072 keys 90 us, 102 where they
+  // are; behind 32,768 31.0 and 30.5). What the rest of the batch reads is not looked at.
   const bool once = rows <= kFewRows && ((uint64_t)it.prefix_keys + it.own_keys) * a.kv_heads * (4 * D) >= kPassing;
   auto load_half = [&](uint32_t half, auto set_) {
     constexpr int set = decltype(set_)::value;
@@ -880,9 +885,11 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
 // 128 rows, 32 a wave, over keys that the workgroup stages in LDS: a sub-step's keys are loaded
 // into registers two sub-steps ahead, and stored one ahead. A SIMD has one wave of each of two
 // workgroups: as these share no barrier, the products of one go on under the other's softmax.
-// 8,192 tokens of 32 heads of 128: 680 us, 810 TFLOP/s, where a library product of 8,192 cubed
-// reaches 1,150 to 1,200. No unit is the limit by itself: of a step's 1.3 us its products, counted
-// at 2.4 GHz, take 0.4, the exponentials with the rest of the softmax 0.5, the LDS 0.5.
+// 8,192 tokens of 32 heads of 128: 630 to 680 us from box to box, 810 to 870 TFLOP/s, where a library
+// product of 8,192 cubed reaches 1,150 to 1,280. No unit is the limit by itself: of a step's 1.3 us
+// its products take 0.4, the exponentials with the rest of the softmax 0.5, the LDS 0.5, as counted
+// from the instructions at 2.4 GHz. With heads of 256, of one workgroup a CU and a barrier every 32
+// keys, 4,096 tokens of 16 heads on 4 take 284 us, 480 TFLOP/s (heads of 128: 118 us, 580).
 //
 // Products are v_mfma_f32_32x32x16 in the same orientation: S^T = K Q^T, O^T = V^T P^T, a lane
 // holding one row's scores with keys 8 i + 4 h .. + 3 (h = lane / 32), which again are P's operand
@@ -1269,7 +1276,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(Atte
 // D/4 lanes take a piece of a row, 4 dims each. Where there are many rows they join all of its
 // pieces, 64 / (D/4) rows a wave; with few rows (kWide) a workgroup's lanes share the pieces of
 // one. Four pieces are in flight at a time. Bound by reading the pieces, or with few by the time
-// of half a dozen loads that wait for each other: 4 to 5 us, 7 for 2,048 rows of some ten pieces.
+// of half a dozen loads that wait for each other: 4 to 5 us, 7 for 2,048 rows of some ten pieces, 2
+// where no row has pieces.
 // Rows that no piece covers are set to nothing seen.
 template <class T, int D, bool kWide>
 __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a) {
@@ -1422,7 +1430,7 @@ gleam_status validate_attention(const gleam_kv_pages* kv, const gleam_prefix_bat
   shape->n_groups = b->n_groups;
   shape->kv_heads = kv->kv_heads;
   shape->ratio = b->q_heads / kv->kv_heads;
-  shape->target = 256;
+  shape->target = kUnits;
   shape->head_dim = kv->head_dim;
   const uint64_t most = steps_of((uint32_t)(b->own_width * kv->page_tokens)) +
                         (uint64_t)steps_of((uint32_t)(b->prefix_width * kv->page_tokens));

@@ -35,7 +35,7 @@ GLEAM_HD uint32_t min_tile_steps(uint32_t head_dim) { return 512 / head_dim; }
 struct PlanShape {  // what the host knows
   uint64_t n_tokens, n_seq, n_groups;
   uint32_t kv_heads, ratio;  // ratio: query heads per key head
-  uint32_t target;           // units of each kind wanted: what the GPU holds at once
+  uint32_t target;           // units of each kind wanted (kUnits of the launch)
   uint32_t most_steps;       // of an item, from the widths of the page tables
   uint32_t head_dim;
 };
