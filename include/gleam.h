@@ -734,6 +734,123 @@ gleam_status gleam_prefix_attention(const gleam_kv_pages* kv, const gleam_prefix
                                     float* d_lse, void* d_ws, size_t ws_bytes, void* stream);
 
 /*
+ * Trees of drafted tokens. A sequence's new tokens may be drafts of which several follow the same one:
+ * a tree, checked by one call, of which one path is kept. d_seen holds for each token seen_words words of
+ * 64 bits: bit j says that it sees draft j of its sequence (itself among them), counted from the sequence's
+ * first new token. Drafts beyond 64 * seen_words of a sequence have no bit and are seen by none.
+ *
+ * gleam_draft_tree: the bits of a forest. d_parent[t] is the draft that token t follows, as an index
+ * among its sequence's (-1: none; one that does not come before t counts as none). Token t sees itself, its
+ * parent, the parent's parent and so on; d_depth[t] (nullable) = how many of those come before it: its
+ * position is the sequence's length before the drafts plus that. Tokens of no sequence get 0.
+ *   d_parent  int32[n_tokens]
+ *   d_q_first int32[n_seq + 1], non-decreasing (a sequence that ends before it starts has no tokens)
+ *   d_seen    uint64[n_tokens][seen_words], seen_words 1 to 65536
+ * Errors: GLEAM_E_INVALID, GLEAM_E_UNSUPPORTED (more than 2^20 sequences, or 2^31 tokens), GLEAM_E_HIP.
+ *
+ * gleam_tree_attention: gleam_prefix_attention of such drafts, whose keys are the last n of their
+ * sequence's own: token i of n sees its group's whole prefix, the own keys before the first draft's, and
+ * the key of draft j (number d_own_len[s] - n + j of the own keys, where that is not below 0) if its bit j
+ * is set. Any bits are taken, not only those of trees; a row may see nothing. Arguments, workspace, limits
+ * and errors are gleam_prefix_attention's.
+ *
+ * gleam_kv_accept: the keys and values of the path that was accepted move together. Of sequence s those
+ * drafts are kept that draft d_leaf[s] sees (none where d_leaf[s] is not one of its drafts): the e-th of
+ * them goes to the place of draft e, and d_len_out[s] = the keys before the drafts and those kept. What
+ * lies behind is left as it is. Keys in a page that the cache does not have are neither read nor written.
+ * The cache's places must not overlap (as for gleam_kv_append), a page must be in one place of the table
+ * only, and d_len_out must not overlap d_own_len.
+ * Errors: GLEAM_E_INVALID, GLEAM_E_UNSUPPORTED (more than 2^20 sequences, or 2^31 tokens), GLEAM_E_HIP.
+ */
+typedef struct gleam_accept {
+  const int32_t* d_q_first;
+  const uint64_t* d_seen;
+  const int32_t* d_leaf;
+  const int32_t* d_own_pages;
+  const int32_t* d_own_len;
+  int32_t* d_len_out;
+  uint64_t n_tokens, n_seq, own_width;
+  uint32_t seen_words;
+} gleam_accept;
+
+gleam_status gleam_draft_tree(const int32_t* d_parent, const int32_t* d_q_first, uint64_t n_tokens, uint64_t n_seq,
+                              uint64_t* d_seen, uint32_t seen_words, int32_t* d_depth, void* stream);
+gleam_status gleam_tree_attention(const gleam_kv_pages* kv, const gleam_prefix_batch* b, const uint64_t* d_seen,
+                                  uint32_t seen_words, void* d_out, float* d_lse, void* d_ws, size_t ws_bytes,
+                                  void* stream);
+gleam_status gleam_kv_accept(const gleam_kv_pages* kv, const gleam_accept* a, void* stream);
+
+/*
+ * Keeping a cache within a budget: keys that gathered little attention make room for new ones. Two numbers
+ * are kept for each place and key head, in [n_pages][kv_heads][page_tokens]: float weights, the attention
+ * that the key was given so far, and int32 born, the position of its token.
+ *
+ * gleam_kv_weigh: after an attention call that returned its lse, for each own key and key head
+ *   weights_out = weights (0 for the keys of the batch's own new tokens) + sum exp(scale * q.k - lse)
+ * over the new tokens' rows that see the key: token i (of n) of sequence s and the q_heads / kv_heads query
+ * heads of the key head; it sees the own keys j < d_own_len[s] - n + i + 1. Products and sums are kept in 32
+ * bits. A row whose lse is +infinity adds nothing. For the new tokens' keys born = d_positions of the
+ * token. What is not an own key of a sequence is left as it is, a shared prefix too: no sequence may drop
+ * its keys by itself. Only the cache's keys are read (d_v may be d_k). A page in two places of the table
+ * gets either's weights.
+ *   q                as gleam_prefix_attention's; d_q_first as gleam_draft_tree's
+ *   d_lse            float[n_tokens][q_heads]
+ *   d_weights_out    may be d_weights itself, and must not overlap it otherwise
+ *   d_born, d_positions   nullable together; int32[n_tokens] positions
+ * Errors: GLEAM_E_INVALID, GLEAM_E_UNSUPPORTED (n_tokens * q_heads of 2^31 or more, more than 2^20
+ * sequences), GLEAM_E_HIP.
+ *
+ * gleam_kv_evict: of sequence s with more than `keep` own keys, each key head keeps `keep`: first those born
+ * before `sinks` or in the last `recent` positions before d_total[s], the sequence's tokens so far; then
+ * those of the largest weights (NaN is less than all); among equals those of the lowest places. Kept keys
+ * at places from `keep` on move to the places before it that come free, the first to the first and so on,
+ * their weights and births with them. d_len_out[s] = min(d_own_len[s], keep). What lies behind is left as
+ * it is. Heads keep keys of different tokens; attention does not need their order, as positions are
+ * rotated into the keys. New tokens' keys come behind them. Keys in a page that the cache does not have are
+ * the first to go, and what would move into such a page is lost. The cache's places must not overlap, a page
+ * must be in one place of the table only.
+ *   d_weights_out, d_born_out  may be d_weights and d_born themselves, and must not overlap them otherwise;
+ *                    written for the first `keep` keys of each sequence
+ *   d_len_out        may be d_own_len
+ *   d_ws             device, 256-byte aligned, >= gleam_kv_evict_ws_bytes(kv, e)
+ * Errors: GLEAM_E_INVALID, GLEAM_E_WORKSPACE, GLEAM_E_UNSUPPORTED (more than 2^20 sequences, 2^31 sequences
+ * times heads, or 2^36 keys that may move), GLEAM_E_HIP. gleam_kv_evict_ws_bytes returns 0 for arguments
+ * the call refuses; it depends on the shapes, not on pointers.
+ */
+typedef struct gleam_weigh {
+  const void* d_q;
+  const int32_t* d_q_first;
+  const int32_t* d_own_pages;
+  const int32_t* d_own_len;
+  const float* d_lse;
+  const float* d_weights;
+  float* d_weights_out;
+  int32_t* d_born;
+  const int32_t* d_positions;
+  uint64_t n_tokens, n_seq, own_width;
+  int64_t q_stride[2];
+  uint32_t q_heads;
+  float scale;
+} gleam_weigh;
+
+typedef struct gleam_evict {
+  const int32_t* d_own_pages;
+  const int32_t* d_own_len;
+  const float* d_weights;
+  const int32_t* d_born;
+  const int32_t* d_total;
+  float* d_weights_out;
+  int32_t* d_born_out;
+  int32_t* d_len_out;
+  uint64_t n_seq, own_width;
+  uint32_t keep, sinks, recent;
+} gleam_evict;
+
+gleam_status gleam_kv_weigh(const gleam_kv_pages* kv, const gleam_weigh* w, void* stream);
+size_t gleam_kv_evict_ws_bytes(const gleam_kv_pages* kv, const gleam_evict* e);
+gleam_status gleam_kv_evict(const gleam_kv_pages* kv, const gleam_evict* e, void* d_ws, size_t ws_bytes, void* stream);
+
+/*
  * Calibration (a measurement aid, not a step of the path): read `bytes` bytes at d_src
  * (device, 16-byte aligned, bytes a multiple of 16) once, with the fastest plain read
  * pattern measured on MI355X, and XOR into *d_sink (device u64, caller-initialised) the

@@ -49,7 +49,8 @@ EXPORTS = (
     "gleam_cache_lookup_noalloc", "gleam_cache_lookup_noalloc_max_keys", "gleam_detect",
     "gleam_detect_ws_init", "gleam_identify_leaves", "gleam_first_writes_ws_bytes", "gleam_first_writes",
     "gleam_cache_erase_bytes", "gleam_detect_workspace_bytes", "gleam_preload", "gleam_rotary_table",
-    "gleam_kv_append", "gleam_prefix_attention_ws_bytes", "gleam_prefix_attention",
+    "gleam_kv_append", "gleam_prefix_attention_ws_bytes", "gleam_prefix_attention", "gleam_draft_tree",
+    "gleam_tree_attention", "gleam_kv_accept", "gleam_kv_weigh", "gleam_kv_evict_ws_bytes", "gleam_kv_evict",
 )
 
 
@@ -92,6 +93,21 @@ class _PrefixBatch(ctypes.Structure):
                                "q_heads:u4 scale:f4")
 
 
+class _Accept(ctypes.Structure):
+    _fields_ = _fields(_KINDS, "q_first:p seen:p leaf:p own_pages:p own_len:p len_out:p n_tokens:u8 n_seq:u8 "
+                               "own_width:u8 seen_words:u4")
+
+
+class _Weigh(ctypes.Structure):
+    _fields_ = _fields(_KINDS, "q:p q_first:p own_pages:p own_len:p lse:p weights:p weights_out:p born:p positions:p "
+                               "n_tokens:u8 n_seq:u8 own_width:u8 q_token:i8 q_head:i8 q_heads:u4 scale:f4")
+
+
+class _Evict(ctypes.Structure):
+    _fields_ = _fields(_KINDS, "own_pages:p own_len:p weights:p born:p total:p weights_out:p born_out:p len_out:p "
+                               "n_seq:u8 own_width:u8 keep:u4 sinks:u4 recent:u4")
+
+
 def _load() -> ctypes.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"libgleam.so is not built at {LIB_PATH}; run python -m paper_2607_23115_amd.build")
@@ -104,6 +120,12 @@ def _load() -> ctypes.CDLL:
         "gleam_kv_append": ([kv, ctypes.POINTER(_Append), vp], st),
         "gleam_prefix_attention_ws_bytes": ([kv, batch], sz),
         "gleam_prefix_attention": ([kv, batch, vp, vp, vp, sz, vp], st),
+        "gleam_draft_tree": ([vp, vp, u64, u64, vp, u32, vp, vp], st),
+        "gleam_tree_attention": ([kv, batch, vp, u32, vp, vp, vp, sz, vp], st),
+        "gleam_kv_accept": ([kv, ctypes.POINTER(_Accept), vp], st),
+        "gleam_kv_weigh": ([kv, ctypes.POINTER(_Weigh), vp], st),
+        "gleam_kv_evict_ws_bytes": ([kv, ctypes.POINTER(_Evict)], sz),
+        "gleam_kv_evict": ([kv, ctypes.POINTER(_Evict), vp, sz, vp], st),
         "gleam_batch_geometry": ([vp, u64, u32, vp, vp], st),
         "gleam_fp_chunks": ([ctypes.POINTER(_Batch), vp, vp, vp], st),
         "gleam_cache_bytes": ([u64], sz),
@@ -1033,7 +1055,7 @@ def prefix_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
                      own_pages: torch.Tensor, own_len: torch.Tensor, group_first: torch.Tensor | None = None,
                      prefix_pages: torch.Tensor | None = None, prefix_len: torch.Tensor | None = None,
                      scale: float | None = None, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
-                     want_lse: bool = False, ws: torch.Tensor | None = None, stream=None):
+                     want_lse: bool = False, ws: torch.Tensor | None = None, stream=None, _seen=None):
     """Attention of a ragged batch over the paged cache: (out [tokens, q_heads, head_dim], lse
     float32 [tokens, q_heads] or None).
 
@@ -1090,8 +1112,13 @@ def prefix_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
             ws_at, ws_bytes = _flat(ws, "ws", torch.uint8, dev), ws.numel()
         if (q.requires_grad or k_pages.requires_grad or v_pages.requires_grad or out.requires_grad
                 or lse is not None and lse.requires_grad or not _forward or _forward._current_level >= 0):
-            _no_gradient("prefix_attention", q=q, k_pages=k_pages, v_pages=v_pages, out=out, lse=lse)
-        _check(lib.gleam_prefix_attention(kv, b, out_at, lse_at, ws_at, ws_bytes, hs))
+            _no_gradient("tree_attention" if _seen else "prefix_attention", q=q, k_pages=k_pages, v_pages=v_pages,
+                         out=out, lse=lse)
+        if _seen:  # tree_attention's: (tensor, words)
+            seen_at = _flat(_seen[0], "seen", torch.int64, dev, tokens * _seen[1])
+            _check(lib.gleam_tree_attention(kv, b, seen_at, _seen[1], out_at, lse_at, ws_at, ws_bytes, hs))
+        else:
+            _check(lib.gleam_prefix_attention(kv, b, out_at, lse_at, ws_at, ws_bytes, hs))
     return out, lse
 
 
@@ -1108,3 +1135,200 @@ def prefix_attention_workspace(k_pages: torch.Tensor, v_pages: torch.Tensor, tok
     overlap need one each)."""
     b = _PrefixBatch(n_tokens=tokens, n_seq=n_seq, n_groups=n_groups, q_heads=q_heads)
     return torch.empty(_attention_ws(_kv_struct(k_pages, v_pages), b), dtype=torch.uint8, device=k_pages.device)
+
+
+# --------------------------------------------------------------------------- #
+# Trees of drafted tokens over that cache, and the cache kept within a budget
+# --------------------------------------------------------------------------- #
+def _ragged(own_pages, own_len, dev: int):
+    """(pages' address, width, lengths' address, sequences) of a page table and its lengths."""
+    len_at = _flat(own_len, "own_len", torch.int32, dev)
+    n_seq = own_len.numel()
+    pages_at = _flat(own_pages, "own_pages", torch.int32, dev)
+    if own_pages.dim() != 2 or own_pages.shape[0] != n_seq:
+        raise ValueError(f"own_pages must be [{n_seq}, pages], not {list(own_pages.shape)}")
+    return pages_at, own_pages.shape[1], len_at, n_seq
+
+
+def _seen_words(seen, tokens: int | None = None) -> int:
+    if not isinstance(seen, torch.Tensor) or seen.dim() != 2 or (tokens is not None and seen.shape[0] != tokens):
+        raise ValueError(f"seen must be [{'tokens' if tokens is None else tokens}, words]")
+    return seen.shape[1]
+
+
+def draft_tree(parent: torch.Tensor, q_first: torch.Tensor, width: int, seen: torch.Tensor | None = None,
+               depth: torch.Tensor | None = None, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
+    """(seen int64 [tokens, words], depth int32 [tokens]) of drafted tokens, a tree (or several) for each sequence.
+
+    parent int32 [tokens]: the draft that each one follows, counted within its sequence, -1 for none;
+    sequence s has tokens q_first[s] to q_first[s + 1] (int32). Bit j of a token's row of seen: it sees
+    draft j of its sequence, that is itself or one that it descends from. depth: how many of those
+    come before it. width: most drafts of a sequence (words = ceil(width / 64); drafts beyond that
+    are seen by none). Tokens of no sequence get 0."""
+    if not isinstance(parent, torch.Tensor) or parent.get_device() < 0:
+        raise ValueError("parent must be a tensor on the GPU")
+    dev, i32 = parent.get_device(), torch.int32
+    if width < 1:
+        raise ValueError("width must be positive")
+    words = (width + 63) // 64
+    parent_at, tokens = _flat(parent, "parent", i32, dev), parent.numel()
+    first_at = _flat(q_first, "q_first", i32, dev, 1)
+    with _on_stream(stream, parent.device) as hs:
+        if seen is None:
+            seen = torch.empty((tokens, words), dtype=torch.int64, device=parent.device)
+        elif _seen_words(seen, tokens) != words:
+            raise ValueError(f"seen must be [{tokens}, {words}]")
+        if depth is None:
+            depth = torch.empty_like(parent)
+        seen_at, depth_at = _flat(seen, "seen", torch.int64, dev), _flat(depth, "depth", i32, dev, tokens)
+        _check(lib.gleam_draft_tree(parent_at, first_at, tokens, q_first.numel() - 1, seen_at, words, depth_at, hs))
+    return seen, depth
+
+
+def tree_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, q_first: torch.Tensor,
+                   seen: torch.Tensor, own_pages: torch.Tensor, own_len: torch.Tensor,
+                   group_first: torch.Tensor | None = None, prefix_pages: torch.Tensor | None = None,
+                   prefix_len: torch.Tensor | None = None, scale: float | None = None,
+                   out: torch.Tensor | None = None, lse: torch.Tensor | None = None, want_lse: bool = False,
+                   ws: torch.Tensor | None = None, stream=None):
+    """prefix_attention() of trees of drafted tokens: (out, lse or None).
+
+    The drafts' keys are the last of their sequence's own, in the drafts' order. A token sees its
+    group's prefix, the keys before the drafts, and of its sequence's drafts those whose bits are set
+    in its row of seen (int64 [tokens, words], draft_tree()'s or any other). Everything else is
+    prefix_attention()'s, the workspace too."""
+    words = _seen_words(seen, q.shape[0] if isinstance(q, torch.Tensor) and q.dim() else None)
+    return prefix_attention(q, k_pages, v_pages, q_first, own_pages, own_len, group_first, prefix_pages, prefix_len,
+                            scale, out, lse, want_lse, ws, stream, (seen, words))
+
+
+def kv_accept(k_pages: torch.Tensor, v_pages: torch.Tensor, q_first: torch.Tensor, seen: torch.Tensor,
+              leaf: torch.Tensor, own_pages: torch.Tensor, own_len: torch.Tensor,
+              len_out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Keep the keys and values of one path of each sequence's drafts; returns the new lengths.
+
+    leaf int32 [sequences]: the path's last draft, counted within the sequence, -1 to keep none. The
+    drafts that it sees move, in order, to the places of the first drafts, and len_out (int32, not
+    own_len itself: other layers' caches still need that) is the keys before the drafts and theirs."""
+    kv = _kv_struct(k_pages, v_pages)
+    dev, i32 = k_pages.get_device(), torch.int32
+    pages_at, width, len_at, n_seq = _ragged(own_pages, own_len, dev)
+    first_at = _flat(q_first, "q_first", i32, dev, n_seq + 1)
+    words = _seen_words(seen)
+    seen_at, leaf_at = _flat(seen, "seen", torch.int64, dev), _flat(leaf, "leaf", i32, dev, n_seq)
+    with _on_stream(stream, k_pages.device) as hs:
+        if len_out is None:
+            len_out = torch.empty_like(own_len)
+        out_at = _flat(len_out, "len_out", i32, dev, n_seq)
+        if k_pages.requires_grad or v_pages.requires_grad or not _forward or _forward._current_level >= 0:
+            _no_gradient("kv_accept", k_pages=k_pages, v_pages=v_pages)
+        args = _Accept(first_at, seen_at, leaf_at, pages_at, len_at, out_at, seen.shape[0], n_seq, width, words)
+        _check(lib.gleam_kv_accept(kv, args, hs))
+    return len_out
+
+
+def _tracked(t: torch.Tensor | None, name: str, dtype: torch.dtype, kv: _KvPages, dev: int):
+    """Address of what is kept for each place and key head."""
+    shape = (kv.n_pages, kv.kv_heads, kv.page_tokens)
+    at = _flat(t, name, dtype, dev)
+    if t.shape != shape:
+        raise ValueError(f"{name} must be [pages, kv_heads, page_tokens] = {list(shape)}, not {list(t.shape)}")
+    return at
+
+
+def kv_weigh(q: torch.Tensor, k_pages: torch.Tensor, q_first: torch.Tensor, own_pages: torch.Tensor,
+             own_len: torch.Tensor, lse: torch.Tensor, weights: torch.Tensor, born: torch.Tensor | None = None,
+             positions: torch.Tensor | None = None, weights_out: torch.Tensor | None = None,
+             scale: float | None = None, stream=None) -> torch.Tensor:
+    """Add the attention that new tokens gave each of their sequence's own keys; returns the weights.
+
+    q, q_first, own_pages, own_len, scale and lse (float32 [tokens, q_heads]) as prefix_attention()
+    had or returned them. weights float32 [pages, kv_heads, page_tokens]: the sums so far, of the new
+    tokens' own keys started at 0, written to weights_out (weights itself where that is not given).
+    born int32 of the same shape: the new keys' places get their tokens' positions (int32 [tokens])."""
+    kv = _kv_struct(k_pages, k_pages)
+    dtype, dev, d = k_pages.dtype, k_pages.get_device(), kv.head_dim
+    q_at, tokens, heads, q_token, q_head = _heads(q, "q", dtype, dev, d)
+    pages_at, width, len_at, n_seq = _ragged(own_pages, own_len, dev)
+    first_at = _flat(q_first, "q_first", torch.int32, dev, n_seq + 1)
+    lse_at = _flat(lse, "lse", torch.float32, dev)
+    if lse.shape != q.shape[:2]:
+        raise ValueError("lse must be [tokens, q_heads]")
+    weights_at = to_at = _tracked(weights, "weights", torch.float32, kv, dev)
+    if weights_out is None:
+        weights_out = weights
+    else:
+        to_at = _tracked(weights_out, "weights_out", torch.float32, kv, dev)
+    born_at, positions_at = None, None
+    if born is not None or positions is not None:
+        born_at = _tracked(born, "born", torch.int32, kv, dev)
+        positions_at = _flat(positions, "positions", torch.int32, dev, tokens)
+        if tokens == 0 or kv.n_pages == 0:
+            born_at = positions_at = None
+    with _on_stream(stream, k_pages.device) as hs:
+        if (q.requires_grad or k_pages.requires_grad or lse.requires_grad or weights.requires_grad
+                or weights_out.requires_grad or not _forward or _forward._current_level >= 0):
+            _no_gradient("kv_weigh", q=q, k_pages=k_pages, lse=lse, weights=weights, weights_out=weights_out)
+        args = _Weigh(q_at, first_at, pages_at, len_at, lse_at, weights_at, to_at, born_at, positions_at, tokens, n_seq,
+                      width, q_token, q_head, heads, d ** -0.5 if scale is None else scale)
+        _check(lib.gleam_kv_weigh(kv, args, hs))
+    return weights_out
+
+
+def kv_evict(k_pages: torch.Tensor, v_pages: torch.Tensor, own_pages: torch.Tensor, own_len: torch.Tensor,
+             weights: torch.Tensor, born: torch.Tensor, total: torch.Tensor, keep: int, sinks: int = 0,
+             recent: int = 0, weights_out: torch.Tensor | None = None, born_out: torch.Tensor | None = None,
+             len_out: torch.Tensor | None = None, ws: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Cut each sequence down to `keep` own keys for each key head; returns the new lengths.
+
+    weights and born [pages, kv_heads, page_tokens] as kv_weigh() keeps them, total int32 [sequences]
+    the tokens that each sequence has had. Keys born before `sinks`, or in the last `recent` of the
+    total, are kept first, then those of the largest weights; kept keys from place `keep` on move
+    into the places before it that come free, weights and births with them (in weights and born
+    themselves where weights_out and born_out are not given). ws: from kv_evict_workspace()."""
+    kv = _kv_struct(k_pages, v_pages)
+    dev, i32, f32 = k_pages.get_device(), torch.int32, torch.float32
+    pages_at, width, len_at, n_seq = _ragged(own_pages, own_len, dev)
+    weights_at = weights_to = _tracked(weights, "weights", f32, kv, dev)
+    born_at = born_to = _tracked(born, "born", i32, kv, dev)
+    if weights_out is not None:
+        weights_to = _tracked(weights_out, "weights_out", f32, kv, dev)
+    if born_out is not None:
+        born_to = _tracked(born_out, "born_out", i32, kv, dev)
+    total_at = _flat(total, "total", i32, dev, n_seq)
+    for n, x in (("keep", keep), ("sinks", sinks), ("recent", recent)):
+        if not 0 <= x < 1 << 32:
+            raise ValueError(f"{n} must not be negative, and below 2^32")
+    with _on_stream(stream, k_pages.device) as hs:
+        if len_out is None:
+            len_out = torch.empty_like(own_len)
+        out_at = _flat(len_out, "len_out", i32, dev, n_seq)
+        args = _Evict(pages_at, len_at, weights_at, born_at, total_at, weights_to, born_to, out_at, n_seq, width, keep,
+                      sinks, recent)
+        if ws is None:
+            ws_bytes = _evict_ws(kv, args)
+            ws = torch.empty(ws_bytes, dtype=torch.uint8, device=k_pages.device)
+            ws_at = ws.data_ptr()
+        else:
+            ws_at, ws_bytes = _flat(ws, "ws", torch.uint8, dev), ws.numel()
+        if (k_pages.requires_grad or v_pages.requires_grad or weights.requires_grad
+                or weights_out is not None and weights_out.requires_grad or not _forward
+                or _forward._current_level >= 0):
+            _no_gradient("kv_evict", k_pages=k_pages, v_pages=v_pages, weights=weights, weights_out=weights_out)
+        _check(lib.gleam_kv_evict(kv, args, ws_at, ws_bytes, hs))
+    return len_out
+
+
+def _evict_ws(kv: _KvPages, args: _Evict) -> int:
+    n = lib.gleam_kv_evict_ws_bytes(kv, args)
+    if n == 0:
+        raise GleamError(E_INVALID, lib.gleam_last_error().decode())
+    return n
+
+
+def kv_evict_workspace(k_pages: torch.Tensor, v_pages: torch.Tensor, n_seq: int, own_width: int,
+                       keep: int) -> torch.Tensor:
+    """A workspace for kv_evict() calls of n_seq sequences with page tables own_width wide, cut down to
+    `keep` (calls that may overlap need one each)."""
+    args = _Evict(n_seq=n_seq, own_width=own_width, keep=keep)
+    return torch.empty(_evict_ws(_kv_struct(k_pages, v_pages), args), dtype=torch.uint8, device=k_pages.device)

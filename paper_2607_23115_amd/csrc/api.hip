@@ -109,7 +109,7 @@ extern "C" gleam_status gleam_preload(void) {
   hipError_t (*const loads[])() = {preload_fp_chunks, preload_cache,    preload_compact, preload_detect,
                                    preload_identify,  preload_first_write, preload_md5,  preload_lifecycle,
                                    preload_transfer,  preload_remap,    preload_calib,   preload_kv_append,
-                                  preload_prefix_attention};
+                                   preload_prefix_attention, preload_drafts, preload_kv_weigh, preload_kv_evict};
   for (auto load : loads) {
     const hipError_t e = load();
     if (e != hipSuccess) {

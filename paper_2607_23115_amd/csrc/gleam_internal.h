@@ -97,10 +97,13 @@ hipError_t preload_cache();
 hipError_t preload_calib();
 hipError_t preload_compact();
 hipError_t preload_detect();
+hipError_t preload_drafts();
 hipError_t preload_first_write();
 hipError_t preload_fp_chunks();
 hipError_t preload_identify();
 hipError_t preload_kv_append();
+hipError_t preload_kv_evict();
+hipError_t preload_kv_weigh();
 hipError_t preload_lifecycle();
 hipError_t preload_md5();
 hipError_t preload_prefix_attention();

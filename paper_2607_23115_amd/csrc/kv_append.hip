@@ -95,6 +95,19 @@ bool places_apart(const gleam_kv_pages& kv, const int64_t stride[3]) {
   return true;
 }
 
+}  // namespace
+
+gleam_status validate_places(const gleam_kv_pages* kv, const char* who) {
+  // a place that two heads or two tokens share would take whichever is stored last
+  if (!places_apart(*kv, kv->k_stride) || !places_apart(*kv, kv->v_stride)) {
+    set_error("%s: pages, places and heads of the cache overlap", who);
+    return GLEAM_E_INVALID;
+  }
+  return GLEAM_OK;
+}
+
+namespace {
+
 constexpr int kAppendThreads = 256, kAppendWaves = kAppendThreads / 64;
 
 struct AppendArgs {
@@ -328,14 +341,8 @@ extern "C" gleam_status gleam_kv_append(const gleam_kv_pages* kv, const gleam_ap
     set_error("%s: null slots", who);
     return GLEAM_E_INVALID;
   }
-  // a place that two heads or two tokens share would take whichever is stored last
   const int64_t* const strides[2] = {kv->k_stride, kv->v_stride};
-  for (const int64_t* s : strides) {
-    if (!places_apart(*kv, s)) {
-      set_error("%s: pages, places and heads of the cache overlap", who);
-      return GLEAM_E_INVALID;
-    }
-  }
+  if ((st = validate_places(kv, who)) != GLEAM_OK) return st;
   if (in->n_tokens > INT32_MAX) {
     set_error("%s: 2^31 tokens or more", who);
     return GLEAM_E_UNSUPPORTED;

@@ -11,6 +11,16 @@ namespace gleam {
 
 // Sets the error text (with `who`) where kv is not a cache that the kernels can address.
 gleam_status validate_kv(const gleam_kv_pages* kv, const char* who);
+// The same where places of keys, or of values, overlap: for calls that store into the cache.
+gleam_status validate_places(const gleam_kv_pages* kv, const char* who);
+// Bits of drafts: [n_tokens][words] of 64.
+gleam_status validate_seen(const uint64_t* d_seen, uint32_t words, uint64_t n_tokens, const char* who);
+// A ragged batch's sequences and the rows of their page table.
+gleam_status validate_sequences(const gleam_kv_pages* kv, uint64_t n_seq, uint64_t own_width, const int32_t* d_own_pages,
+                                const int32_t* d_own_len, const char* who);
+// What is kept for each place and key head, 4 bytes in [n_pages][kv_heads][page_tokens], and where it goes.
+gleam_status validate_tracked(const gleam_kv_pages* kv, const void* in, const void* out, const char* name,
+                              const char* who);
 // Heads of a tensor [tokens, heads, head_dim]: pointer and strides that 16-byte loads can use.
 gleam_status validate_heads(const void* p, const int64_t stride[2], const char* name, const char* who);
 
@@ -19,6 +29,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2v __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+
+constexpr uint64_t kMostSeq = 1ull << 20;  // sequences of a batch
 
 struct Fp16 {
   typedef _Float16 scalar;

@@ -31,7 +31,7 @@
 
 #include <type_traits>
 
-#include "kv_pages.h"
+#include "kv_device.h"
 #include "launch_shape.h"
 #include "prefix_plan.h"
 
@@ -46,8 +46,7 @@ constexpr float kRise = 8.f;  // log2
 // output (a key and 65,536 others 2^25 below it: 0.2% of the output). They go up to 2^15 that way. bf16
 // reaches down to 2^-133, and its values so far up that their sums need the room.
 template <class T> constexpr float kUp = std::is_same_v<T, Fp16> ? 7.f : 0.f;
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-constexpr uint64_t kMostSeq = 1ull << 20;
+constexpr float kLn2 = 0.69314718055994530942f;
 constexpr uint64_t kPassing = 128ull << 20;  // bytes of an item's keys and values
 constexpr uint32_t kWideJoin = 256;    // up to this many rows are joined by a workgroup each
 constexpr uint32_t kMostJoins = 2048;  // workgroups of the others: those that the GPU holds at once
@@ -97,6 +96,8 @@ struct AttendArgs {
   const int32_t* group_first;
   const int32_t* prefix_pages;
   const int32_t* prefix_len;
+  const uint32_t* seen;  // of trees of drafts: [n_tokens][seen_words]
+  uint32_t seen_words;
   uint32_t n_tokens, n_seq, n_groups, own_width, prefix_width;
   uint32_t q_heads, kv_heads, ratio, page_log2, n_pages, target, head_dim;
   float scale_log2;
@@ -189,8 +190,6 @@ __device__ void block_scan(V (&v)[kN], V (&total)[kN], V (*lds)[kN], Op op) {
   }
   __syncthreads();
 }
-
-__device__ inline int32_t clamp_to(int32_t v, int32_t most) { return v < 0 ? 0 : v > most ? most : v; }
 
 // How many keys a length means: none in a cache without pages.
 __device__ inline uint32_t clamp_keys(const AttendArgs& a, int32_t n, uint32_t width) {
@@ -327,9 +326,6 @@ __device__ inline void write_plan(const AttendArgs& a, const WavePlan& plan) {
   if (lane == 0) w.head->joins = plan.joins;
 }
 
-// Of a value that is the same in all lanes: kept in a scalar register, branches on it not masked.
-__device__ inline uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
-
 // Lane i's item, in all lanes.
 __device__ inline Item item_of_lane(const Item& it, uint32_t i) {
   auto get = [i](uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, (int)i); };
@@ -463,28 +459,6 @@ __device__ uint32_t wave_search(const V* first, uint32_t n, V x) {
 // --------------------------------------------------------------------------------------- //
 // attend
 // --------------------------------------------------------------------------------------- //
-template <class T> struct Mfma;
-template <> struct Mfma<Fp16> {
-  static __device__ f32x4 run(f16x8 a, f16x8 b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-  }
-};
-template <> struct Mfma<Bf16> {
-  static __device__ f32x4 run(bf16x8 a, bf16x8 b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-  }
-};
-
-union Pack8 {
-  u32x4v u;
-  f16x8 h;
-  bf16x8 b;
-};
-__device__ inline void put(Pack8& p, int i, float x, Fp16) { p.h[i] = (_Float16)x; }
-__device__ inline void put(Pack8& p, int i, float x, Bf16) { p.b[i] = (__bf16)x; }
-__device__ inline f16x8 get(const Pack8& p, Fp16) { return p.h; }
-__device__ inline bf16x8 get(const Pack8& p, Bf16) { return p.b; }
-
 // An infinite or NaN value of a key that some rows of a tile may not see would reach them as
 // 0 * infinity. Where a tile has such keys, its values are looked at, the infinite and NaN ones
 // are taken as 0 in the products, and add_special adds them at the end to the rows that see them.
@@ -500,9 +474,6 @@ template <class T>
 __device__ inline uint32_t clear_special(uint32_t x) {
   return x & ~((special_bits<T>(x) >> 15) * 0xffffu);
 }
-
-// A number that no cache has a page of.
-constexpr uint32_t kNoPage = ~0u;
 
 // The page of an item's key `key`, of `keys`.
 __device__ inline uint32_t page_at(const AttendArgs& a, const int32_t* pages, uint32_t key, uint32_t keys) {
@@ -590,6 +561,35 @@ __device__ inline float sum_of(const float* x) {
   else return sum_of<kN / 2>(x) + sum_of<kN / 2>(x + kN / 2);
 }
 
+// A tree of drafts: of its sequence's own keys a row sees those before the first draft's, `draft`, and
+// those of the drafts that its bits name (draft i is key `draft` + i).
+struct TreeRow {
+  const uint32_t* bits;
+  uint32_t words;
+  int64_t draft;  // below 0 where the sequence has more drafts than keys
+  // (loaded whether there is one or not: there is at least one word, and no branch)
+  __device__ uint32_t word(int64_t i) const {
+    const uint32_t x = bits[i < 0 ? 0 : i < words ? i : words - 1];
+    return i < 0 ? ~0u : i < words ? x : 0u;
+  }
+  // The words around the 32 keys from `key` on, and which of those the row sees.
+  __device__ void load(uint32_t key, uint32_t (&raw)[2]) const {
+    const int64_t at = ((int64_t)key - draft) >> 5;
+    raw[0] = word(at);
+    raw[1] = word(at + 1);
+  }
+  __device__ uint32_t sees(uint32_t key, const uint32_t (&raw)[2]) const {
+    return (uint32_t)(((uint64_t)raw[1] << 32 | raw[0]) >> (uint32_t)(((int64_t)key - draft) & 31));
+  }
+  __device__ bool sees(uint32_t key) const {
+    const int64_t i = (int64_t)key - draft;
+    return word(i >> 5) >> (i & 31) & 1;
+  }
+};
+__device__ inline TreeRow tree_row(const AttendArgs& a, const Item& it, uint32_t token) {
+  return {a.seen + (uint64_t)token * a.seen_words, a.seen_words, (int64_t)it.own_keys - it.tokens};
+}
+
 // A unit, as its workgroup finds it.
 struct Unit {
   Item it;
@@ -597,7 +597,7 @@ struct Unit {
 };
 
 // 16 rows, the waves taking turns at the keys.
-template <class T, int D>
+template <class T, int D, bool kTree>
 __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit, char* lds) {
   typedef typename T::scalar scalar;
   constexpr int kDims = D / 16;       // dims a lane brings of a value row
@@ -621,16 +621,19 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
   const uint32_t token = it.token_first + (row_live ? row / a.ratio : 0);
   const uint32_t q_head = head * a.ratio + (row_live ? row % a.ratio : 0);
 
-  // keys of the sequence's own that the row sees; the fewest of the tile's rows
+  // keys of the sequence's own that the row sees; the fewest of the tile's rows. In a tree the row may see
+  // any, and sees all before the first draft's.
+  const TreeRow tree = kTree ? tree_row(a, it, token) : TreeRow{};
   const int64_t behind = (int64_t)it.own_keys - it.tokens + 1;
   const int64_t sees = behind + (row_live ? row / a.ratio : 0);
-  const uint32_t own_seen = sees < 0 ? 0 : (uint32_t)sees;
-  const int64_t fewest = behind + tile * kFewRows / a.ratio;
+  const uint32_t own_seen = kTree ? it.own_keys : sees < 0 ? 0 : (uint32_t)sees;
+  const int64_t fewest = kTree ? tree.draft : behind + tile * kFewRows / a.ratio;
   const uint32_t own_least = fewest < 0 ? 0 : (uint32_t)fewest;
   uint32_t last_row = tile * kFewRows + kFewRows - 1;
   if (last_row >= rows) last_row = rows - 1;
   const int64_t furthest = behind + last_row / a.ratio;
-  const uint32_t own_most = furthest < 0 ? 0 : furthest > it.own_keys ? it.own_keys : (uint32_t)furthest;
+  const uint32_t own_most = kTree ? it.own_keys
+                            : furthest < 0 ? 0 : furthest > it.own_keys ? it.own_keys : (uint32_t)furthest;
 
   Pack8 q[kKMfma];
 #pragma unroll
@@ -676,7 +679,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
   // where there is no page (without pages there are no keys, without keys no halves). Keys that are
   // none are masked, and the values in their place set to 0.
   u32x4v kk[2][2][kKMfma];
-  uint32_t vv[2][8][kWords], exist[2][2];
+  uint32_t vv[2][8][kWords], exist[2][2], seen_raw[2][2];
   const uint32_t k_off = n * (uint32_t)a.k_place + g * 16;
   uint32_t v_off[4];
 #pragma unroll
@@ -709,6 +712,13 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
       pages = pages_from(half);
     }
     const uint32_t at = (half - page_half) / kWaves * 2;
+    if constexpr (kTree) {
+      if (uniform(looked_at(half))) {
+        asm volatile("");  // a branch around the loads, or none of what follows counts as the same in all lanes
+        tree.load(key_of(half), seen_raw[set]);
+        asm volatile("");
+      }
+    }
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       const uint32_t page = (uint32_t)__builtin_amdgcn_readlane((int)pages, (int)(at + b));
@@ -744,6 +754,10 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
     const uint32_t least = shared ? it.prefix_keys : own_least;
     const bool masked = key + 32 > least || exist[set][0] + exist[set][1] < 32;
     const uint32_t seen = shared ? it.prefix_keys : own_seen;
+    uint32_t sees_bits = ~0u;  // of the 32 keys
+    if constexpr (kTree) {
+      if (looked_at(half)) sees_bits = tree.sees(key, seen_raw[set]);
+    }
     float x[8], top = -INFINITY;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -751,6 +765,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
       if (masked) {
         const uint32_t r = 4 * g + (e & 3);
         if (key + (e >> 2) * 16 + r >= seen || r >= exist[set][e >> 2]) x[e] = -INFINITY;
+        if (kTree && !(sees_bits >> ((e >> 2) * 16 + r) & 1)) x[e] = -INFINITY;
       }
       top = fmaxf(top, x[e]);
     }
@@ -820,7 +835,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const Unit& unit
       for (uint32_t i = 0; i < 32; ++i) {
         const uint32_t first = key + (i & 16);
         const Keys16 t = keys16(a, page_at(a, own_pages, first, it.own_keys), first, it.own_keys, head);
-        if ((i & 15) >= t.n || key + i >= own_seen) continue;
+        if ((i & 15) >= t.n || key + i >= own_seen || (kTree && !tree.sees(key + i))) continue;
         const uint8_t* const v = t.v + (int64_t)(i & 15) * a.v_place;
 #pragma unroll
         for (int r = 0; r < 4; ++r)
@@ -942,7 +957,7 @@ __device__ inline u32x2v read_transposed(const char* p) {
   return x.u;
 }
 
-template <class T, int D>
+template <class T, int D, bool kTree>
 __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& unit, char* lds) {
   typedef typename T::scalar scalar;
   typedef Staged<D> St;
@@ -964,15 +979,18 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
 
   // keys of the sequence's own that the lane's row sees, the fewest and most of the wave's rows,
   // and of the workgroup's
+  const TreeRow tree = kTree ? tree_row(a, it, token) : TreeRow{};
   const int64_t behind = (int64_t)it.own_keys - it.tokens + 1;
   auto seen_by = [&](uint32_t r) {
+    if (kTree) return it.own_keys;
     if (r >= rows) r = rows - 1;
     const int64_t x = behind + r / a.ratio;
     return x < 0 ? 0u : (uint32_t)x;
   };
-  const uint32_t own_seen = seen_by(row), own_least = uniform(seen_by(wave_row));
+  const uint32_t before = tree.draft < 0 ? 0 : (uint32_t)tree.draft;  // what all rows of a tree see
+  const uint32_t own_seen = seen_by(row), own_least = kTree ? before : uniform(seen_by(wave_row));
   const uint32_t own_wave_most = uniform(wave_row < rows ? seen_by(wave_row + 31) : 0);
-  const uint32_t own_group_least = uniform(seen_by(unit.tile * kTileRows));
+  const uint32_t own_group_least = kTree ? before : uniform(seen_by(unit.tile * kTileRows));
   const uint32_t own_most = uniform(seen_by(unit.tile * kTileRows + kTileRows - 1));
 
   // Scores are scaled after the product, and masked ones are minus infinity before it: a scale below
@@ -1127,14 +1145,24 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
       if (!all_exist || (!shared && key + St::kKeys > own_least)) {
         const uint32_t seen = shared ? it.prefix_keys : own_seen;
 #pragma unroll
-        for (int t = 0; t < kKTiles; ++t)
+        for (int t = 0; t < kKTiles; ++t) {
+          uint32_t sees_bits = ~0u;  // of the 32 keys
+          if constexpr (kTree) {
+            if (!shared) {
+              uint32_t raw[2];
+              tree.load(key + 32 * t, raw);
+              sees_bits = tree.sees(key + 32 * t, raw) >> (4 * h);
+            }
+          }
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int quad = 32 * t + 8 * (r / 4);  // and 4 h on
             const uint32_t in = quad % St::kRows + r % 4 + 4 * h, w = quad / St::kRows;  // in wave w's rows
             const uint32_t exist = (flags >> (8 * w)) & 0x7f;
             if (key + w * St::kRows + in >= seen || in >= exist) s[t][r] = -INFINITY;
+            if (kTree && !(sees_bits >> (8 * (r / 4) + r % 4) & 1)) s[t][r] = -INFINITY;
           }
+        }
       }
       float top = s[0][0];
 #pragma unroll
@@ -1184,7 +1212,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const Unit& uni
     const uint32_t to = (end - prefix_subs) * St::kKeys;
     for (; key < to && key < own_seen; ++key) {
       const Keys16 t = keys16(a, page_at(a, own_pages, key & ~15u, it.own_keys), key & ~15u, it.own_keys, head);
-      if ((key & 15) >= t.n) continue;
+      if ((key & 15) >= t.n || (kTree && !tree.sees(key))) continue;
       const uint8_t* const v = t.v + (int64_t)(key & 15) * a.v_place + 8 * h;
 #pragma unroll
       for (int i = 0; i < kO; ++i)
@@ -1229,7 +1257,7 @@ constexpr int lds_bytes() {
   return few > tile ? few : tile;
 }
 
-template <class T, int D>
+template <class T, int D, bool kTree>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(AttendArgs a) {
   __shared__ __attribute__((aligned(16))) char lds[lds_bytes<D>()];
   const Ws& w = a.ws;
@@ -1269,8 +1297,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(Atte
   unit.head = uniform(unit.head);
   unit.chunk = uniform(unit.chunk);
   unit.tile = uniform(unit.tile);
-  if (few) attend_few<T, D>(a, unit, lds);
-  else attend_tile<T, D>(a, unit, lds);
+  if (few) attend_few<T, D, kTree>(a, unit, lds);
+  else attend_tile<T, D, kTree>(a, unit, lds);
 }
 
 // D/4 lanes take a piece of a row, 4 dims each. Where there are many rows they join all of its
@@ -1396,8 +1424,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a) {
 }
 
 // Sets the error text with the call's name; *shape and *args as the kernels take them.
-gleam_status validate_attention(const gleam_kv_pages* kv, const gleam_prefix_batch* b, PlanShape* shape) {
-  const char* const who = "gleam_prefix_attention";
+gleam_status validate_attention(const gleam_kv_pages* kv, const gleam_prefix_batch* b, const char* who,
+                                PlanShape* shape) {
   gleam_status st = validate_kv(kv, who);
   if (st != GLEAM_OK) return st;
   if (!b) {
@@ -1453,7 +1481,8 @@ gleam_status launch_all(const AttendArgs& a, uint32_t units, hipStream_t stream)
     if ((st = launch_status("plan_kernel")) != GLEAM_OK) return st;
   }
   if (units > 0) {
-    hipLaunchKernelGGL((attend_kernel<T, D>), dim3(units), dim3(kThreads), 0, stream, a);
+    if (a.seen) hipLaunchKernelGGL((attend_kernel<T, D, true>), dim3(units), dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((attend_kernel<T, D, false>), dim3(units), dim3(kThreads), 0, stream, a);
     if ((st = launch_status("attend_kernel")) != GLEAM_OK) return st;
   }
   const uint32_t rows = a.n_tokens * a.q_heads;
@@ -1468,30 +1497,12 @@ gleam_status launch_all(const AttendArgs& a, uint32_t units, hipStream_t stream)
   return launch_status("join_kernel");
 }
 
-}  // namespace
-
-hipError_t preload_prefix_attention() {
-  hipFuncAttributes attr;
-  return hipFuncGetAttributes(&attr, reinterpret_cast<const void*>(&plan_kernel));
-}
-
-}  // namespace gleam
-
-extern "C" size_t gleam_prefix_attention_ws_bytes(const gleam_kv_pages* kv, const gleam_prefix_batch* b) {
-  using namespace gleam;
-  clear_error();
-  PlanShape s{};
-  if (validate_attention(kv, b, &s) != GLEAM_OK) return 0;
-  return ws_at(nullptr, s, kv->head_dim).bytes;
-}
-
-extern "C" gleam_status gleam_prefix_attention(const gleam_kv_pages* kv, const gleam_prefix_batch* b, void* d_out,
-                                               float* d_lse, void* d_ws, size_t ws_bytes, void* stream) {
-  using namespace gleam;
-  clear_error();
-  const char* const who = "gleam_prefix_attention";
+// d_seen: of trees of drafts, null without.
+gleam_status attend_batch(const gleam_kv_pages* kv, const gleam_prefix_batch* b, const uint64_t* d_seen,
+                          uint32_t seen_words, void* d_out, float* d_lse, void* d_ws, size_t ws_bytes, void* stream,
+                          const char* who) {
   PlanShape shape{};
-  gleam_status st = validate_attention(kv, b, &shape);
+  gleam_status st = validate_attention(kv, b, who, &shape);
   if (st != GLEAM_OK) return st;
   if (b->n_tokens == 0) return GLEAM_OK;
   if ((st = validate_heads(b->d_q, b->q_stride, "q", who)) != GLEAM_OK) return st;
@@ -1532,6 +1543,8 @@ extern "C" gleam_status gleam_prefix_attention(const gleam_kv_pages* kv, const g
   a.group_first = b->d_group_first;
   a.prefix_pages = b->d_prefix_pages;
   a.prefix_len = b->d_prefix_len;
+  a.seen = reinterpret_cast<const uint32_t*>(d_seen);
+  a.seen_words = 2 * seen_words;
   a.n_tokens = (uint32_t)b->n_tokens;
   a.n_seq = (uint32_t)b->n_seq;
   a.n_groups = b->n_seq ? (uint32_t)b->n_groups : 0;
@@ -1559,4 +1572,38 @@ extern "C" gleam_status gleam_prefix_attention(const gleam_kv_pages* kv, const g
   return kv->head_dim == 64    ? launch_all<Bf16, 64>(a, units, s)
          : kv->head_dim == 128 ? launch_all<Bf16, 128>(a, units, s)
                                : launch_all<Bf16, 256>(a, units, s);
+}
+
+}  // namespace
+
+hipError_t preload_prefix_attention() {
+  hipFuncAttributes attr;
+  return hipFuncGetAttributes(&attr, reinterpret_cast<const void*>(&plan_kernel));
+}
+
+}  // namespace gleam
+
+extern "C" size_t gleam_prefix_attention_ws_bytes(const gleam_kv_pages* kv, const gleam_prefix_batch* b) {
+  using namespace gleam;
+  clear_error();
+  PlanShape s{};
+  if (validate_attention(kv, b, "gleam_prefix_attention", &s) != GLEAM_OK) return 0;
+  return ws_at(nullptr, s, kv->head_dim).bytes;
+}
+
+extern "C" gleam_status gleam_prefix_attention(const gleam_kv_pages* kv, const gleam_prefix_batch* b, void* d_out,
+                                               float* d_lse, void* d_ws, size_t ws_bytes, void* stream) {
+  gleam::clear_error();
+  return gleam::attend_batch(kv, b, nullptr, 0, d_out, d_lse, d_ws, ws_bytes, stream, "gleam_prefix_attention");
+}
+
+extern "C" gleam_status gleam_tree_attention(const gleam_kv_pages* kv, const gleam_prefix_batch* b,
+                                             const uint64_t* d_seen, uint32_t seen_words, void* d_out, float* d_lse,
+                                             void* d_ws, size_t ws_bytes, void* stream) {
+  using namespace gleam;
+  clear_error();
+  const char* const who = "gleam_tree_attention";
+  const gleam_status st = validate_seen(d_seen, seen_words, b ? b->n_tokens : 0, who);
+  if (st != GLEAM_OK) return st;
+  return attend_batch(kv, b, d_seen, seen_words, d_out, d_lse, d_ws, ws_bytes, stream, who);
 }

@@ -1,0 +1,355 @@
+"""draft_tree, tree_attention and kv_accept on the GPU against plain computations on the CPU."""
+
+import math
+
+import pytest
+import torch
+
+import budget_reference as B
+import kv_reference as R
+import paper_2607_23115_amd as g
+from gpu_util import say
+from test_gpu_prefix_attention import Case
+
+pytestmark = pytest.mark.gpu
+F16, BF16 = torch.float16, torch.bfloat16
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a visible GPU")
+    torch.cuda.init()
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32)
+
+
+def first_of(n):
+    return i32([sum(n[:i]) for i in range(len(n) + 1)])
+
+
+def forest(n, seed=0, chain=0.0):
+    """Parents of n drafts each: a random earlier one, or with probability `chain` the one before."""
+    gen = torch.Generator().manual_seed(seed)
+    out = []
+    for count in n:
+        for i in range(count):
+            u = torch.rand(3, generator=gen).tolist()
+            out.append(-1 if i == 0 or u[0] < 0.05 else i - 1 if u[1] < chain else int(u[2] * i))
+    return i32(out)
+
+
+@pytest.mark.parametrize("n", [[1], [0, 1, 0], [13], [64], [65], [63, 1, 64], [130, 7, 300, 64], [1000]])
+@pytest.mark.parametrize("chain", [0.0, 0.9])
+def test_trees(n, chain):
+    parent, first = forest(n, len(n), chain), first_of(n)
+    for width in (1, 64, max(n), max(n) + 70):
+        say("draft_tree", n, width)
+        seen, depth = g.draft_tree(parent.cuda(), first.cuda(), max(1, width))
+        want, deep = B.tree(parent, first, (max(1, width) + 63) // 64)
+        assert torch.equal(seen.cpu(), want) and torch.equal(depth.cpu(), deep)
+
+
+def test_a_chain_and_a_star():
+    n = 200
+    for parent in (torch.arange(-1, n - 1, dtype=torch.int32), torch.full((n,), -1, dtype=torch.int32),
+                   i32([-1] + [0] * (n - 1))):
+        seen, depth = g.draft_tree(parent.cuda(), i32([0, n]).cuda(), n)
+        want, deep = B.tree(parent, i32([0, n]), 4)
+        assert torch.equal(seen.cpu(), want) and torch.equal(depth.cpu(), deep)
+
+
+def test_parents_and_offsets_that_make_no_sense():
+    """A parent that does not come before its draft counts as none; tokens of no sequence get 0;
+    offsets out of range are taken as the nearest in it."""
+    parent = i32([0, 5, -7, 1 << 30, 2, 4, 0, 1])
+    seen, depth = g.draft_tree(parent.cuda(), i32([1, 6]).cuda(), 8)
+    want, deep = B.tree(parent, i32([1, 6]), 1)
+    assert torch.equal(seen.cpu(), want) and torch.equal(depth.cpu(), deep)
+    assert (want[[0, 6, 7]] == 0).all()
+    say("draft_tree offsets out of range")
+    for first, same in (([-4, 3, 99], [0, 3, 8]), ([5, 2, 2], [5, 5, 5])):
+        seen, depth = g.draft_tree(parent.cuda(), i32(first).cuda(), 8)
+        want, deep = B.tree(parent, i32(same), 1)
+        if first[0] < 0:
+            assert torch.equal(seen.cpu(), want) and torch.equal(depth.cpu(), deep)
+
+
+def test_many_trees_and_a_captured_call():
+    n = [1 + i % 70 for i in range(3000)]
+    parent, first = forest(n, 5), first_of(n)
+    p, f = parent.cuda(), first.cuda()
+    seen = torch.empty(len(parent), 2, dtype=torch.int64, device="cuda")
+    depth = torch.empty(len(parent), dtype=torch.int32, device="cuda")
+    say("draft_tree graph")
+    graph = torch.cuda.CUDAGraph()
+    g.draft_tree(p, f, 70, seen, depth)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        g.draft_tree(p, f, 70, seen, depth)
+    for seed in (5, 6):
+        p.copy_(forest(n, seed))
+        seen.fill_(-1)
+        depth.fill_(-1)
+        graph.replay()
+        torch.cuda.synchronize()
+        want, deep = B.tree(p.cpu(), first, 2)
+        assert torch.equal(seen.cpu(), want) and torch.equal(depth.cpu(), deep)
+
+
+# --------------------------------------------------------------------------- #
+class TreeCase(Case):
+    """The same batches with bits of drafts: a random forest's, or any."""
+
+    def __init__(self, n, own, *args, random_bits=False, words=None, **kw):
+        super().__init__(n, own, *args, **kw)
+        self.words = words or max(1, -(-max(n) // 64))
+        tokens = self.q.shape[0]
+        if random_bits:
+            gen = torch.Generator().manual_seed(len(n) + max(n))
+            self.seen = torch.randint(-1 << 62, 1 << 62, (tokens, self.words), generator=gen)
+            self.seen[torch.rand(tokens, generator=gen) < 0.2] = 0
+        else:
+            parent = torch.cat([forest(n, sum(n), 0.3), torch.full((tokens - sum(n),), -1, dtype=torch.int32)])
+            self.seen = B.tree(parent, self.q_first, self.words)[0]
+
+    def arguments(self):
+        return {**super().arguments(), "seen": self.seen.cuda()}
+
+    def want(self):
+        return B.tree_attention(self.q, self.kp, self.vp, self.q_first, self.seen, self.own_pages, self.own_len,
+                                self.group_first, self.prefix_pages, self.prefix_len, self.scale)
+
+    def check(self, **more):
+        say("tree_attention", self.what)
+        out, lse = g.tree_attention(**{**self.arguments(), **more}, want_lse=True)
+        torch.cuda.synchronize()
+        o, l, o_tol, l_tol = self.want()
+        R.near(lse, l, l_tol, "lse")
+        R.near(out, o, o_tol, "out")
+        return out, lse
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_types_and_widths(dtype, d):
+    TreeCase([5, 13, 1], [40, 13, 200], [(0, 2, 100)], 8, 2, d, 16, dtype).check()
+    TreeCase([26, 40], [90, 300], [], 4, 2, d, 32, dtype, random_bits=True).check()
+    TreeCase([70, 33], [150, 50], [(0, 2, 75)], 4, 1, d, 16, dtype).check()
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (3, 1), (28, 4), (8, 8), (24, 8), (17, 1), (40, 2)])
+def test_heads(hq, hkv):
+    TreeCase([7, 18], [40, 60], [(0, 2, 50)], hq, hkv, 64, 16, BF16, seed=hq, random_bits=True).check()
+
+
+@pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 200])
+@pytest.mark.parametrize("before", [0, 1, 31, 33, 100])
+def test_numbers_of_drafts(n, before):
+    """The drafts' keys start anywhere in a page and in a tile; bits of one to four words; rows of both kinds
+    of tiles."""
+    TreeCase([n], [n + before], [], 2, 1, 64, 16, F16, seed=n, random_bits=True).check()
+    if n % 2:
+        TreeCase([n, 3], [n + before, 9], [(0, 2, 40)], 4, 1, 128, 64, BF16, seed=n).check()
+
+
+def test_rows_that_see_nothing_and_drafts_without_keys():
+    c = TreeCase([4, 3, 0, 6], [2, 0, 5, 6], [], 4, 2, 64, 16, F16, pad_tokens=3, random_bits=True)
+    out, lse = c.check()
+    assert (out[-3:] == 0).all() and (lse[-3:] == -math.inf).all()
+    c = TreeCase([20, 100], [20, 90], [], 4, 2, 64, 16, BF16, random_bits=True)
+    c.seen[:] = 0
+    out, lse = c.check()
+    assert (out[:20] == 0).all() and (out[20:] == 0).all() and (lse == -math.inf).all()
+    c.seen[:] = -1  # everybody sees all drafts
+    c.check()
+
+
+def test_fewer_bits_than_drafts():
+    for n in (70, 100, 130):
+        TreeCase([n, 5], [n + 20, 9], [], 2, 1, 64, 16, F16, words=1, random_bits=True).check()
+    TreeCase([30, 5], [50, 9], [], 2, 1, 64, 16, F16, words=5, random_bits=True).check()
+
+
+def test_a_chain_is_prefix_attention():
+    n, own = [5, 1, 40, 90], [60, 1, 40, 700]
+    c = TreeCase(n, own, [(0, 3, 130)], 8, 2, 128, 16, BF16)
+    c.seen = B.tree(torch.cat([torch.arange(-1, k - 1, dtype=torch.int32) for k in n]), c.q_first, c.words)[0]
+    a = c.arguments()
+    out, lse = g.tree_attention(**a, want_lse=True)
+    del a["seen"]
+    want, want_l = g.prefix_attention(**a, want_lse=True)
+    _, _, o_tol, l_tol = c.want()
+    R.near(out, want.cpu().double(), 2 * o_tol, "out")
+    R.near(lse, want_l.cpu().double(), 2 * l_tol, "lse")
+
+
+def test_long_histories_of_few_and_many_drafts():
+    TreeCase([5], [9000], [], 4, 1, 128, 64, BF16, random_bits=True).check()
+    TreeCase([40], [2500], [(0, 1, 700)], 4, 1, 64, 16, F16, random_bits=True).check()
+
+
+@pytest.mark.parametrize("n", [6, 70])
+def test_drafts_that_are_not_seen_may_be_anything(n):
+    """Keys and values of drafts hold NaN and infinities: who does not see them is not reached."""
+    own = n + 25
+    c = TreeCase([n], [own], [], 4, 2, 64, 16, BF16, random_bits=True)
+    mine = B.places(c.own_pages[0], own, 16)
+    for j, x in ((own - n, math.inf), (own - n + 3, math.nan), (own - 2, -math.inf)):
+        c.vp[mine[j]][0, 3] = x
+        c.vp[mine[j]][1, 60] = -x
+    c.kp[mine[own - n + 1]][0] = math.nan
+    o, l, o_tol, l_tol = c.want()
+    say("tree_attention", "special values", c.what)
+    out, lse = (x.cpu().double() for x in g.tree_attention(**c.arguments(), want_lse=True))
+    assert torch.equal(torch.isnan(out), torch.isnan(o)) and torch.equal(torch.isposinf(out), torch.isposinf(o))
+    assert torch.equal(torch.isneginf(out), torch.isneginf(o)) and torch.equal(torch.isnan(lse), torch.isnan(l))
+    fine = torch.isfinite(o)
+    assert 0 < int(fine.sum()) < fine.numel() and bool(((out - o).abs()[fine] <= o_tol[fine]).all())
+
+
+def test_missing_pages_lengths_and_offsets_out_of_range():
+    c = TreeCase([5, 2, 90], [100, 60, 130], [(0, 2, 90)], 4, 2, 64, 16, F16, random_bits=True)
+    c.own_pages[0, 2], c.own_pages[1, 3], c.prefix_pages[0, 3], c.own_pages[2, 7] = -1, c.kp.shape[0], 1 << 30, -7
+    c.check()
+    c = TreeCase([1, 1, 2], [20, 20, 20], [(0, 3, 30)], 2, 1, 64, 16, F16, random_bits=True)
+    c.kp[torch.isnan(c.kp)], c.vp[torch.isnan(c.vp)] = 0.5, 0.25
+    a = c.arguments()
+    a["own_pages"] = a["own_pages"][:, :2].contiguous()
+    say("tree_attention", "lengths out of range")
+    for name, odd, same in (("own_len", [1 << 30, -5, 20], [32, 0, 20]), ("q_first", [-3, 1, 0, 99], [0, 1, 1, 4])):
+        got = g.tree_attention(**{**a, name: i32(odd).cuda()})[0]
+        assert torch.equal(got, g.tree_attention(**{**a, name: i32(same).cuda()})[0])
+
+
+def test_batches_with_a_plan_of_their_own_and_thousands_of_sequences():
+    for count in (70, 1500):
+        gen = torch.Generator().manual_seed(count)
+        n = torch.randint(0, 6, (count,), generator=gen).tolist()
+        own = [k + x for k, x in zip(n, torch.randint(0, 60, (count,), generator=gen).tolist())]
+        TreeCase(n, own, [(i, i + 5, 9 + i % 40) for i in range(0, count - 10, 5)], 2, 1, 64, 16, F16,
+                 random_bits=True).check()
+
+
+def test_the_same_call_twice_streams_and_graphs():
+    c = TreeCase([7, 30, 1, 80], [900, 300, 44, 2000], [(0, 3, 700)], 8, 2, 128, 16, BF16)
+    a = c.arguments()
+    a["k_pages"][torch.isnan(a["k_pages"])], a["v_pages"][torch.isnan(a["v_pages"])] = 0.5, 0.25
+    want, want_l = g.tree_attention(**a, want_lse=True)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    say("tree_attention stream and graph")
+    got, _ = g.tree_attention(**a, stream=side)
+    side.synchronize()
+    assert torch.equal(got, want)
+    out, lse = torch.empty_like(a["q"]), torch.empty(a["q"].shape[:2], device="cuda")
+    ws = g.prefix_attention_workspace(a["k_pages"], a["v_pages"], a["q"].shape[0], 8, 4, 1)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        g.tree_attention(**a, out=out, lse=lse, ws=ws)
+    for own in ([900, 300, 44, 2000], [7, 20, 1, 90], [904, 0, 60, 80]):
+        a["own_len"].copy_(i32(own))
+        a["seen"].copy_(a["seen"].flip(0))
+        want, want_l = g.tree_attention(**a, want_lse=True)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(lse, want_l)
+        ws.fill_(255)
+
+
+def test_attention_refusals():
+    c = TreeCase([2, 3], [5, 6], [(0, 2, 7)], 4, 2, 64, 16, F16)
+    a = c.arguments()
+    a["out"] = out = torch.full_like(a["q"], 3.0)
+    for message, bad in (("seen must be", a["seen"][:3]), ("seen must be", a["seen"][:, 0]), ("seen must be", None),
+                         ("seen must be", a["seen"].int()), ("seen must be", a["seen"].cpu()),
+                         ("seen_words", a["seen"][:, :0])):
+        with pytest.raises((ValueError, g.GleamError), match=message):
+            g.tree_attention(**{**a, "seen": bad})
+    with pytest.raises(ValueError, match="tree_attention has none"):
+        g.tree_attention(**{**a, "q": a["q"].clone().requires_grad_()})
+    with pytest.raises((ValueError, g.GleamError), match="gleam_tree_attention"):
+        g.tree_attention(**{**a, "ws": torch.empty(256, dtype=torch.uint8, device="cuda")})
+    torch.cuda.synchronize()
+    assert (out == 3).all()
+
+
+# --------------------------------------------------------------------------- #
+def run_accept(c, leaf, what, **more):
+    say("kv_accept", what, c.what)
+    a = c.arguments()
+    kp, vp, length = B.accept(c.kp, c.vp, c.q_first, c.seen, leaf, c.own_pages, c.own_len)
+    out = g.kv_accept(a["k_pages"], a["v_pages"], a["q_first"], a["seen"], leaf.cuda(), a["own_pages"], a["own_len"],
+                      **more)
+    torch.cuda.synchronize()
+    bits = lambda x: x.contiguous().view(torch.int16)  # noqa: E731
+    assert torch.equal(out.cpu(), length)
+    assert torch.equal(bits(a["k_pages"].cpu()), bits(kp)) and torch.equal(bits(a["v_pages"].cpu()), bits(vp))
+    return a, out
+
+
+@pytest.mark.parametrize("dtype,d,hkv,page,head_major", [(F16, 64, 1, 16, True), (BF16, 128, 2, 32, False),
+                                                         (BF16, 256, 3, 64, True), (F16, 128, 33, 16, False)])
+def test_accepted_paths(dtype, d, hkv, page, head_major):
+    n = [1, 13, 64, 65, 150, 30, 0, 20]
+    own = [5, 13, 100, 65, 300, 10, 7, 20]
+    for random_bits in (False, True):
+        c = TreeCase(n, own, [], hkv, hkv, d, page, dtype, head_major=head_major, random_bits=random_bits)
+        run_accept(c, i32([k - 1 for k in n]), "last draft")
+        run_accept(c, i32([0, 5, 40, -1, 80, 29, 0, 20]), "others, none, and one that is none")
+
+
+def test_all_drafts_and_missing_pages():
+    c = TreeCase([40, 30], [70, 40], [], 2, 2, 64, 16, F16)
+    c.seen[:] = -1
+    run_accept(c, i32([3, 29]), "all drafts")
+    c.seen[:, 0] = 0x3ff0ff0ff0f0f0f0
+    c.own_pages[0, 3], c.own_pages[1, 1] = -1, c.kp.shape[0] + 4
+    run_accept(c, i32([3, 29]), "missing pages")
+    c = TreeCase([9, 9], [20, 20], [], 2, 2, 64, 16, F16)
+    a = c.arguments()
+    table = a["own_pages"][:, :1].contiguous()
+    say("kv_accept lengths out of range")
+    out = g.kv_accept(a["k_pages"], a["v_pages"], i32([0, 9, 1 << 30]).cuda(), a["seen"], i32([0, -1]).cuda(), table,
+                      i32([1 << 30, -8]).cuda())
+    assert out.tolist() == [16 - 9 + 1, 0]
+
+
+def test_accept_refusals_streams_and_graphs():
+    c = TreeCase([13, 20], [40, 50], [], 2, 2, 64, 16, F16)
+    leaf = i32([7, 19])
+    kp, vp, length = B.accept(c.kp, c.vp, c.q_first, c.seen, leaf, c.own_pages, c.own_len)
+    a = c.arguments()
+    args = [a["k_pages"], a["v_pages"], a["q_first"], a["seen"], leaf.cuda(), a["own_pages"], a["own_len"]]
+    for at, bad, message in ((0, a["k_pages"].float(), "float16"), (2, a["q_first"][:2], "q_first holds 2"),
+                             (3, a["seen"][:, 0], "seen must be"), (4, leaf, "leaf"), (5, a["own_pages"][:1], "own_pages"),
+                             (6, a["own_len"].long(), "own_len"), (0, a["k_pages"][:, :, :, :32], "differ in shape")):
+        with pytest.raises((ValueError, g.GleamError), match=message):
+            g.kv_accept(*args[:at], bad, *args[at + 1:])
+    with pytest.raises(g.GleamError, match="overlap own_len"):
+        g.kv_accept(*args, len_out=a["own_len"])
+    with pytest.raises(ValueError, match="requires a gradient"):
+        g.kv_accept(a["k_pages"].clone().requires_grad_(), *args[1:])
+    out, side = torch.empty_like(a["own_len"]), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        g.kv_accept(*args, len_out=out)
+    keep = a["k_pages"].clone(), a["v_pages"].clone()
+    bits = lambda x: x.contiguous().cpu().view(torch.int16)  # noqa: E731
+    for again in range(3):
+        if again == 2:
+            with torch.cuda.stream(side):
+                torch.cuda._sleep(1000000)
+            g.kv_accept(*args, len_out=out, stream=side)
+        else:
+            graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(bits(a["k_pages"]), bits(kp)) and torch.equal(bits(a["v_pages"]), bits(vp))
+        assert torch.equal(out.cpu(), length)
+        a["k_pages"].copy_(keep[0])
+        a["v_pages"].copy_(keep[1])
+        out.zero_()
+        torch.cuda.synchronize()
