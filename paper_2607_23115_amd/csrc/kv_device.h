@@ -15,6 +15,66 @@ __device__ inline uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdg
 // A number that no cache has a page of.
 constexpr uint32_t kNoPage = ~0u;
 
+// What is at a base that is the same in all lanes and the lane's own offset, added by the load;
+// kOnce: what nobody reads again soon is not kept in the caches.
+template <class V, bool kOnce = false>
+__device__ inline V load_at(const uint8_t* base, uint32_t offset) {
+  uint64_t x = reinterpret_cast<uint64_t>(base);
+  asm("" : "+s"(x));  // kept apart from the offset
+  typedef const __attribute__((address_space(1))) uint8_t* Global;
+  const auto* p = reinterpret_cast<const __attribute__((address_space(1))) V*>(reinterpret_cast<Global>(x) + offset);
+  return kOnce ? __builtin_nontemporal_load(p) : *p;
+}
+
+struct SumOp {
+  template <class V> __device__ V operator()(V a, V b) const { return a + b; }
+};
+struct MaxOp {
+  template <class V> __device__ V operator()(V a, V b) const { return a > b ? a : b; }
+};
+
+// The value that a DPP control brings to each lane, `none` where it brings nothing.
+template <int kCtrl, int kRows>
+__device__ inline uint32_t dpp(uint32_t v, uint32_t none) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, kCtrl, kRows, 0xf, false);
+}
+template <int kCtrl, int kRows>
+__device__ inline int32_t dpp(int32_t v, int32_t none) {
+  return __builtin_amdgcn_update_dpp(none, v, kCtrl, kRows, 0xf, false);
+}
+template <int kCtrl, int kRows>
+__device__ inline uint64_t dpp(uint64_t v, uint64_t none) {
+  return (uint64_t)dpp<kCtrl, kRows>((uint32_t)(v >> 32), (uint32_t)(none >> 32)) << 32 |
+         dpp<kCtrl, kRows>((uint32_t)v, (uint32_t)none);
+}
+
+// Inclusive scan over a wave of values that 0 leaves as they are: shifts by 1, 2, 4 and 8 within
+// rows of 16 lanes, then the last lanes of rows 0 and 2 to the rows after them, then lane 31 to
+// the upper half.
+template <class V, class Op>
+__device__ V wave_scan(V v, Op op) {
+  v = op(dpp<0x111, 0xf>(v, (V)0), v);
+  v = op(dpp<0x112, 0xf>(v, (V)0), v);
+  v = op(dpp<0x114, 0xf>(v, (V)0), v);
+  v = op(dpp<0x118, 0xf>(v, (V)0), v);
+  v = op(dpp<0x142, 0xa>(v, (V)0), v);
+  v = op(dpp<0x143, 0xc>(v, (V)0), v);
+  return v;
+}
+
+// Memory behind an address that is the same in all lanes, or none: loads from none give 0 and go nowhere, so that
+// a loop can ask for what it may not need without a branch.
+typedef __amdgpu_buffer_rsrc_t Window;
+__device__ inline Window window(const uint8_t* base, bool there) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, (int)uniform(there ? ~0u : 0u), 0x00020000);
+}
+// 16 bytes at the lane's offset and one that is the same in all lanes; kOnce: what nobody reads again soon is not
+// kept in the caches.
+template <bool kOnce>
+__device__ inline u32x4v load_from(Window w, uint32_t lane_offset, uint32_t offset) {
+  return __builtin_amdgcn_raw_buffer_load_b128(w, (int)lane_offset, (int)offset, kOnce ? 2 : 0);
+}
+
 // Products of 16 x 32 by 32 x 16 values.
 template <class T> struct Mfma;
 template <> struct Mfma<Fp16> {

@@ -2,11 +2,16 @@
 // head of the key's head) that see it of exp(scale q.k - lse), lse the row's log sum of exponentials from
 // the attention itself.
 //
-// A key's sum needs no other key, so keys are cut into units of any size and nothing is joined afterwards:
-// a wave holds 64 keys in registers (of heads of 256, 32) as the row operand of v_mfma_f32_16x16x32, S^T = K
-// Q^T, and walks 16 rows at a time; a lane keeps the sums of its scores' keys, and the 16 lanes of the same
-// keys add theirs up at the end. With few rows the time is that of reading the keys, with many that of the
-// products and the exponentials.
+// A key's sum needs no other key, so the keys are cut anywhere and nothing is joined afterwards. S^T = K Q^T by
+// v_mfma_f32_16x16x32, 16 rows at a time: a lane gets one row's scores with four keys of 16, keeps the sums of
+// its keys' exponentials, and the 16 lanes of the same keys add theirs up at the end.
+//   few rows   a wave for itself streams through 32 keys at a time, the next 32 on their way during the
+//              products. All halves of 64 keys of all sequences and heads are dealt out evenly, in order, so
+//              that lengths do not matter. The time is that of reading the keys.
+//   many rows  a workgroup keeps 64 keys (of heads of 256, 32) in registers, the same in all waves, and these
+//              share the rows. The time is that of the products and the exponentials.
+
+#include <type_traits>
 
 #include "kv_device.h"
 #include "launch_shape.h"
@@ -14,10 +19,10 @@
 namespace gleam {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr uint32_t kRows = 16;          // rows of a tile
-constexpr uint32_t kSplitTiles = 8;     // from this many tiles on a workgroup's waves share keys and split the rows
-constexpr uint32_t kMostGroups = 512;   // workgroups: two a CU
+constexpr uint32_t kRows = 16;        // rows of a tile
+constexpr uint32_t kSplitTiles = 8;   // from this many tiles on the rows are shared by a workgroup's waves
+constexpr uint32_t kGroups = 256;     // workgroups: one a CU, and as many waves in it as its registers hold
+template <int D> constexpr int kWaves = D == 256 ? 4 : 8;
 
 struct WeighArgs {
   const uint8_t* q;
@@ -37,197 +42,460 @@ struct WeighArgs {
   float scale_log2;
 };
 
-// A sequence as a workgroup finds it.
+// A sequence as a wave finds it: of its keys, units of the two kinds for each head.
 struct Seq {
   uint32_t first, tokens, keys;
-  uint32_t units;  // a head's
+  uint32_t blocks;  // many rows: of kBlock keys
+  uint32_t halves;  // few rows: of 32 keys
 };
 
-// The keys of a unit: a wave's own 64 for each wave, or the same 64 for all.
-template <int D> constexpr uint32_t kWaveKeys = D == 256 ? 32 : 64;
-
-__device__ inline bool splits_rows(uint32_t tokens, uint32_t ratio) {
-  return (uint64_t)tokens * ratio > kRows * (kSplitTiles - 1);
-}
+template <int D> constexpr uint32_t kBlock = D == 256 ? 32 : 64;
 
 template <int D>
 __device__ inline Seq seq_at(const WeighArgs& a, uint32_t s) {
   Seq r{};
+  if (s >= a.n_seq) return r;
   const uint32_t first = (uint32_t)clamp_to(a.q_first[s], (int32_t)a.n_tokens);
   const uint32_t end = (uint32_t)clamp_to(a.q_first[s + 1], (int32_t)a.n_tokens);
   r.first = first;
   r.tokens = end > first ? end - first : 0;
   r.keys = a.n_pages ? (uint32_t)clamp_to(a.own_len[s], (int32_t)(a.own_width << a.page_log2)) : 0;
-  const uint32_t per = splits_rows(r.tokens, a.ratio) ? kWaveKeys<D> : kWaves * kWaveKeys<D>;
-  r.units = (r.keys + per - 1) / per;
+  if ((uint64_t)r.tokens * a.ratio > kRows * (kSplitTiles - 1)) r.blocks = (r.keys + kBlock<D> - 1) / kBlock<D>;
+  else r.halves = (r.keys + 31) / 32;
   return r;
 }
 
-// The value that the lane `by` further on among the same 16 has, going round.
+__device__ inline Seq of_lane(const Seq& s, uint32_t i) {
+  auto get = [i](uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, (int)i); };
+  return {get(s.first), get(s.tokens), get(s.keys), get(s.blocks), get(s.halves)};
+}
+
+// The value that the lane kBy further on among the same 16 has, going round.
 template <int kBy>
 __device__ inline float turned(float x) {
   return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x120 + kBy, 0xf, 0xf, false));
 }
+__device__ inline float sum_of_16(float x) {
+  x += turned<8>(x);
+  x += turned<4>(x);
+  x += turned<2>(x);
+  return x + turned<1>(x);
+}
 
-template <class T, int D>
-__device__ __forceinline__ void weigh_unit(const WeighArgs& a, const Seq& seq, uint32_t s, uint32_t head, uint32_t unit,
-                                           float (*lds)[64]) {
-  constexpr uint32_t kKeys = kWaveKeys<D>;
-  constexpr int kTiles = kKeys / 16, kSteps = D / 32;
-  const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-  const uint32_t n = lane & 15, g = lane >> 4;
-  const bool split = splits_rows(seq.tokens, a.ratio);
-  const uint32_t key0 = (split ? unit : unit * kWaves + wave) * kKeys;
-  const int64_t base = (int64_t)seq.keys - seq.tokens;  // the first new token's key
-  // the lane's own key, whose sum it stores: 4 g + its place among four of the 16 keys that n / 4 names
-  const uint32_t own = key0 + 16 * (n >> 2) + 4 * g + (n & 3);
-  const bool has = (n >> 2) < kTiles && own < seq.keys;
-  const int32_t* const pages = a.own_pages + (uint64_t)s * a.own_width;
-  const uint32_t page = has ? (uint32_t)pages[own >> a.page_log2] : kNoPage;
-  const uint32_t place_mask = (1u << a.page_log2) - 1;
+// What is added for the lane's four keys of 16 from `key` on to the sums of `acc`. seen: how many keys the
+// lane's row sees; masked: whether that matters to any row.
+__device__ inline void add_weights(const f32x4& score, float scale, float down, bool masked, uint32_t key, uint32_t seen,
+                                   float (&acc)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float p = __builtin_amdgcn_exp2f(fmaf(score[e], scale, down));
+    acc[e] += masked && key + e >= seen ? 0.f : p;
+  }
+}
 
-  if (key0 < seq.keys) {
-    Pack8 k[kTiles][kSteps];
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-      // 16 keys lie in one page; those that are none are of page 0, and their sums are not stored
-      uint32_t p = (uint32_t)__builtin_amdgcn_readlane((int)page, 4 * t);
-      if (p >= a.n_pages) p = 0;
-      const uint8_t* const at = a.k + (int64_t)p * a.k_page + (int64_t)((key0 + 16 * t) & place_mask) * a.k_place +
-                                (int64_t)head * a.k_head + n * a.k_place + g * 16;
-#pragma unroll
-      for (int i = 0; i < kSteps; ++i) k[t][i].u = *reinterpret_cast<const u32x4v*>(at + i * 64);
-    }
-    const bool stored = has && page < a.n_pages;
-    const uint64_t to = ((uint64_t)page * a.kv_heads + head) << a.page_log2 | (own & place_mask);
-    float sum = 0.f;
-    const bool is_new = own >= base;
-    if (stored && !is_new && !(split && wave > 0)) sum = a.weights[to];
+// How many keys a row sees: none where there is no such row.
+__device__ inline uint32_t seen_by(const WeighArgs& a, const Seq& seq, uint32_t row) {
+  const int64_t sees = (int64_t)seq.keys - seq.tokens + row / a.ratio + 1;
+  return row < seq.tokens * a.ratio && sees > 0 ? (uint32_t)sees : 0;
+}
 
-    float acc[kTiles][4];
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[t][e] = 0.f;
-    // the first row that sees the first key
-    const uint32_t rows = seq.tokens * a.ratio;
-    const uint32_t row_least = key0 <= base ? 0 : (uint32_t)(key0 - base) * a.ratio;
-    const uint32_t step = split ? kWaves * kRows : kRows;
-    const uint32_t step_tokens = step / a.ratio, step_rest = step % a.ratio;
-    uint32_t row0 = row_least / kRows * kRows + (split ? wave * kRows : 0);
-    uint32_t token = (row0 + n) / a.ratio, in_head = (row0 + n) % a.ratio;
+// Waits for a value here: where a branch may have asked for it, whatever uses it behind the branch would wait
+// for all loads, the keys on their way among them.
+template <class V>
+__device__ inline void arrived(V& x) {
+  asm volatile("" : "+v"(x));
+}
 
-    Pack8 q[kSteps];
-    float bias;
-    auto load = [&]() {
-      const bool live = row0 + n < rows;
-      const uint64_t t = seq.first + (live ? token : 0), h = head * a.ratio + in_head;
-      const uint8_t* const at = a.q + t * a.q_token + h * a.q_head + g * 16;
+// Rows are loaded whole, and pass through LDS into the products' layout: loads of 64 bytes of 16 rows, straight
+// into it, take the caches four times as many accesses (keys read 15% slower, queries bound many rows).
+template <int D>
+struct Staged {
+  static constexpr uint32_t kPieces = D / 8, kLoadRows = 64 / kPieces;  // 16-byte pieces of a row, rows of a load
+  static constexpr int kLoads = 16 / kLoadRows;                         // of 16 rows
+  static constexpr uint32_t kTile = 16 * 2 * D;                         // bytes of 16 rows
+  static constexpr uint32_t kBytes = 2 * kTile;                         // of a wave
+  // rows of one piece each, or of one row all pieces, fall into different banks
+  static __device__ uint32_t at(uint32_t row, uint32_t piece) {
+    return row * (2 * D) + ((piece ^ (D == 64 ? (row >> 1) & 7 : row & 15)) << 4);
+  }
+  // What the lane loads of 16 rows goes to row load_row() + i * kLoadRows, piece().
+  static __device__ uint32_t load_row() { return (threadIdx.x & 63) / kPieces; }
+  static __device__ uint32_t piece() { return (threadIdx.x & 63) % kPieces; }
+  static __device__ void store(char* lds, const u32x4v (&x)[kLoads]) {
 #pragma unroll
-      for (int i = 0; i < kSteps; ++i) q[i].u = *reinterpret_cast<const u32x4v*>(at + i * 64);
-      bias = a.lse[t * a.q_heads + h];
+    for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4v*>(lds + at(i * kLoadRows + load_row(), piece())) = x[i];
+  }
+  // The 32 dims from 32 i on of a row, a lane's eight; from: at(row, lane / 16).
+  static __device__ Pack8 read(const char* lds, uint32_t from, int i) {
+    Pack8 x;
+    x.u = *reinterpret_cast<const u32x4v*>(lds + (from ^ (i << 6)));
+    return x;
+  }
+};
+
+// Rows of a sequence and key head, 16 a tile, on their way.
+template <int D>
+struct Rows {
+  static constexpr int kLoads = Staged<D>::kLoads;
+  u32x4v q[kLoads];
+  float lse;  // of row lane % 16
+  const uint8_t* at[kLoads];
+  const float* lse_at;
+
+  // From row `row` on; rows that there are not are the last one again.
+  __device__ void find(const WeighArgs& a, const Seq& seq, uint32_t head, uint32_t row) {
+    const uint32_t last = seq.tokens * a.ratio - 1;
+    auto of = [&](uint32_t r, uint64_t* h) {
+      if (r > last) r = last;
+      *h = head * a.ratio + r % a.ratio;
+      return seq.first + (uint64_t)(r / a.ratio);
     };
-    if (row0 < rows) load();
-    while (row0 < rows) {
-      f32x4 score[kTiles];
+    uint64_t h;
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t) {
-        score[t] = (f32x4)0.f;
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) score[t] = Mfma<T>::run(get(k[t][i], T()), get(q[i], T()), score[t]);
-      }
-      const float down = -bias * kLog2e;
-      const uint32_t row = row0 + n;
-      // keys that the row sees: those before this one
-      const int64_t seen = row < rows ? base + token + 1 : 0;
-      // whether some row of the tile is none, or must not see some key
-      const bool masked = row0 + kRows > rows || row0 < ((int64_t)key0 + kKeys - 1 - base) * a.ratio;
-      row0 += step;
-      token += step_tokens;
-      in_head += step_rest;
-      if (in_head >= a.ratio) {
-        in_head -= a.ratio;
-        ++token;
-      }
-      if (row0 < rows) load();
-      if (masked) {
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float p = __builtin_amdgcn_exp2f(fmaf(score[t][e], a.scale_log2, down));
-            acc[t][e] += (int64_t)(key0 + 16 * t + 4 * g + e) < seen ? p : 0.f;
-          }
-      } else {
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[t][e] += __builtin_amdgcn_exp2f(fmaf(score[t][e], a.scale_log2, down));
-      }
+    for (int i = 0; i < kLoads; ++i) {
+      const uint64_t t = of(row + i * Staged<D>::kLoadRows + Staged<D>::load_row(), &h);
+      at[i] = a.q + t * a.q_token + h * a.q_head + Staged<D>::piece() * 16;
     }
-    float mine = 0.f;
+    const uint64_t t = of(row + (threadIdx.x & 15), &h);
+    lse_at = a.lse + t * a.q_heads + h;
+  }
+  __device__ void step_back(int64_t q_bytes, int64_t lses) {
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t)
+    for (int i = 0; i < kLoads; ++i) at[i] -= q_bytes;
+    lse_at -= lses;
+  }
+  __device__ void load() {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) q[i] = *reinterpret_cast<const u32x4v*>(at[i]);
+    lse = *lse_at;
+  }
+  __device__ void wait() {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) arrived(q[i]);
+    arrived(lse);
+  }
+};
+
+// --------------------------------------------------------------------------------------- //
+// few rows
+// --------------------------------------------------------------------------------------- //
+// Halves [from, to) of a sequence and head. lds: the wave's own.
+template <class T, int D>
+__device__ __forceinline__ void weigh_few(const WeighArgs& a, const Seq& seq, uint32_t s, uint32_t head, uint32_t from,
+                                          uint32_t to, char* lds) {
+  typedef Staged<D> St;
+  constexpr int kLoads = St::kLoads;
+  constexpr int kSteps = D / 32;
+  const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int64_t base = (int64_t)seq.keys - seq.tokens;  // the first new token's key
+  const uint32_t rows = seq.tokens * a.ratio, tiles = (rows + kRows - 1) / kRows;
+  const uint32_t place_mask = (1u << a.page_log2) - 1;
+  const int32_t* const pages = a.own_pages + (uint64_t)s * a.own_width;
+  const uint8_t* const k_head = a.k + (int64_t)head * a.k_head;
+  // which of the 32 keys' sums the lane stores (n < 8): of four keys of 16 those that it has scores of
+  const uint32_t mine = 16 * (n >> 2) + 4 * g + (n & 3);
+
+  // the rows of a tile, in the products' layout
+  Rows<D> r;
+  Pack8 q[kSteps];
+  uint32_t seen = 0;  // keys that the lane's row sees
+  float down = 0.f;
+  const uint32_t from_lds = St::at(n, g);
+  auto take_rows = [&](uint32_t tile) {
+    r.find(a, seq, head, kRows * tile);
+    r.load();
+    St::store(lds + St::kTile, r.q);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) q[i] = St::read(lds + St::kTile, from_lds, i);
+    down = -r.lse * kLog2e;
+    seen = seen_by(a, seq, kRows * tile + n);
+  };
+  if (tiles == 1) take_rows(0);
+
+  // pages of 16 keys each, 64 of them ahead, a lane each
+  auto pages_from = [&](uint32_t half) {
+    const uint32_t key = 32 * half + 16 * lane;
+    return key < seq.keys && key < 32 * to ? (uint32_t)pages[key >> a.page_log2] : kNoPage;
+  };
+  uint32_t page_half = from, ahead = pages_from(from);
+  u32x4v kk[2][2][kLoads];
+  const uint32_t k_off = St::load_row() * (uint32_t)a.k_place + St::piece() * 16;
+  typedef std::integral_constant<int, 0> Even;
+  typedef std::integral_constant<int, 1> Odd;
+  uint64_t at[2];
+  float old[2];
+  // Asks for the keys; returns where the lane's sum goes.
+  auto load = [&](uint32_t half, auto set_) -> uint64_t {
+    constexpr int set = decltype(set_)::value;
+    if (half - page_half >= 32) {
+      page_half = half;
+      ahead = pages_from(half);
+      arrived(ahead);
+    }
+    uint32_t p[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      p[b] = (uint32_t)__builtin_amdgcn_readlane((int)ahead, (int)(2 * (half - page_half) + b));
+      // 16 keys lie in one page
+      const Window k = window(k_head + (int64_t)p[b] * a.k_page + (int64_t)((32 * half + 16 * b) & place_mask) * a.k_place,
+                              p[b] < a.n_pages);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        kk[set][b][i] = load_from<true>(k, k_off, (uint32_t)(i * St::kLoadRows) * (uint32_t)a.k_place);
+    }
+    const uint32_t key = 32 * half + mine, page = n < 4 ? p[0] : p[1];
+    return n < 8 && key < seq.keys && page < a.n_pages
+               ? ((uint64_t)page * a.kv_heads + head) << a.page_log2 | (key & place_mask) : ~0ull;
+  };
+  auto load_old = [&](uint64_t to_at, auto set_) {
+    constexpr int set = decltype(set_)::value;
+    at[set] = to_at;
+    old[set] = a.weights[to_at != ~0ull ? to_at : 0];
+  };
+  // Both sets are on their way most of the time: a set is asked for again as soon as it is in LDS.
+  auto add = [&](uint32_t half, auto set_) {
+    constexpr int set = decltype(set_)::value;
+    float acc[2][4] = {};
+    uint64_t next;
+    auto products = [&](const char* keys, int b) {
+      f32x4 score = (f32x4)0.f;
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) score = Mfma<T>::run(get(St::read(keys, from_lds, i), T()), get(q[i], T()), score);
+      add_weights(score, a.scale_log2, down, true, 32 * half + 16 * b + 4 * g, seen, acc[b]);
+    };
+    if (tiles == 1) {
+      St::store(lds, kk[set][0]);
+      St::store(lds + St::kTile, kk[set][1]);
+      next = load(half + 2, set_);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) products(lds + b * St::kTile, b);
+    } else {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        St::store(lds, kk[set][b]);
+        for (uint32_t t = 0; t < tiles; ++t) {
+          take_rows(t);
+          products(lds, b);
+        }
+      }
+      next = load(half + 2, set_);
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        float x = acc[t][e];
-        x += turned<8>(x);
-        x += turned<4>(x);
-        x += turned<2>(x);
-        x += turned<1>(x);
-        if (n == 4 * t + e) mine = x;
+        const float x = sum_of_16(acc[b][e]);
+        if (n == 4 * b + e) sum = x;
       }
-    if (split) {
-      lds[wave][lane] = mine;
-      __syncthreads();
-      mine = lds[0][lane] + lds[1][lane] + (lds[2][lane] + lds[3][lane]);
-      __syncthreads();
+    const int64_t young = (int64_t)(32 * half + mine) - base;
+    sum += young < 0 ? old[set] : 0.f;
+    if (at[set] != ~0ull) {
+      a.weights_out[at[set]] = sum;
+      if (a.born && young >= 0) a.born[at[set]] = a.positions[seq.first + (uint32_t)young];
     }
-    if (stored && !(split && wave > 0)) {
-      a.weights_out[to] = sum + mine;
-      if (is_new && a.born) a.born[to] = a.positions[seq.first + (uint32_t)(own - base)];
-    }
+    load_old(next, set_);
+  };
+  typedef std::integral_constant<int, 0> Even;
+  typedef std::integral_constant<int, 1> Odd;
+  // No load is in a branch that does not wait for it, as every use behind the branch would wait for all loads:
+  // halves behind the last have no pages, and are asked for in vain.
+  arrived(ahead);
+  load_old(load(from, Even()), Even());
+  load_old(load(from + 1, Odd()), Odd());
+  for (uint32_t half = from; half < to; half += 2) {
+    add(half, Even());
+    if (half + 1 < to) add(half + 1, Odd());
   }
 }
 
-// Workgroups take units in turn, so that the first ones of a prompt, which most rows see, go out first and
-// to different CUs. Each finds its own by walking over the sequences' lengths, 64 a step.
+// --------------------------------------------------------------------------------------- //
+// many rows
+// --------------------------------------------------------------------------------------- //
 template <class T, int D>
-__global__ __launch_bounds__(kThreads, 2) void weigh_kernel(WeighArgs a) {
-  __shared__ float lds[kWaves][64];
-  const uint32_t lane = threadIdx.x & 63;
-  uint64_t before = 0;  // units of the sequences that were walked over
-  uint64_t u = blockIdx.x;
-  for (uint32_t s0 = 0; s0 < a.n_seq; s0 += 64) {
-    Seq mine{};
-    if (s0 + lane < a.n_seq) mine = seq_at<D>(a, s0 + lane);
-    uint64_t upto = (uint64_t)mine.units * a.kv_heads;  // inclusive sum over the lanes
+__device__ __forceinline__ void weigh_many(const WeighArgs& a, const Seq& seq, uint32_t s, uint32_t head, uint32_t block,
+                                           char* lds) {
+  typedef Staged<D> St;
+  constexpr int kTiles = kBlock<D> / 16, kSteps = D / 32;
+  const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const uint32_t n = lane & 15, g = lane >> 4;
+  const uint32_t key0 = block * kBlock<D>;
+  const int64_t base = (int64_t)seq.keys - seq.tokens;
+  // the lane's own key, whose sum it stores: of 16 keys those four that it has scores of
+  const uint32_t own = key0 + 16 * (n >> 2) + 4 * g + (n & 3);
+  const bool has = (n >> 2) < kTiles && own < seq.keys;
+  const uint32_t page = has ? (uint32_t)a.own_pages[(uint64_t)s * a.own_width + (own >> a.page_log2)] : kNoPage;
+  const uint32_t place_mask = (1u << a.page_log2) - 1;
+  Pack8 k[kTiles][kSteps];
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const uint64_t x = __shfl_up(upto, d, 64);
-      if ((int)lane >= d) upto += x;
+  for (int t = 0; t < kTiles; ++t) {
+    uint32_t p = (uint32_t)__builtin_amdgcn_readlane((int)page, 4 * t);
+    if (p >= a.n_pages) p = 0;  // not stored
+    const uint8_t* const at = a.k + (int64_t)p * a.k_page + (int64_t)((key0 + 16 * t) & place_mask) * a.k_place +
+                              (int64_t)head * a.k_head + n * a.k_place + g * 16;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) k[t][i].u = *reinterpret_cast<const u32x4v*>(at + i * 64);
+  }
+  float acc[kTiles][4] = {};
+  const uint32_t rows = seq.tokens * a.ratio;
+  // the first row that sees the first key, and from where on all see all keys
+  const uint32_t row_least = key0 <= base ? 0 : (uint32_t)(key0 - base) * a.ratio;
+  const int64_t row_all = ((int64_t)key0 + kBlock<D> - 1 - base) * a.ratio;
+  // From the last rows to the first that see a key: all blocks of a head that run at a time read the same
+  // queries then, from the caches. A wave's tiles are kWaves<D> apart, two are on their way. Where the rows of
+  // two such tiles are whole tokens, each lane only steps back over those.
+  const int64_t tile_least = row_least / kRows;
+  int64_t tile = (int64_t)((rows - 1) / kRows) - wave;
+  constexpr uint32_t kBack = 2 * kWaves<D> * kRows;
+  const bool whole = kBack % a.ratio == 0;
+  const int64_t back_q = kBack / a.ratio * a.q_token, back_lse = (int64_t)(kBack / a.ratio) * a.q_heads;
+  char* const mine = lds + wave * St::kTile;
+  const uint32_t from_lds = St::at(n, g);
+  Rows<D> r[2];
+  auto add = [&](auto set_) {
+    constexpr int set = decltype(set_)::value;
+    St::store(mine, r[set].q);
+    const float down = -r[set].lse * kLog2e;
+    if (tile >= 2 * kWaves<D>) {  // otherwise the same again, in vain
+      if (whole) r[set].step_back(back_q, back_lse);
+      else r[set].find(a, seq, head, (uint32_t)(tile - 2 * kWaves<D>) * kRows);
     }
-    const uint64_t all = __shfl(upto, 63, 64);
-    for (; u < before + all; u += gridDim.x) {
-      const uint32_t i = (uint32_t)__builtin_ctzll(__ballot(upto > u - before));
-      Seq seq;
-      seq.first = (uint32_t)__builtin_amdgcn_readlane((int)mine.first, (int)i);
-      seq.tokens = (uint32_t)__builtin_amdgcn_readlane((int)mine.tokens, (int)i);
-      seq.keys = (uint32_t)__builtin_amdgcn_readlane((int)mine.keys, (int)i);
-      seq.units = (uint32_t)__builtin_amdgcn_readlane((int)mine.units, (int)i);
-      const uint64_t end = __shfl(upto, (int)i, 64);
-      const uint32_t in = uniform((uint32_t)(u - before - (end - (uint64_t)seq.units * a.kv_heads)));
-      weigh_unit<T, D>(a, seq, s0 + i, in % a.kv_heads, in / a.kv_heads, lds);
+    r[set].load();
+    f32x4 score[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) score[t] = (f32x4)0.f;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const Pack8 q = St::read(mine, from_lds, i);
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) score[t] = Mfma<T>::run(get(k[t][i], T()), get(q, T()), score[t]);
     }
-    before += all;
+    const int64_t row0 = tile * kRows;
+    if (row0 + kRows > rows || row0 < row_all) {
+      const uint32_t seen = seen_by(a, seq, (uint32_t)row0 + n);
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+        add_weights(score[t], a.scale_log2, down, true, key0 + 16 * t + 4 * g, seen, acc[t]);
+    } else {
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) add_weights(score[t], a.scale_log2, down, false, 0, 0, acc[t]);
+    }
+    tile -= kWaves<D>;
+  };
+  typedef std::integral_constant<int, 0> Even;
+  typedef std::integral_constant<int, 1> Odd;
+  if (tile >= tile_least) {
+    // The last tile may have fewer rows than 16: it is found again where steps go back from it.
+    r[0].find(a, seq, head, (uint32_t)tile * kRows);
+    r[0].load();
+    r[1].find(a, seq, head, (uint32_t)(tile >= kWaves<D> ? tile - kWaves<D> : 0) * kRows);
+    r[1].load();
+    if (tile >= 2 * kWaves<D>) {
+      r[0].find(a, seq, head, (uint32_t)(tile - 2 * kWaves<D>) * kRows);
+      r[0].step_back(-back_q, -back_lse);
+    }
+  }
+  while (tile >= tile_least) {
+    add(Even());
+    if (tile >= tile_least) add(Odd());
+  }
+  float sum = 0.f;
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float x = sum_of_16(acc[t][e]);
+      if (n == 4 * t + e) sum = x;
+    }
+  float(*const sums)[64] = reinterpret_cast<float(*)[64]>(lds + kWaves<D> * St::kTile);
+  sums[wave][lane] = sum;
+  __syncthreads();
+  if (wave == 0 && has && page < a.n_pages) {
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves<D>; ++w) sum += sums[w][lane];
+    const uint64_t to = ((uint64_t)page * a.kv_heads + head) << a.page_log2 | (own & place_mask);
+    if (own < base) sum += a.weights[to];
+    a.weights_out[to] = sum;
+    if (a.born && own >= base) a.born[to] = a.positions[seq.first + (uint32_t)(own - base)];
+  }
+  __syncthreads();
+}
+
+// Each wave finds its work by walking over the sequences' lengths, 64 a step.
+template <class T, int D>
+__global__ __launch_bounds__(64 * kWaves<D>) void weigh_kernel(WeighArgs a) {
+  __shared__ __attribute__((aligned(16))) char lds[kWaves<D> * Staged<D>::kBytes];
+  const uint32_t lane = threadIdx.x & 63;
+  uint64_t blocks = 0, halves = 0;
+  Seq mine{};
+  uint64_t upto_blocks = 0, upto_halves = 0;
+  for (uint32_t s0 = 0; s0 < a.n_seq; s0 += 64) {
+    mine = seq_at<D>(a, s0 + lane);
+    upto_blocks = wave_scan((uint64_t)mine.blocks * a.kv_heads, SumOp());
+    upto_halves = wave_scan((uint64_t)mine.halves * a.kv_heads, SumOp());
+    blocks += __shfl(upto_blocks, 63, 64);
+    halves += __shfl(upto_halves, 63, 64);
+  }
+  const bool one_step = a.n_seq <= 64;  // what was found still is at hand
+
+  if (blocks) {
+    // A prompt's first keys are seen by the most rows. Every other round goes the other way round, so that who
+    // has the longest of one gets the shortest of the next.
+    uint64_t round = 0, before = 0;
+    auto unit_of = [&](uint64_t r) {
+      return r * gridDim.x + (r & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+    };
+    for (uint32_t s0 = 0; s0 < a.n_seq; s0 += 64) {
+      if (!one_step) {
+        mine = seq_at<D>(a, s0 + lane);
+        upto_blocks = wave_scan((uint64_t)mine.blocks * a.kv_heads, SumOp());
+      }
+      const uint64_t all = __shfl(upto_blocks, 63, 64);
+      for (uint64_t u; (u = unit_of(round)) < before + all; ++round) {
+        const uint32_t i = uniform((uint32_t)__builtin_ctzll(__ballot(upto_blocks > u - before)));
+        const Seq seq = of_lane(mine, i);
+        const uint64_t end = __shfl(upto_blocks, (int)i, 64);
+        const uint32_t at = uniform((uint32_t)(u - before - (end - (uint64_t)seq.blocks * a.kv_heads)));
+        const uint32_t block = uniform(at / a.kv_heads);
+        weigh_many<T, D>(a, seq, s0 + i, at - block * a.kv_heads, block, lds);
+      }
+      before += all;
+    }
+  }
+  if (halves) {
+    const uint64_t waves = (uint64_t)gridDim.x * kWaves<D>, wave = (uint64_t)blockIdx.x * kWaves<D> + uniform(threadIdx.x >> 6);
+    uint64_t from = halves * wave / waves, before = 0;
+    const uint64_t to = halves * (wave + 1) / waves;
+    for (uint32_t s0 = 0; s0 < a.n_seq && from < to; s0 += 64) {
+      if (!one_step) {
+        mine = seq_at<D>(a, s0 + lane);
+        upto_halves = wave_scan((uint64_t)mine.halves * a.kv_heads, SumOp());
+      }
+      const uint64_t all = __shfl(upto_halves, 63, 64);
+      while (from < to && from < before + all) {
+        const uint32_t i = uniform((uint32_t)__builtin_ctzll(__ballot(upto_halves > from - before)));
+        const Seq seq = of_lane(mine, i);
+        const uint64_t end = __shfl(upto_halves, (int)i, 64);
+        const uint32_t at = uniform((uint32_t)(from - before - (end - (uint64_t)seq.halves * a.kv_heads)));
+        const uint32_t head = uniform(at / seq.halves), half = at - head * seq.halves;
+        uint32_t last = seq.halves;
+        if (to - from < last - half) last = half + (uint32_t)(to - from);
+        last = uniform(last);
+        weigh_few<T, D>(a, seq, s0 + i, head, half, last, lds + uniform(threadIdx.x >> 6) * Staged<D>::kBytes);
+        from += last - half;
+      }
+      before += all;
+    }
   }
 }
 
-template <class T>
-void launch_weigh(const WeighArgs& a, uint32_t head_dim, uint32_t groups, hipStream_t s) {
-  if (head_dim == 64) hipLaunchKernelGGL((weigh_kernel<T, 64>), dim3(groups), dim3(kThreads), 0, s, a);
-  else if (head_dim == 128) hipLaunchKernelGGL((weigh_kernel<T, 128>), dim3(groups), dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL((weigh_kernel<T, 256>), dim3(groups), dim3(kThreads), 0, s, a);
+template <class T, int D>
+void launch_weigh(const WeighArgs& a, uint64_t halves, hipStream_t s) {
+  // no more than there may be with work, where each takes two halves of many rows
+  const uint64_t groups = (halves + 1) / 2;
+  const uint32_t n = (uint32_t)(groups < kGroups ? groups : kGroups);
+  hipLaunchKernelGGL((weigh_kernel<T, D>), dim3(n), dim3(64 * kWaves<D>), 0, s, a);
 }
 
 }  // namespace
@@ -267,6 +535,10 @@ extern "C" gleam_status gleam_kv_weigh(const gleam_kv_pages* kv, const gleam_wei
   if (in->q_heads == 0 || in->q_heads % kv->kv_heads != 0 || in->q_heads > 65535) {
     set_error("%s: q_heads must be a multiple of kv_heads, up to 65535", who);
     return GLEAM_E_INVALID;
+  }
+  if (kv->k_stride[1] >= 1 << 26) {  // places of 16 keys are reached by 32-bit offsets
+    set_error("%s: places of a page 2^26 elements apart or more", who);
+    return GLEAM_E_UNSUPPORTED;
   }
   if (in->n_tokens > (uint64_t)INT32_MAX / in->q_heads) {
     set_error("%s: n_tokens * q_heads of 2^31 or more", who);
@@ -310,11 +582,16 @@ extern "C" gleam_status gleam_kv_weigh(const gleam_kv_pages* kv, const gleam_wei
   a.page_log2 = (uint32_t)log2_exact(kv->page_tokens);
   a.n_pages = (uint32_t)kv->n_pages;
   a.scale_log2 = in->scale * kLog2e;
-  // no more than there are units of the smallest kind
-  const uint64_t keys = in->own_width * kv->page_tokens;
-  const uint64_t units = in->n_seq * kv->kv_heads * ((keys + 31) / 32);
-  const uint32_t groups = (uint32_t)(units < kMostGroups ? units : kMostGroups);
-  if (kv->dtype == GLEAM_FP16) launch_weigh<Fp16>(a, kv->head_dim, groups, (hipStream_t)stream);
-  else launch_weigh<Bf16>(a, kv->head_dim, groups, (hipStream_t)stream);
+  const uint64_t halves = in->n_seq * kv->kv_heads * ((in->own_width * kv->page_tokens + 31) / 32);
+  hipStream_t s = (hipStream_t)stream;
+  if (kv->dtype == GLEAM_FP16) {
+    kv->head_dim == 64    ? launch_weigh<Fp16, 64>(a, halves, s)
+    : kv->head_dim == 128 ? launch_weigh<Fp16, 128>(a, halves, s)
+                          : launch_weigh<Fp16, 256>(a, halves, s);
+  } else {
+    kv->head_dim == 64    ? launch_weigh<Bf16, 64>(a, halves, s)
+    : kv->head_dim == 128 ? launch_weigh<Bf16, 128>(a, halves, s)
+                          : launch_weigh<Bf16, 256>(a, halves, s);
+  }
   return launch_status("weigh_kernel");
 }

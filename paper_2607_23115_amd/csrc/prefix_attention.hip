@@ -131,42 +131,6 @@ Ws ws_at(uint8_t* base, const PlanShape& s, uint32_t head_dim) {
 // --------------------------------------------------------------------------------------- //
 // plan
 // --------------------------------------------------------------------------------------- //
-struct SumOp {
-  template <class V> __device__ V operator()(V a, V b) const { return a + b; }
-};
-struct MaxOp {
-  template <class V> __device__ V operator()(V a, V b) const { return a > b ? a : b; }
-};
-
-// The value that a DPP control brings to each lane, `none` where it brings nothing.
-template <int kCtrl, int kRows>
-__device__ inline uint32_t dpp(uint32_t v, uint32_t none) {
-  return (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, kCtrl, kRows, 0xf, false);
-}
-template <int kCtrl, int kRows>
-__device__ inline int32_t dpp(int32_t v, int32_t none) {
-  return __builtin_amdgcn_update_dpp(none, v, kCtrl, kRows, 0xf, false);
-}
-template <int kCtrl, int kRows>
-__device__ inline uint64_t dpp(uint64_t v, uint64_t none) {
-  return (uint64_t)dpp<kCtrl, kRows>((uint32_t)(v >> 32), (uint32_t)(none >> 32)) << 32 |
-         dpp<kCtrl, kRows>((uint32_t)v, (uint32_t)none);
-}
-
-// Inclusive scan over a wave of values that 0 leaves as they are: shifts by 1, 2, 4 and 8 within
-// rows of 16 lanes, then the last lanes of rows 0 and 2 to the rows after them, then lane 31 to
-// the upper half.
-template <class V, class Op>
-__device__ V wave_scan(V v, Op op) {
-  v = op(dpp<0x111, 0xf>(v, (V)0), v);
-  v = op(dpp<0x112, 0xf>(v, (V)0), v);
-  v = op(dpp<0x114, 0xf>(v, (V)0), v);
-  v = op(dpp<0x118, 0xf>(v, (V)0), v);
-  v = op(dpp<0x142, 0xa>(v, (V)0), v);
-  v = op(dpp<0x143, 0xc>(v, (V)0), v);
-  return v;
-}
-
 // The same over the workgroup, of kN values at once (two barriers); every thread calls it. `total`
 // gets the last values.
 template <int kN, class V, class Op>
@@ -495,17 +459,6 @@ __device__ inline Keys16 keys16(const AttendArgs& a, uint32_t page, uint32_t key
   t.v = a.v + (int64_t)page * a.v_page + (int64_t)place * a.v_place + (int64_t)head * a.v_head;
   t.n = keys - key < 16 ? keys - key : 16;
   return t;
-}
-
-// What is at a base that is the same in all lanes and the lane's own offset, added by the load;
-// kOnce: what nobody reads again soon is not kept in the caches.
-template <class V, bool kOnce = false>
-__device__ inline V load_at(const uint8_t* base, uint32_t offset) {
-  uint64_t x = reinterpret_cast<uint64_t>(base);
-  asm("" : "+s"(x));  // kept apart from the offset
-  typedef const __attribute__((address_space(1))) uint8_t* Global;
-  const auto* p = reinterpret_cast<const __attribute__((address_space(1))) V*>(reinterpret_cast<Global>(x) + offset);
-  return kOnce ? __builtin_nontemporal_load(p) : *p;
 }
 
 // Calls add(i, value) for kN values, with 0 in the place of finite ones.
