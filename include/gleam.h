@@ -811,7 +811,7 @@ gleam_status gleam_kv_accept(const gleam_kv_pages* kv, const gleam_accept* a, vo
  * must be in one place of the table only.
  *   d_weights_out, d_born_out  may be d_weights and d_born themselves, and must not overlap them otherwise;
  *                    written for the first `keep` keys of each sequence
- *   d_len_out        may be d_own_len
+ *   d_len_out        must not overlap d_own_len (other layers' caches still need that)
  *   d_ws             device, 256-byte aligned, >= gleam_kv_evict_ws_bytes(kv, e)
  * Errors: GLEAM_E_INVALID, GLEAM_E_WORKSPACE, GLEAM_E_UNSUPPORTED (more than 2^20 sequences, 2^31 sequences
  * times heads, or 2^36 keys that may move), GLEAM_E_HIP. gleam_kv_evict_ws_bytes returns 0 for arguments

@@ -1285,7 +1285,8 @@ def kv_evict(k_pages: torch.Tensor, v_pages: torch.Tensor, own_pages: torch.Tens
     the tokens that each sequence has had. Keys born before `sinks`, or in the last `recent` of the
     total, are kept first, then those of the largest weights; kept keys from place `keep` on move
     into the places before it that come free, weights and births with them (in weights and born
-    themselves where weights_out and born_out are not given). ws: from kv_evict_workspace()."""
+    themselves where weights_out and born_out are not given). len_out int32: not own_len itself, other
+    layers' caches still need that. ws: from kv_evict_workspace()."""
     kv = _kv_struct(k_pages, v_pages)
     dev, i32, f32 = k_pages.get_device(), torch.int32, torch.float32
     pages_at, width, len_at, n_seq = _ragged(own_pages, own_len, dev)

@@ -7,10 +7,12 @@
 // places within it that come free, the i-th such key into the i-th such place. A sequence a few tokens over
 // its budget moves a few keys, not all of them, and no place that is read is written.
 //
-// select_kernel, a workgroup for each sequence and head: weights as integers in their order, the weight of
-// the last key kept found in three rounds of counting 11, 11 and 10 bits, then two running counts in the
-// keys' order: of the keys of just that weight, to keep the first ones, and of places that come free and
-// keys that move. move_kernel copies the pairs.
+// A workgroup chooses for each sequence and head: weights become integers of the same order, that of the last
+// key kept is found in four rounds of counting eight bits, then two running counts in the keys' order: of the
+// keys of just that weight, to keep the first ones (unless all are kept), and of places that come free and keys
+// that move. Where there are many sequences and heads, the workgroup also copies its pairs; with few,
+// move_kernel does, over all CUs. A chain of short steps that wait for each other; loops are kept rolled, as
+// each instruction runs a few times only and a CU has to fetch it first.
 
 #include "kv_device.h"
 #include "launch_shape.h"
@@ -19,11 +21,15 @@ namespace gleam {
 namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
+// Keys of a thread, in LDS: for tables of up to 4,096 keys, and for wider ones. Longer sequences than those
+// hold read their weights again for each count.
+constexpr int kNarrowKeys = 4, kWideKeys = 32;
+constexpr uint32_t kBins = 256;
 constexpr int kMoveThreads = 256;
-constexpr uint32_t kBins = 2048;
-// Weights of up to this many keys are kept in LDS between the rounds; of more they are read again.
-constexpr uint32_t kLdsKeys = 32768;
 constexpr uint32_t kMoveGroups = 2048;  // of move_kernel
+constexpr uint64_t kMostPairs = 1ull << 36;
+// From this many sequences times heads on a narrow table's workgroups copy their pairs themselves.
+constexpr uint32_t kManyPairs = 128;
 
 struct EvictArgs {
   uint8_t* base[2];  // keys, values
@@ -39,8 +45,8 @@ struct EvictArgs {
   uint32_t* moves;  // [n_seq][kv_heads]
   uint2* pairs;     // [n_seq][kv_heads][most]: the place a key leaves and the one that it goes to
   uint32_t most;
+  uint32_t copies;  // select_kernel copies the pairs
   uint32_t n_seq, own_width, page_log2, n_pages, kv_heads, keep, sinks, recent;
-  uint32_t lds_keys;
 };
 
 __device__ inline uint32_t keys_of(const EvictArgs& a, uint32_t s) {
@@ -60,29 +66,111 @@ __device__ inline uint32_t order_of(float w) {
   return w != w ? 0 : b ^ ((b >> 31) ? ~0u : 0x80000000u);
 }
 
-// Of key i; ~0 for one that is kept whatever its weight.
-__device__ inline uint32_t rank_of(const EvictArgs& a, const int32_t* pages, uint32_t head, uint32_t i, int64_t late) {
-  const uint64_t at = tracked_at(a, pages, head, i);
-  if (at == ~0ull) return 0;
-  const float w = a.weights[at];
-  const int64_t born = a.born[at];
-  return born < (int64_t)a.sinks || born >= late ? ~0u : order_of(w);
+// What a key counts for: ~0 for one that is kept whatever its weight.
+__device__ inline uint32_t rank_of(const EvictArgs& a, float w, int32_t born, int64_t late) {
+  return (int64_t)born < (int64_t)a.sinks || (int64_t)born >= late ? ~0u : order_of(w);
+}
+
+// Copies pairs number first, first + step ..., kAhead of them at a time. D / 8 lanes copy a key, as many its
+// value, 16 bytes each; the first of them what is kept about it. pair(m): places from and to.
+// pages: the sequence's, in memory or LDS.
+template <int D, int kAhead, class Page, class Pair>
+__device__ inline void copy_pairs(const EvictArgs& a, const Page* pages, uint32_t head, uint32_t moves, uint32_t group,
+                                  uint32_t groups, const Pair& pair) {
+  constexpr uint32_t kLanes = D / 8, kTeam = 2 * kLanes;
+  const uint32_t teams = blockDim.x / kTeam, team = threadIdx.x / kTeam, in = threadIdx.x % kTeam;
+  const int which = in >= kLanes;
+  const uint32_t mask = (1u << a.page_log2) - 1;
+  uint8_t* const base = a.base[which] + (int64_t)head * a.head[which] + (in - which * kLanes) * 16;
+  const int64_t page_stride = a.page[which], place_stride = a.place[which];
+  for (uint32_t m0 = group * teams * kAhead + team; m0 < moves; m0 += groups * teams * kAhead) {
+    uint32_t from[kAhead], to[kAhead], src[kAhead], dst[kAhead];
+    u32x4v data[kAhead];
+    float w[kAhead];
+    int32_t b[kAhead];
+    bool live[kAhead];
+#pragma unroll
+    for (int r = 0; r < kAhead; ++r) {
+      const uint32_t m = m0 + r * teams;
+      live[r] = m < moves;
+      const uint2 p = pair(live[r] ? m : m0);
+      from[r] = p.x;
+      to[r] = p.y;
+    }
+#pragma unroll
+    for (int r = 0; r < kAhead; ++r) {
+      src[r] = (uint32_t)pages[from[r] >> a.page_log2];
+      dst[r] = (uint32_t)pages[to[r] >> a.page_log2];
+    }
+#pragma unroll
+    for (int r = 0; r < kAhead; ++r) {
+      live[r] = live[r] && src[r] < a.n_pages && dst[r] < a.n_pages;
+      if (!live[r]) continue;
+      data[r] = *reinterpret_cast<const u32x4v*>(base + (int64_t)src[r] * page_stride +
+                                                 (int64_t)(from[r] & mask) * place_stride);
+      if (in == 0) {
+        const uint64_t at = ((uint64_t)src[r] * a.kv_heads + head) << a.page_log2 | (from[r] & mask);
+        w[r] = a.weights[at];
+        b[r] = a.born[at];
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < kAhead; ++r) {
+      if (!live[r]) continue;
+      *reinterpret_cast<u32x4v*>(base + (int64_t)dst[r] * page_stride + (int64_t)(to[r] & mask) * place_stride) = data[r];
+      if (in == 0) {
+        const uint64_t at = ((uint64_t)dst[r] * a.kv_heads + head) << a.page_log2 | (to[r] & mask);
+        a.weights_out[at] = w[r];
+        a.born_out[at] = b[r];
+      }
+    }
+  }
+}
+
+// The counts of a round, from the largest bin down: which one the `left`-th key is in, how many of it are kept
+// (left again), and how many it has. By a wave for itself, four bins a lane.
+struct Found {
+  uint32_t bin, count;
+};
+__device__ inline Found bin_of(const uint32_t* bins, uint32_t* left) {
+  const uint32_t lane = threadIdx.x & 63;
+  const u32x4v c = *reinterpret_cast<const u32x4v*>(bins + kBins - 4 * (lane + 1));
+  const uint32_t sum = c[0] + c[1] + c[2] + c[3], upto = wave_scan(sum, SumOp());
+  const uint32_t at = uniform((uint32_t)__builtin_ctzll(__ballot(upto >= *left)));
+  uint32_t rest = *left - (upto - sum), bin = kBins - 4 * lane - 1, count = c[3];  // of lane `at` these hold
+#pragma unroll
+  for (int i = 2; i >= 0; --i) {
+    const bool on = rest > count && bin == kBins - 4 * lane - (uint32_t)(3 - i);
+    rest -= on ? count : 0;
+    bin -= on;
+    count = on ? c[i] : count;
+  }
+  auto get = [at](uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, (int)at); };
+  *left = get(rest);
+  return {get(bin), get(count)};
+}
+
+// Adds what a wave's lanes found to a round's counts. Lanes of one bin wait for each other: where it is the same
+// for all, it is added to once.
+__device__ inline void count_bins(uint32_t* bins, uint32_t bin, bool counts) {
+  if (!counts) return;
+  const uint32_t lead = uniform(bin);
+  if (__ballot(bin != lead) == 0) {
+    const uint64_t who = __ballot(true);
+    if ((threadIdx.x & 63) == (uint32_t)__builtin_ctzll(who)) atomicAdd(&bins[lead], (uint32_t)__popcll(who));
+  } else {
+    atomicAdd(&bins[bin], 1u);
+  }
 }
 
 // Exclusive sum over the workgroup; `total` gets the sum. Two barriers.
 __device__ inline uint32_t sum_before(uint32_t v, uint32_t* lds, uint32_t* total) {
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t upto = v;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const uint32_t x = __shfl_up(upto, d, 64);
-    if ((int)lane >= d) upto += x;
-  }
+  const uint32_t upto = wave_scan(v, SumOp());
   if (lane == 63) lds[wave] = upto;
   __syncthreads();
   uint32_t before = 0, all = 0;
-#pragma unroll
-  for (uint32_t w = 0; w < kWaves; ++w) {
+  for (uint32_t w = 0; w < blockDim.x / 64; ++w) {
     if (w == wave) before = all;
     all += lds[w];
   }
@@ -91,176 +179,245 @@ __device__ inline uint32_t sum_before(uint32_t v, uint32_t* lds, uint32_t* total
   return before + upto - v;
 }
 
-__global__ __launch_bounds__(kThreads) void select_kernel(EvictArgs a) {
-  extern __shared__ uint32_t lds_rank[];
-  __shared__ uint32_t bins[kBins];
-  __shared__ uint32_t lds_sum[kWaves], lds_found[2];
+// Longer sequences than registers hold: a run of keys for each thread.
+__device__ void select_long(const EvictArgs& a, const int32_t* pages, uint32_t head, uint32_t keys, int64_t late,
+                            uint2* out, uint32_t* bins, uint32_t* lds_sum, uint32_t* moves) {
+  auto rank_at = [&](uint32_t i) {
+    const uint64_t at = tracked_at(a, pages, head, i);
+    return at == ~0ull ? 0u : rank_of(a, a.weights[at], a.born[at], late);
+  };
+  const uint32_t tid = threadIdx.x, threads = blockDim.x, keep = a.keep;
+  uint32_t known = 0, known_mask = 0, left = keep;
+#pragma unroll 1
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    uint32_t* const mine = bins + shift / 8 * kBins;
+    for (uint32_t i0 = 0; i0 < keys; i0 += threads) {
+      const uint32_t i = i0 + tid, r = i < keys ? rank_at(i) : 0;
+      count_bins(mine, (r >> shift) & 255, i < keys && (r & known_mask) == known);
+    }
+    __syncthreads();
+    known |= bin_of(mine, &left).bin << shift;
+    known_mask |= 255u << shift;
+  }
+  const uint32_t per = (keys + threads - 1) / threads;
+  const uint32_t from = tid * per < keys ? tid * per : keys, to = from + per < keys ? from + per : keys;
+  uint32_t same = 0, all;
+  for (uint32_t i = from; i < to; ++i) same += rank_at(i) == known;
+  const uint32_t same_before = sum_before(same, lds_sum, &all);
+  uint32_t count = 0;
+  same = same_before;
+  for (uint32_t i = from; i < to; ++i) {
+    const uint32_t r = rank_at(i);
+    const bool kept = r > known || (r == known && same++ < left);
+    count += i < keep ? !kept : kept;
+  }
+  uint32_t at = sum_before(count, lds_sum, &all);
+  *moves = all / 2;
+  same = same_before;
+  for (uint32_t i = from; i < to; ++i) {
+    const uint32_t r = rank_at(i);
+    const bool kept = r > known || (r == known && same++ < left);
+    if (i < keep ? kept : !kept) continue;
+    // free places all lie before keep, moving keys behind: as many of both
+    if (i < keep) out[at++].y = i;
+    else out[at++ - *moves].x = i;
+  }
+}
+
+// How many of the workgroup's keys with a flag come before a thread's key number r, in the keys' order. counts:
+// kKeys times the waves, of the workgroup. One barrier.
+template <int kKeys>
+struct Ordered {
+  static constexpr int kEntries = kKeys * kWaves / 64;  // a lane's
+  uint32_t flags;  // of the thread's keys, a bit each
+  uint32_t before[kEntries];
+  uint32_t all;
+
+  __device__ void count(uint32_t* counts) {
+    const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    uint32_t mine = 0;
+#pragma unroll 4
+    for (int r = 0; r < kKeys; ++r) {
+      const uint32_t n = (uint32_t)__popcll(__ballot(flags >> r & 1));
+      if (lane == (uint32_t)r) mine = n;
+    }
+    if (lane < kKeys) counts[lane * kWaves + wave] = mine;
+    __syncthreads();
+    uint32_t sum = 0;
+#pragma unroll
+    for (int i = 0; i < kEntries; ++i) {
+      before[i] = sum;
+      sum += counts[lane * kEntries + i];
+    }
+    const uint32_t upto = wave_scan(sum, SumOp());
+    all = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+#pragma unroll
+    for (int i = 0; i < kEntries; ++i) before[i] += upto - sum;
+  }
+  // (by whole waves)
+  __device__ uint32_t of(uint32_t r) const {
+    const uint32_t wave = uniform(threadIdx.x >> 6), entry = r * kWaves + wave;
+    uint32_t x = 0;
+#pragma unroll
+    for (int i = 0; i < kEntries; ++i)  // one of them, chosen by the wave's number
+      if (entry % kEntries == (uint32_t)i) x = (uint32_t)__builtin_amdgcn_readlane((int)before[i], (int)(entry / kEntries));
+    const uint64_t who = __ballot(flags >> r & 1);
+    return x + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+  }
+};
+
+template <int D, int kKeys>
+__global__ __launch_bounds__(kThreads, kKeys == kNarrowKeys ? 8 : 4) void select_kernel(EvictArgs a) {
+  constexpr bool kNarrow = kKeys == kNarrowKeys;
+  constexpr int kGroup = kNarrow ? 4 : 8;  // loads of a kind that go out together
+  __shared__ __attribute__((aligned(16))) uint32_t rank[kKeys * kThreads], bins[4 * kBins];
+  __shared__ uint32_t counts[2][kKeys * kWaves];
   const uint32_t tid = threadIdx.x;
   for (uint32_t pair = blockIdx.x; pair < a.n_seq * a.kv_heads; pair += gridDim.x) {
     const uint32_t s = pair / a.kv_heads, head = pair % a.kv_heads;
     const int32_t* const pages = a.own_pages + (uint64_t)s * a.own_width;
+    // the first keys' pages are looked up while the length is on its way
+    const uint32_t places = a.own_width << a.page_log2;
+    uint32_t page[kGroup];
+#pragma unroll
+    for (int r = 0; r < kGroup; ++r) {
+      const uint32_t i = r * kThreads + tid;
+      page[r] = places ? (uint32_t)pages[(i < places ? i : 0) >> a.page_log2] : kNoPage;
+    }
     const uint32_t keys = keys_of(a, s), keep = a.keep < keys ? a.keep : keys;
     const int64_t late = (int64_t)a.total[s] - a.recent;
-    if (keys <= a.keep || keep == 0) {  // all stay, or none
-      for (uint32_t i = tid; i < keep; i += kThreads) {
-        const uint64_t at = tracked_at(a, pages, head, i);
-        if (at == ~0ull) continue;
-        if (a.weights_out != a.weights) a.weights_out[at] = a.weights[at];
-        if (a.born_out != a.born) a.born_out[at] = a.born[at];
-      }
-      if (tid == 0) a.moves[pair] = 0;
-      continue;
-    }
-    const bool in_lds = keys <= a.lds_keys;
-    if (in_lds) {
-      for (uint32_t i = tid; i < keys; i += kThreads) lds_rank[i] = rank_of(a, pages, head, i, late);
-    }
-    auto rank_at = [&](uint32_t i) { return in_lds ? lds_rank[i] : rank_of(a, pages, head, i, late); };
+    if (head == 0 && tid == 0) a.len_out[s] = (int32_t)keep;
+    if (tid < 4 * kBins) bins[tid] = 0;
 
-    // the rank of the last one kept: its bits from the top, and how many of the keys that have them are kept
-    uint32_t known = 0, known_mask = 0, left = keep;
+    // What stays where it is is written on, and the others' places by who copies pairs. For no key a first one's
+    // weight is loaded.
+#pragma unroll 1
+    for (uint32_t i0 = 0; i0 < keys; i0 += kGroup * kThreads) {
+      float w[kGroup];
+      int32_t b[kGroup];
+      uint64_t at[kGroup];
 #pragma unroll
-    for (int round = 0; round < 3; ++round) {
-      const int shift = round == 0 ? 21 : round == 1 ? 10 : 0;
-      const uint32_t mask = round == 2 ? 1023u : 2047u;
-      for (uint32_t b = tid; b < kBins; b += kThreads) bins[b] = 0;
-      __syncthreads();
-      for (uint32_t i0 = 0; i0 < keys; i0 += kThreads) {
-        const uint32_t i = i0 + tid;
-        uint32_t r = 0;
-        bool counts = i < keys;
-        if (counts) {
-          r = rank_at(i);
-          counts = (r & known_mask) == known;
+      for (int r = 0; r < kGroup; ++r) {
+        const uint32_t i = i0 + r * kThreads + tid;
+        at[r] = i < keys && page[r] < a.n_pages
+                    ? ((uint64_t)page[r] * a.kv_heads + head) << a.page_log2 | (i & ((1u << a.page_log2) - 1)) : ~0ull;
+        w[r] = a.weights[at[r] != ~0ull ? at[r] : 0];
+        b[r] = a.born[at[r] != ~0ull ? at[r] : 0];
+      }
+      if (!kNarrow) {
+#pragma unroll
+        for (int r = 0; r < kGroup; ++r) {
+          const uint32_t i = i0 + (kGroup + r) * kThreads + tid;
+          page[r] = (uint32_t)pages[(i < keys ? i : 0) >> a.page_log2];
         }
-        const uint32_t bin = (r >> shift) & mask;
-        // equal bins of a wave would wait for each other: those of its first key are added as one
-        const uint64_t who = __ballot(counts);
-        if (!who) continue;
-        const uint32_t lead = (uint32_t)__builtin_ctzll(who);
-        const bool with_lead = counts && bin == __shfl(bin, (int)lead, 64);
-        const uint64_t together = __ballot(with_lead);
-        if ((tid & 63) == lead) atomicAdd(&bins[bin], (uint32_t)__popcll(together));
-        else if (counts && !with_lead) atomicAdd(&bins[bin], 1u);
       }
-      __syncthreads();
-      // bins from the largest down, two a thread: the one that the last kept key is in
-      const uint32_t hi = kBins - 1 - 2 * tid, c0 = bins[hi], c1 = bins[hi - 1];
-      uint32_t all;
-      const uint32_t before = sum_before(c0 + c1, lds_sum, &all);
-      if (before < left && left <= before + c0) {
-        lds_found[0] = hi;
-        lds_found[1] = left - before;
-      } else if (before + c0 < left && left <= before + c0 + c1) {
-        lds_found[0] = hi - 1;
-        lds_found[1] = left - before - c0;
+#pragma unroll
+      for (int r = 0; r < kGroup; ++r) {
+        const uint32_t i = i0 + r * kThreads + tid;
+        const bool there = at[r] != ~0ull, stays = there && i < keep;
+        if (i < kKeys * kThreads) rank[i] = there ? rank_of(a, w[r], b[r], late) : 0;
+        if (stays && a.weights_out != a.weights) a.weights_out[at[r]] = w[r];
+        if (stays && a.born_out != a.born) a.born_out[at[r]] = b[r];
       }
-      __syncthreads();
-      known |= lds_found[0] << shift;
-      known_mask |= mask << shift;
-      left = lds_found[1];
     }
-
-    // a run of keys for each thread: how many of just that rank come before, then free places and moving keys
-    const uint32_t per = (keys + kThreads - 1) / kThreads;
-    const uint32_t from = tid * per < keys ? tid * per : keys, to = from + per < keys ? from + per : keys;
-    uint32_t same = 0, all;
-    for (uint32_t i = from; i < to; ++i) same += rank_at(i) == known;
-    const uint32_t same_before = sum_before(same, lds_sum, &all);
-    uint32_t count = 0;
-    same = same_before;
-    for (uint32_t i = from; i < to; ++i) {
-      const uint32_t r = rank_at(i);
-      const bool kept = r > known || (r == known && same++ < left);
-      count += i < keep ? !kept : kept;
-    }
-    // free places all lie before keep, moving keys behind: the sum before a thread is that of the former,
-    // then all of those and the latter
-    uint32_t at = sum_before(count, lds_sum, &all);
-    const uint32_t moves = all / 2;  // as many of both
+    __syncthreads();
+    uint32_t moves = 0;
     uint2* const out = a.pairs + (uint64_t)pair * a.most;
-    same = same_before;
-    for (uint32_t i = from; i < to; ++i) {
-      const uint32_t r = rank_at(i);
-      const bool kept = r > known || (r == known && same++ < left);
-      if (i < keep ? !kept : kept) {
-        if (i < keep) out[at++].y = i;
-        else out[at++ - moves].x = i;
+    if (keys <= a.keep || keep == 0) {  // all stay, or none
+    } else if (!kNarrow && keys > kKeys * kThreads) {
+      select_long(a, pages, head, keys, late, out, bins, counts[0], &moves);
+    } else {
+      uint32_t known = 0, known_mask = 0, left = keep, same = 0;  // same: keys of the last kept one's rank
+#pragma unroll 1
+      for (int shift = 24; shift >= 0; shift -= 8) {
+        uint32_t* const mine = bins + shift / 8 * kBins;
+#pragma unroll 4
+        for (uint32_t i0 = 0; i0 < keys; i0 += kThreads) {
+          const uint32_t r = rank[i0 + tid];  // (of no key, of none of these bits or not counted)
+          count_bins(mine, (r >> shift) & 255, i0 + tid < keys && (r & known_mask) == known);
+        }
+        __syncthreads();
+        const Found found = bin_of(mine, &left);
+        known |= found.bin << shift;
+        known_mask |= 255u << shift;
+        same = found.count;
+      }
+      const bool all_same = left == same;  // all of them are kept: no need to know which come first
+      Ordered<kKeys> order;
+      order.flags = 0;
+      uint32_t more = 0, there = 0;  // of a larger rank; keys at all
+#pragma unroll 4
+      for (uint32_t r = 0; r * kThreads < keys; ++r) {
+        const uint32_t i = r * kThreads + tid, x = rank[i], is = i < keys ? 1u : 0u;
+        there |= is << r;
+        order.flags |= (x == known ? is : 0u) << r;
+        more |= (x > known ? is : 0u) << r;
+      }
+      if (!all_same) {
+        order.count(counts[0]);
+        uint32_t first = 0;
+#pragma unroll 1
+        for (uint32_t r = 0; r * kThreads < keys; ++r) first |= (order.of(r) < left ? 1u : 0u) << r;
+        order.flags &= first;
+      }
+      const uint32_t kept = more | order.flags;
+      uint32_t within = 0;  // places within the budget
+#pragma unroll 1
+      for (uint32_t r = 0; r * kThreads + tid < keep; ++r) within |= 1u << r;
+      order.flags = (kept ^ within) & there;
+      order.count(counts[1]);
+      moves = order.all / 2;  // free places all lie before keep, moving keys behind: as many of both
+      uint16_t* const half = reinterpret_cast<uint16_t*>(rank);
+      // (ranks are not needed any more once all have counted)
+#pragma unroll 1
+      for (uint32_t r = 0; r * kThreads < keys; ++r) {
+        const uint32_t i = r * kThreads + tid, at = order.of(r);
+        if (!(order.flags >> r & 1)) continue;
+        if (kNarrow && a.copies) {
+          if (i < keep) half[2 * at + 1] = (uint16_t)i;
+          else half[2 * (at - moves)] = (uint16_t)i;
+        } else {
+          if (i < keep) out[at].y = i;
+          else out[at - moves].x = i;
+        }
       }
     }
-    if (a.weights_out != a.weights || a.born_out != a.born) {
-      // what stays where it is; move_kernel writes the others' places
+    if (kNarrow && a.copies) {
       __syncthreads();
-      for (uint32_t i = tid; i < keep; i += kThreads) {
-        const uint64_t where = tracked_at(a, pages, head, i);
-        if (where == ~0ull) continue;
-        if (a.weights_out != a.weights) a.weights_out[where] = a.weights[where];
-        if (a.born_out != a.born) a.born_out[where] = a.born[where];
-      }
+      copy_pairs<D, 2>(a, pages, head, moves, 0, 1, [&](uint32_t m) { return uint2{rank[m] & 0xffffu, rank[m] >> 16}; });
+    } else if (tid == 0) {
+      a.moves[pair] = moves;
     }
-    if (tid == 0) a.moves[pair] = moves;
     __syncthreads();
   }
 }
 
-// D / 8 lanes copy a key, as many its value, 16 bytes each; the first of them what is kept about it.
 template <int D>
 __global__ __launch_bounds__(kMoveThreads) void move_kernel(EvictArgs a) {
-  constexpr uint32_t kLanes = D / 8, kTeam = 2 * kLanes, kTeams = kMoveThreads / kTeam;
-  constexpr uint32_t kAhead = 4;
-  const uint32_t team = threadIdx.x / kTeam, in = threadIdx.x % kTeam;
-  const int which = in >= kLanes;
-  const uint32_t mask = (1u << a.page_log2) - 1;
   for (uint32_t pair = blockIdx.y; pair < a.n_seq * a.kv_heads; pair += gridDim.y) {
-    const uint32_t s = pair / a.kv_heads, head = pair % a.kv_heads;
-    if (blockIdx.x == 0 && head == 0 && threadIdx.x == 0) {
-      const uint32_t keys = keys_of(a, s);
-      a.len_out[s] = (int32_t)(keys < a.keep ? keys : a.keep);
-    }
-    const uint32_t moves = a.moves[pair];
-    const int32_t* const pages = a.own_pages + (uint64_t)s * a.own_width;
+    const uint32_t s = pair / a.kv_heads;
     const uint2* const pairs = a.pairs + (uint64_t)pair * a.most;
-    uint8_t* const base = a.base[which] + (int64_t)head * a.head[which] + (in - which * kLanes) * 16;
-    for (uint32_t m0 = blockIdx.x * kTeams * kAhead + team; m0 < moves; m0 += gridDim.x * kTeams * kAhead) {
-      u32x4v data[kAhead];
-      int64_t to[kAhead];
-      float w[kAhead];
-      int32_t b[kAhead];
-      uint64_t tracked[kAhead];
-      bool live[kAhead];
-#pragma unroll
-      for (uint32_t r = 0; r < kAhead; ++r) {
-        const uint32_t m = m0 + r * kTeams;
-        live[r] = false;
-        if (m >= moves) continue;
-        const uint2 p = pairs[m];
-        const uint32_t src = (uint32_t)pages[p.x >> a.page_log2], dst = (uint32_t)pages[p.y >> a.page_log2];
-        live[r] = src < a.n_pages && dst < a.n_pages;
-        if (!live[r]) continue;
-        data[r] = *reinterpret_cast<const u32x4v*>(base + (int64_t)src * a.page[which] +
-                                                   (int64_t)(p.x & mask) * a.place[which]);
-        to[r] = (int64_t)dst * a.page[which] + (int64_t)(p.y & mask) * a.place[which];
-        if (in == 0) {
-          const uint64_t at = ((uint64_t)src * a.kv_heads + head) << a.page_log2 | (p.x & mask);
-          tracked[r] = ((uint64_t)dst * a.kv_heads + head) << a.page_log2 | (p.y & mask);
-          w[r] = a.weights[at];
-          b[r] = a.born[at];
-        }
-      }
-#pragma unroll
-      for (uint32_t r = 0; r < kAhead; ++r) {
-        if (!live[r]) continue;
-        *reinterpret_cast<u32x4v*>(base + to[r]) = data[r];
-        if (in == 0) {
-          a.weights_out[tracked[r]] = w[r];
-          a.born_out[tracked[r]] = b[r];
-        }
-      }
-    }
+    copy_pairs<D, 4>(a, a.own_pages + (uint64_t)s * a.own_width, pair - s * a.kv_heads, a.moves[pair], blockIdx.x, gridDim.x,
+                  [&](uint32_t m) { return pairs[m]; });
   }
 }
 
-constexpr uint64_t kMostPairs = 1ull << 36;
+template <int D>
+gleam_status launch_evict(const EvictArgs& a, bool narrow, hipStream_t s) {
+  const uint32_t n = a.n_seq * a.kv_heads;
+  const uint64_t most = max_workgroups(kThreads);
+  const dim3 grid((uint32_t)(n < most ? n : most));
+  if (narrow) hipLaunchKernelGGL((select_kernel<D, kNarrowKeys>), grid, dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((select_kernel<D, kWideKeys>), grid, dim3(kThreads), 0, s, a);
+  const gleam_status st = launch_status("select_kernel");
+  if (st != GLEAM_OK || a.copies || a.most == 0) return st;
+  // workgroups for each sequence and head: as many as there may be moves for, and as give kMoveGroups in all
+  constexpr uint32_t teams = kMoveThreads / (D / 4);
+  const uint32_t want = (a.most + 4 * teams - 1) / (4 * teams), share = kMoveGroups / n;
+  const uint32_t x = want < share ? want : share;
+  hipLaunchKernelGGL(move_kernel<D>, dim3(x ? x : 1, n < 65535 ? n : 65535), dim3(kMoveThreads), 0, s, a);
+  return launch_status("move_kernel");
+}
 
 // Pairs of places that a sequence and head can have.
 uint64_t most_moves(const gleam_kv_pages* kv, const gleam_evict* in) {
@@ -311,7 +468,7 @@ gleam_status validate_evict(const gleam_kv_pages* kv, const gleam_evict* in, con
 
 hipError_t preload_kv_evict() {
   hipFuncAttributes attr;
-  return hipFuncGetAttributes(&attr, reinterpret_cast<const void*>(&select_kernel));
+  return hipFuncGetAttributes(&attr, reinterpret_cast<const void*>(&move_kernel<128>));
 }
 
 }  // namespace gleam
@@ -336,6 +493,12 @@ extern "C" gleam_status gleam_kv_evict(const gleam_kv_pages* kv, const gleam_evi
   if (in->n_seq == 0) return GLEAM_OK;
   if (!in->d_total || !in->d_len_out) {
     set_error("%s: null total or len_out", who);
+    return GLEAM_E_INVALID;
+  }
+  // workgroups read the lengths at different times
+  const uintptr_t from = reinterpret_cast<uintptr_t>(in->d_own_len), to = reinterpret_cast<uintptr_t>(in->d_len_out);
+  if ((from < to ? to - from : from - to) < 4 * in->n_seq) {
+    set_error("%s: len_out must not overlap own_len", who);
     return GLEAM_E_INVALID;
   }
   if ((st = validate_tracked(kv, in->d_weights, in->d_weights_out, "weights", who)) != GLEAM_OK) return st;
@@ -377,20 +540,10 @@ extern "C" gleam_status gleam_kv_evict(const gleam_kv_pages* kv, const gleam_evi
   a.keep = in->keep;
   a.sinks = in->sinks;
   a.recent = in->recent;
-  const uint64_t keys = in->own_width * kv->page_tokens;
-  a.lds_keys = keys < kLdsKeys ? (uint32_t)keys : kLdsKeys;
+  const bool narrow = in->own_width * kv->page_tokens <= kNarrowKeys * kThreads;
+  a.copies = narrow && in->n_seq * kv->kv_heads >= kManyPairs;
   hipStream_t s = (hipStream_t)stream;
-  const uint32_t n = a.n_seq * a.kv_heads;
-  const uint32_t most = (uint32_t)max_workgroups(kThreads);
-  hipLaunchKernelGGL(select_kernel, dim3(n < most ? n : most), dim3(kThreads), a.lds_keys * 4, s, a);
-  if ((st = launch_status("select_kernel")) != GLEAM_OK) return st;
-  // workgroups for each sequence and head: as many as there may be moves for, and as give kMoveGroups in all
-  const uint32_t teams = kMoveThreads / (kv->head_dim / 4);
-  const uint32_t want = (a.most + 4 * teams - 1) / (4 * teams), share = kMoveGroups / n;
-  const uint32_t x = want < share ? want : share;
-  const dim3 grid(x ? x : 1, n < 65535 ? n : 65535);
-  if (kv->head_dim == 64) hipLaunchKernelGGL(move_kernel<64>, grid, dim3(kMoveThreads), 0, s, a);
-  else if (kv->head_dim == 128) hipLaunchKernelGGL(move_kernel<128>, grid, dim3(kMoveThreads), 0, s, a);
-  else hipLaunchKernelGGL(move_kernel<256>, grid, dim3(kMoveThreads), 0, s, a);
-  return launch_status("move_kernel");
+  return kv->head_dim == 64    ? launch_evict<64>(a, narrow, s)
+         : kv->head_dim == 128 ? launch_evict<128>(a, narrow, s)
+                               : launch_evict<256>(a, narrow, s);
 }

@@ -326,11 +326,18 @@ def test_more_to_keep_than_the_budget():
     c.check()
 
 
-@pytest.mark.parametrize("own,keep", [(1023, 512), (1024, 1), (1025, 1000), (2050, 2048), (5000, 700), (40000, 300),
-                                      (33000, 32000)])
+@pytest.mark.parametrize("own,keep", [(255, 100), (257, 256), (1023, 512), (1025, 1000), (2050, 2048), (4000, 1500),
+                                      (4070, 2001), (4500, 700), (20000, 9000), (40000, 300), (33000, 32000)])
 def test_long_sequences(own, keep):
-    """On both sides of a thread's first key, and of what LDS holds of a sequence."""
+    """On both sides of what a workgroup's registers hold, for narrow tables and for wide ones."""
     Evicted([own], 1, 64, 16, F16, keep, sinks=4, recent=keep // 8, kind="few" if own % 2 else "random").check()
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_many_sequences_and_heads_of_narrow_tables(d):
+    """Whose workgroups copy the pairs themselves."""
+    Evicted([600 + 7 * i for i in range(16)], 8, d, 16, BF16, 400, recent=30, kind="few", seed=d).check()
+    Evicted([4000, 3100, 1, 0, 2049, 2047, 4064, 2500], 16, d, 32, F16, 2048, sinks=3, recent=100).check()
 
 
 def test_missing_pages():
@@ -377,15 +384,6 @@ def test_evict_streams_graphs_and_lengths_out_of_range():
     assert g.kv_evict(**{**a, "keep": 100}).tolist() == [0, 100, 3]
 
 
-def test_the_lengths_may_change_in_place():
-    c = Evicted([300, 500, 40], 3, 64, 16, BF16, 200)
-    a, want = c.arguments(), c.want()
-    assert g.kv_evict(**a, len_out=a["own_len"]) is a["own_len"]
-    torch.cuda.synchronize()
-    for x, y in zip((a["k_pages"], a["v_pages"], a["weights"], a["born"], a["own_len"]), want):
-        assert torch.equal(bits(x), bits(y))
-
-
 def test_evict_refusals():
     c = Evicted([50, 60], 2, 64, 16, F16, 20)
     a = c.arguments()
@@ -396,7 +394,7 @@ def test_evict_refusals():
                          ("workspace of 256 bytes", {"ws": torch.empty(256, dtype=torch.uint8, device="cuda")}),
                          ("overlap", {"k_pages": a["k_pages"][:, :, :1].expand(-1, -1, 2, -1)}),
                          ("differ in shape", {"v_pages": a["v_pages"][:1]}),
-                         ("len_out holds", {"len_out": a["own_len"][:1]})):
+                         ("len_out holds", {"len_out": a["own_len"][:1]}), ("overlap own_len", {"len_out": a["own_len"]})):
         with pytest.raises((ValueError, g.GleamError), match=message):
             g.kv_evict(**{**a, **bad})
     for name in ("k_pages", "v_pages", "weights"):

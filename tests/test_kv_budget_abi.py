@@ -38,7 +38,7 @@ def weigh(cache=None, **kw):
 
 
 def evict_args(**kw):
-    return put(g._Evict(256, 256, 1 << 20, 1 << 21, 256, 1 << 20, 1 << 21, 256, 2, 3, 20, 0, 0), **kw)
+    return put(g._Evict(256, 256, 1 << 20, 1 << 21, 256, 1 << 20, 1 << 21, 512, 2, 3, 20, 0, 0), **kw)
 
 
 def evict(cache=None, ws=256, ws_bytes=1 << 40, **kw):
@@ -121,6 +121,7 @@ def test_weigh_limits():
 
 @pytest.mark.parametrize("bad", [{"own_len": None}, {"own_pages": None}, {"weights": None}, {"born": None},
                                  {"total": None}, {"weights_out": None}, {"born_out": None}, {"len_out": None},
+                                 {"len_out": 256}, {"len_out": 260},
                                  {"weights_out": (1 << 20) + 4}, {"born_out": (1 << 21) - 4}, {"weights": (1 << 20) + 1},
                                  {"own_width": 1 << 27}, {"ws": None}, {"ws": 128}])
 def test_evictions_that_are_refused(bad):
