@@ -132,7 +132,7 @@ constexpr int kAcceptRows = 8;  // rows in flight
 // The path's drafts, in order, are the leaf's bits. Draft number e of the path goes to where draft e was:
 // never behind its own place, so a lane that takes 16 bytes of each row in turn overwrites none that it
 // still has to read, and no other lane has to do with them. D / 8 lanes take a head's keys, others its
-// values and the next heads; the bits and pages are the same for all of a workgroup.
+// values and the next heads. Where 64 drafts' keys are, and go to, is looked up at once, by a lane each.
 template <int D>
 __global__ __launch_bounds__(kAcceptThreads) void accept_kernel(AcceptArgs a) {
   constexpr uint32_t kLanes = D / 8;
@@ -154,44 +154,37 @@ __global__ __launch_bounds__(kAcceptThreads) void accept_kernel(AcceptArgs a) {
     if (leaf >= 0 && (uint32_t)leaf < n) {
       const uint64_t* const bits = a.seen + (uint64_t)(first + leaf) * a.words;
       const int32_t* const pages = a.own_pages + (uint64_t)s * a.own_width;
-      uint32_t word = 0;
-      uint64_t left = bits[0];
-      // the next draft of the path that has a key, n after the last one
-      auto next = [&]() -> uint32_t {
-        for (;;) {
-          while (left == 0) {
-            if (++word >= a.words || word * 64 >= n) return n;
-            left = bits[word];
+      const uint32_t lane = threadIdx.x & 63, mask = (1u << a.page_log2) - 1;
+      for (uint32_t word = 0; word < a.words && word * 64 < n; ++word) {
+        const uint32_t j = word * 64 + lane;
+        const int64_t key = draft + j;
+        const uint64_t on = __ballot((bits[word] >> lane & 1) && j < n && key >= 0);
+        const uint32_t src = (uint32_t)key, dst = kept + path + (uint32_t)__popcll(on & ((1ull << lane) - 1));
+        path += (uint32_t)__popcll(on);
+        uint32_t src_page = kNoPage, dst_page = kNoPage;
+        if ((on >> lane & 1) && src != dst) {
+          src_page = (uint32_t)pages[src >> a.page_log2];
+          dst_page = (uint32_t)pages[dst >> a.page_log2];
+        }
+        uint64_t todo = __ballot(src_page < a.n_pages && dst_page < a.n_pages);
+        while (todo) {
+          u32x4v data[kAcceptRows];
+          int64_t to[kAcceptRows];
+#pragma unroll
+          for (int r = 0; r < kAcceptRows; ++r) {
+            to[r] = -1;
+            if (!todo) continue;
+            const int at = __builtin_ctzll(todo);
+            todo &= todo - 1;
+            auto get = [at](uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, at); };
+            const uint8_t* const from = base + (int64_t)get(src_page) * page_stride + (int64_t)(get(src) & mask) * place_stride;
+            to[r] = (int64_t)get(dst_page) * page_stride + (int64_t)(get(dst) & mask) * place_stride;
+            if (live) data[r] = *reinterpret_cast<const u32x4v*>(from);
           }
-          const uint32_t j = word * 64 + (uint32_t)__builtin_ctzll(left);
-          left &= left - 1;
-          if (j >= n) return n;
-          if (draft + j >= 0) return j;
-        }
-      };
-      for (bool more = true; more;) {
-        u32x4v data[kAcceptRows];
-        uint64_t to[kAcceptRows];
-        bool moves[kAcceptRows];
 #pragma unroll
-        for (int r = 0; r < kAcceptRows; ++r) {
-          const uint32_t j = more ? next() : n;
-          more = more && j < n;
-          moves[r] = false;
-          if (!more) continue;
-          const uint32_t src = (uint32_t)(draft + j), dst = kept + path++;
-          if (src == dst) continue;
-          const uint32_t mask = (1u << a.page_log2) - 1;
-          const uint32_t src_page = (uint32_t)pages[src >> a.page_log2], dst_page = (uint32_t)pages[dst >> a.page_log2];
-          moves[r] = live && src_page < a.n_pages && dst_page < a.n_pages;
-          if (!moves[r]) continue;
-          data[r] = *reinterpret_cast<const u32x4v*>(base + (int64_t)src_page * page_stride +
-                                                     (int64_t)(src & mask) * place_stride);
-          to[r] = (uint64_t)((int64_t)dst_page * page_stride + (int64_t)(dst & mask) * place_stride);
+          for (int r = 0; r < kAcceptRows; ++r)
+            if (live && to[r] >= 0) *reinterpret_cast<u32x4v*>(base + to[r]) = data[r];
         }
-#pragma unroll
-        for (int r = 0; r < kAcceptRows; ++r)
-          if (moves[r]) *reinterpret_cast<u32x4v*>(base + to[r]) = data[r];
       }
     }
     if (blockIdx.y == 0 && threadIdx.x == 0) a.len_out[s] = (int32_t)(kept + path);
