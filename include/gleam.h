@@ -751,8 +751,8 @@ gleam_status gleam_prefix_attention(const gleam_kv_pages* kv, const gleam_prefix
  * gleam_tree_attention: gleam_prefix_attention of such drafts, whose keys are the last n of their
  * sequence's own: token i of n sees its group's whole prefix, the own keys before the first draft's, and
  * the key of draft j (number d_own_len[s] - n + j of the own keys, where that is not below 0) if its bit j
- * is set. Any bits are taken, not only those of trees; a row may see nothing. Arguments, workspace, limits
- * and errors are gleam_prefix_attention's.
+ * is set. Any bits are taken, not only those of trees; a row may see nothing. Arguments, limits and errors
+ * are gleam_prefix_attention's, the workspace is of gleam_tree_attention_ws_bytes.
  *
  * gleam_kv_accept: the keys and values of the path that was accepted move together. Of sequence s those
  * drafts are kept that draft d_leaf[s] sees (none where d_leaf[s] is not one of its drafts): the e-th of
@@ -775,6 +775,7 @@ typedef struct gleam_accept {
 
 gleam_status gleam_draft_tree(const int32_t* d_parent, const int32_t* d_q_first, uint64_t n_tokens, uint64_t n_seq,
                               uint64_t* d_seen, uint32_t seen_words, int32_t* d_depth, void* stream);
+size_t gleam_tree_attention_ws_bytes(const gleam_kv_pages* kv, const gleam_prefix_batch* b);
 gleam_status gleam_tree_attention(const gleam_kv_pages* kv, const gleam_prefix_batch* b, const uint64_t* d_seen,
                                   uint32_t seen_words, void* d_out, float* d_lse, void* d_ws, size_t ws_bytes,
                                   void* stream);

@@ -50,7 +50,7 @@ EXPORTS = (
     "gleam_detect_ws_init", "gleam_identify_leaves", "gleam_first_writes_ws_bytes", "gleam_first_writes",
     "gleam_cache_erase_bytes", "gleam_detect_workspace_bytes", "gleam_preload", "gleam_rotary_table",
     "gleam_kv_append", "gleam_prefix_attention_ws_bytes", "gleam_prefix_attention", "gleam_draft_tree",
-    "gleam_tree_attention", "gleam_kv_accept", "gleam_kv_weigh", "gleam_kv_evict_ws_bytes", "gleam_kv_evict",
+    "gleam_tree_attention_ws_bytes", "gleam_tree_attention", "gleam_kv_accept", "gleam_kv_weigh", "gleam_kv_evict_ws_bytes", "gleam_kv_evict",
 )
 
 
@@ -121,6 +121,7 @@ def _load() -> ctypes.CDLL:
         "gleam_prefix_attention_ws_bytes": ([kv, batch], sz),
         "gleam_prefix_attention": ([kv, batch, vp, vp, vp, sz, vp], st),
         "gleam_draft_tree": ([vp, vp, u64, u64, vp, u32, vp, vp], st),
+        "gleam_tree_attention_ws_bytes": ([kv, batch], sz),
         "gleam_tree_attention": ([kv, batch, vp, u32, vp, vp, vp, sz, vp], st),
         "gleam_kv_accept": ([kv, ctypes.POINTER(_Accept), vp], st),
         "gleam_kv_weigh": ([kv, ctypes.POINTER(_Weigh), vp], st),
@@ -1105,7 +1106,7 @@ def prefix_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
             lse = q.new_empty((tokens, heads), dtype=torch.float32)
             lse_at = lse.data_ptr()
         if ws is None:
-            ws_bytes = _attention_ws(kv, b)
+            ws_bytes = _attention_ws(kv, b, _seen)
             ws = q.new_empty(ws_bytes, dtype=torch.uint8)
             ws_at = ws.data_ptr()
         else:
@@ -1122,8 +1123,8 @@ def prefix_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
     return out, lse
 
 
-def _attention_ws(kv: _KvPages, b: _PrefixBatch) -> int:
-    n = lib.gleam_prefix_attention_ws_bytes(kv, b)
+def _attention_ws(kv: _KvPages, b: _PrefixBatch, tree=None) -> int:
+    n = lib.gleam_tree_attention_ws_bytes(kv, b) if tree else lib.gleam_prefix_attention_ws_bytes(kv, b)
     if n == 0:
         raise GleamError(E_INVALID, lib.gleam_last_error().decode())
     return n
@@ -1195,11 +1196,19 @@ def tree_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor
 
     The drafts' keys are the last of their sequence's own, in the drafts' order. A token sees its
     group's prefix, the keys before the drafts, and of its sequence's drafts those whose bits are set
-    in its row of seen (int64 [tokens, words], draft_tree()'s or any other). Everything else is
-    prefix_attention()'s, the workspace too."""
+    in its row of seen (int64 [tokens, words], draft_tree()'s or any other). ws: a workspace from
+    tree_attention_workspace(). Everything else is prefix_attention()'s."""
     words = _seen_words(seen, q.shape[0] if isinstance(q, torch.Tensor) and q.dim() else None)
     return prefix_attention(q, k_pages, v_pages, q_first, own_pages, own_len, group_first, prefix_pages, prefix_len,
                             scale, out, lse, want_lse, ws, stream, (seen, words))
+
+
+def tree_attention_workspace(k_pages: torch.Tensor, v_pages: torch.Tensor, tokens: int, q_heads: int, n_seq: int,
+                             n_groups: int = 0) -> torch.Tensor:
+    """A workspace for tree_attention() calls of these shapes on this cache (calls that may overlap need
+    one each)."""
+    b = _PrefixBatch(n_tokens=tokens, n_seq=n_seq, n_groups=n_groups, q_heads=q_heads)
+    return torch.empty(_attention_ws(_kv_struct(k_pages, v_pages), b, True), dtype=torch.uint8, device=k_pages.device)
 
 
 def kv_accept(k_pages: torch.Tensor, v_pages: torch.Tensor, q_first: torch.Tensor, seen: torch.Tensor,

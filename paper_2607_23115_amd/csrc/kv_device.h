@@ -68,11 +68,21 @@ typedef __amdgpu_buffer_rsrc_t Window;
 __device__ inline Window window(const uint8_t* base, bool there) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, (int)uniform(there ? ~0u : 0u), 0x00020000);
 }
-// 16 bytes at the lane's offset and one that is the same in all lanes; kOnce: what nobody reads again soon is not
-// kept in the caches.
-template <bool kOnce>
-__device__ inline u32x4v load_from(Window w, uint32_t lane_offset, uint32_t offset) {
-  return __builtin_amdgcn_raw_buffer_load_b128(w, (int)lane_offset, (int)offset, kOnce ? 2 : 0);
+// 4, 8 or 16 bytes at the lane's offset and one that is the same in all lanes; kOnce: what nobody reads again
+// soon is not kept in the caches.
+template <class V, bool kOnce>
+__device__ inline V load_from(Window w, uint32_t lane_offset, uint32_t offset) {
+  constexpr int kPolicy = kOnce ? 2 : 0;
+  if constexpr (sizeof(V) == 16) return __builtin_amdgcn_raw_buffer_load_b128(w, (int)lane_offset, (int)offset, kPolicy);
+  else if constexpr (sizeof(V) == 8) return __builtin_amdgcn_raw_buffer_load_b64(w, (int)lane_offset, (int)offset, kPolicy);
+  else return __builtin_amdgcn_raw_buffer_load_b32(w, (int)lane_offset, (int)offset, kPolicy);
+}
+
+// Waits for a value here. Where a branch may have asked for it, whatever uses it behind the branch would wait for
+// all loads, those on their way for later among them.
+template <class V>
+__device__ inline void arrived(V& x) {
+  asm volatile("" : "+v"(x));
 }
 
 // Products of 16 x 32 by 32 x 16 values.

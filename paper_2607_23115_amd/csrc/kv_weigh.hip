@@ -99,13 +99,6 @@ __device__ inline uint32_t seen_by(const WeighArgs& a, const Seq& seq, uint32_t 
   return row < seq.tokens * a.ratio && sees > 0 ? (uint32_t)sees : 0;
 }
 
-// Waits for a value here: where a branch may have asked for it, whatever uses it behind the branch would wait
-// for all loads, the keys on their way among them.
-template <class V>
-__device__ inline void arrived(V& x) {
-  asm volatile("" : "+v"(x));
-}
-
 // Rows are loaded whole, and pass through LDS into the products' layout: loads of 64 bytes of 16 rows, straight
 // into it, take the caches four times as many accesses (keys read 15% slower, queries bound many rows).
 template <int D>
@@ -241,7 +234,7 @@ __device__ __forceinline__ void weigh_few(const WeighArgs& a, const Seq& seq, ui
                               p[b] < a.n_pages);
 #pragma unroll
       for (int i = 0; i < kLoads; ++i)
-        kk[set][b][i] = load_from<true>(k, k_off, (uint32_t)(i * St::kLoadRows) * (uint32_t)a.k_place);
+        kk[set][b][i] = load_from<u32x4v, true>(k, k_off, (uint32_t)(i * St::kLoadRows) * (uint32_t)a.k_place);
     }
     const uint32_t key = 32 * half + mine, page = n < 4 ? p[0] : p[1];
     return n < 8 && key < seq.keys && page < a.n_pages

@@ -54,6 +54,11 @@ constexpr uint32_t kMostJoins = 2048;  // workgroups of the others: those that t
 // with 512 an item is cut into twice the pieces: 1.6% slower over twelve cases and fourteen drawn ones, 128
 // sequences behind 8,192 keys 70 us for 58.
 constexpr uint32_t kUnits = 256;
+// Of trees of drafts, which fill few tiles and have long histories: with two a CU one's products go on under the
+// other's softmax, which is worth the pieces (4 sequences of 17 to 48 drafts of 28 heads on 4 behind 60,000 keys 276
+// us with 256, 250 with 512; 32 of up to 62 behind up to 2,000 keys and a prefix 102 and 94), but not of one short
+// sequence (26 rows behind 1,021 keys 16.9 and 18.6).
+constexpr uint32_t kTreeUnits = 512;
 
 struct Item {
   uint32_t token_first, tokens;  // rows: tokens * ratio
@@ -1377,7 +1382,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a) {
 }
 
 // Sets the error text with the call's name; *shape and *args as the kernels take them.
-gleam_status validate_attention(const gleam_kv_pages* kv, const gleam_prefix_batch* b, const char* who,
+gleam_status validate_attention(const gleam_kv_pages* kv, const gleam_prefix_batch* b, bool tree, const char* who,
                                 PlanShape* shape) {
   gleam_status st = validate_kv(kv, who);
   if (st != GLEAM_OK) return st;
@@ -1411,7 +1416,7 @@ gleam_status validate_attention(const gleam_kv_pages* kv, const gleam_prefix_bat
   shape->n_groups = b->n_groups;
   shape->kv_heads = kv->kv_heads;
   shape->ratio = b->q_heads / kv->kv_heads;
-  shape->target = kUnits;
+  shape->target = tree && b->n_tokens * shape->ratio > kMostFew ? kTreeUnits : kUnits;
   shape->head_dim = kv->head_dim;
   const uint64_t most = steps_of((uint32_t)(b->own_width * kv->page_tokens)) +
                         (uint64_t)steps_of((uint32_t)(b->prefix_width * kv->page_tokens));
@@ -1455,7 +1460,7 @@ gleam_status attend_batch(const gleam_kv_pages* kv, const gleam_prefix_batch* b,
                           uint32_t seen_words, void* d_out, float* d_lse, void* d_ws, size_t ws_bytes, void* stream,
                           const char* who) {
   PlanShape shape{};
-  gleam_status st = validate_attention(kv, b, who, &shape);
+  gleam_status st = validate_attention(kv, b, d_seen != nullptr, who, &shape);
   if (st != GLEAM_OK) return st;
   if (b->n_tokens == 0) return GLEAM_OK;
   if ((st = validate_heads(b->d_q, b->q_stride, "q", who)) != GLEAM_OK) return st;
@@ -1540,7 +1545,15 @@ extern "C" size_t gleam_prefix_attention_ws_bytes(const gleam_kv_pages* kv, cons
   using namespace gleam;
   clear_error();
   PlanShape s{};
-  if (validate_attention(kv, b, "gleam_prefix_attention", &s) != GLEAM_OK) return 0;
+  if (validate_attention(kv, b, false, "gleam_prefix_attention", &s) != GLEAM_OK) return 0;
+  return ws_at(nullptr, s, kv->head_dim).bytes;
+}
+
+extern "C" size_t gleam_tree_attention_ws_bytes(const gleam_kv_pages* kv, const gleam_prefix_batch* b) {
+  using namespace gleam;
+  clear_error();
+  PlanShape s{};
+  if (validate_attention(kv, b, true, "gleam_tree_attention", &s) != GLEAM_OK) return 0;
   return ws_at(nullptr, s, kv->head_dim).bytes;
 }
 

@@ -245,7 +245,7 @@ def test_the_same_call_twice_streams_and_graphs():
     side.synchronize()
     assert torch.equal(got, want)
     out, lse = torch.empty_like(a["q"]), torch.empty(a["q"].shape[:2], device="cuda")
-    ws = g.prefix_attention_workspace(a["k_pages"], a["v_pages"], a["q"].shape[0], 8, 4, 1)
+    ws = g.tree_attention_workspace(a["k_pages"], a["v_pages"], a["q"].shape[0], 8, 4, 1)
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         g.tree_attention(**a, out=out, lse=lse, ws=ws)

@@ -80,7 +80,12 @@ def test_tree_attention_that_is_refused(bad):
 def test_tree_attention_limits():
     assert tree_attend(words=65537) == g.E_UNSUPPORTED
     assert tree_attend(n_tokens=1 << 30) == g.E_UNSUPPORTED
-    assert tree_attend(ws_bytes=256) == g.E_WORKSPACE
+    need = [g.lib.gleam_tree_attention_ws_bytes(ctypes.byref(kv()), ctypes.byref(batch(n_tokens=t))) for t in (4, 400)]
+    assert need[0] == g.lib.gleam_prefix_attention_ws_bytes(ctypes.byref(kv()), ctypes.byref(batch()))
+    assert need[1] > g.lib.gleam_prefix_attention_ws_bytes(ctypes.byref(kv()), ctypes.byref(batch(n_tokens=400)))
+    for t, n in zip((4, 400), need):
+        assert tree_attend(n_tokens=t, ws_bytes=n - 1) == g.E_WORKSPACE
+    assert g.lib.gleam_tree_attention_ws_bytes(ctypes.byref(kv(head_dim=96)), ctypes.byref(batch())) == 0
     assert tree_attend(n_tokens=0, seen=None) == g.OK
     assert attend(n_tokens=0) == g.OK
 
