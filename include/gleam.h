@@ -799,7 +799,7 @@ gleam_status gleam_kv_accept(const gleam_kv_pages* kv, const gleam_accept* a, vo
  *   d_weights_out    may be d_weights itself, and must not overlap it otherwise
  *   d_born, d_positions   nullable together; int32[n_tokens] positions
  * Errors: GLEAM_E_INVALID, GLEAM_E_UNSUPPORTED (n_tokens * q_heads of 2^31 or more, more than 2^20
- * sequences), GLEAM_E_HIP.
+ * sequences, places of a page 2^26 elements apart or more), GLEAM_E_HIP.
  *
  * gleam_kv_evict: of sequence s with more than `keep` own keys, each key head keeps `keep`: first those born
  * before `sinks` or in the last `recent` positions before d_total[s], the sequence's tokens so far; then

@@ -1169,8 +1169,8 @@ def draft_tree(parent: torch.Tensor, q_first: torch.Tensor, width: int, seen: to
     if not isinstance(parent, torch.Tensor) or parent.get_device() < 0:
         raise ValueError("parent must be a tensor on the GPU")
     dev, i32 = parent.get_device(), torch.int32
-    if width < 1:
-        raise ValueError("width must be positive")
+    if not 1 <= width <= 1 << 22:
+        raise ValueError("width must be 1 to 2^22 drafts")
     words = (width + 63) // 64
     parent_at, tokens = _flat(parent, "parent", i32, dev), parent.numel()
     first_at = _flat(q_first, "q_first", i32, dev, 1)

@@ -29,7 +29,7 @@ constexpr int kMoveThreads = 256;
 constexpr uint32_t kMoveGroups = 2048;  // of move_kernel
 constexpr uint64_t kMostPairs = 1ull << 36;
 // From this many sequences times heads on a narrow table's workgroups copy their pairs themselves.
-constexpr uint32_t kManyPairs = 128;
+constexpr uint32_t kManyPairs = 256;
 
 struct EvictArgs {
   uint8_t* base[2];  // keys, values
@@ -179,49 +179,90 @@ __device__ inline uint32_t sum_before(uint32_t v, uint32_t* lds, uint32_t* total
   return before + upto - v;
 }
 
-// Longer sequences than registers hold: a run of keys for each thread.
+// Longer sequences than LDS holds: a run of keys for each wave, read again for each count.
+constexpr int kBatch = 8;  // loads of a kind that go out together
+
+// Calls each(i, rank, whether there is such a key) for keys i = from + `step` times 0, 1 ... + `lane`, in order,
+// while from + `step` times that is below `end`. (from, step, end: the same for all that call together.)
+template <class Each>
+__device__ inline void each_rank(const EvictArgs& a, const int32_t* pages, uint32_t head, int64_t late, uint32_t from,
+                                 uint32_t step, uint32_t lane, uint32_t end, const Each& each) {
+#pragma unroll 1
+  for (uint64_t i0 = from; i0 < end; i0 += (uint64_t)step * kBatch) {
+    uint64_t at[kBatch];
+    float w[kBatch];
+    int32_t b[kBatch];
+#pragma unroll
+    for (int r = 0; r < kBatch; ++r) {
+      const uint64_t i = i0 + (uint64_t)r * step + lane;
+      at[r] = (uint32_t)pages[(i < end ? i : i0) >> a.page_log2];
+    }
+#pragma unroll
+    for (int r = 0; r < kBatch; ++r) {
+      const uint64_t i = i0 + (uint64_t)r * step + lane;
+      at[r] = i < end && at[r] < a.n_pages ? (at[r] * a.kv_heads + head) << a.page_log2 | (i & ((1u << a.page_log2) - 1))
+                                           : ~0ull;
+      w[r] = a.weights[at[r] != ~0ull ? at[r] : 0];
+      b[r] = a.born[at[r] != ~0ull ? at[r] : 0];
+    }
+#pragma unroll
+    for (int r = 0; r < kBatch; ++r) {
+      const uint64_t i = i0 + (uint64_t)r * step + lane;
+      each((uint32_t)i, at[r] != ~0ull ? rank_of(a, w[r], b[r], late) : 0, i < end);
+    }
+  }
+}
+
 __device__ void select_long(const EvictArgs& a, const int32_t* pages, uint32_t head, uint32_t keys, int64_t late,
                             uint2* out, uint32_t* bins, uint32_t* lds_sum, uint32_t* moves) {
-  auto rank_at = [&](uint32_t i) {
-    const uint64_t at = tracked_at(a, pages, head, i);
-    return at == ~0ull ? 0u : rank_of(a, a.weights[at], a.born[at], late);
-  };
-  const uint32_t tid = threadIdx.x, threads = blockDim.x, keep = a.keep;
+  const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), keep = a.keep;
   uint32_t known = 0, known_mask = 0, left = keep;
 #pragma unroll 1
   for (int shift = 24; shift >= 0; shift -= 8) {
     uint32_t* const mine = bins + shift / 8 * kBins;
-    for (uint32_t i0 = 0; i0 < keys; i0 += threads) {
-      const uint32_t i = i0 + tid, r = i < keys ? rank_at(i) : 0;
-      count_bins(mine, (r >> shift) & 255, i < keys && (r & known_mask) == known);
-    }
+    each_rank(a, pages, head, late, 0, kThreads, threadIdx.x, keys, [&](uint32_t, uint32_t r, bool there) {
+      count_bins(mine, (r >> shift) & 255, there && (r & known_mask) == known);
+    });
     __syncthreads();
     known |= bin_of(mine, &left).bin << shift;
     known_mask |= 255u << shift;
   }
-  const uint32_t per = (keys + threads - 1) / threads;
-  const uint32_t from = tid * per < keys ? tid * per : keys, to = from + per < keys ? from + per : keys;
+  const uint32_t per = ((keys + kWaves - 1) / kWaves + 63) & ~63u;
+  const uint32_t from = wave * per < keys ? wave * per : keys, to = from + per < keys ? from + per : keys;
+  auto before = [&](bool on) {  // lanes before this one, and all
+    const uint64_t who = __ballot(on);
+    return uint2{__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0)),
+                 (uint32_t)__popcll(who)};
+  };
+  // a wave's count, and all before it
+  auto before_wave = [&](uint32_t count, uint32_t* all) {
+    return uniform(sum_before(lane == 0 ? count : 0, lds_sum, all));
+  };
   uint32_t same = 0, all;
-  for (uint32_t i = from; i < to; ++i) same += rank_at(i) == known;
-  const uint32_t same_before = sum_before(same, lds_sum, &all);
+  each_rank(a, pages, head, late, from, 64, lane, to,
+            [&](uint32_t, uint32_t r, bool there) { same += before(there && r == known).y; });
+  const uint32_t same_before = before_wave(same, &all);
+  auto flag = [&](uint32_t i, uint32_t r, bool there) {  // of a place that comes free, or a key that moves
+    const bool equal = there && r == known;
+    const uint2 n = before(equal);
+    const bool kept = r > known || (equal && same + n.x < left);
+    same += n.y;
+    return there && kept != (i < keep);
+  };
   uint32_t count = 0;
   same = same_before;
-  for (uint32_t i = from; i < to; ++i) {
-    const uint32_t r = rank_at(i);
-    const bool kept = r > known || (r == known && same++ < left);
-    count += i < keep ? !kept : kept;
-  }
-  uint32_t at = sum_before(count, lds_sum, &all);
-  *moves = all / 2;
+  each_rank(a, pages, head, late, from, 64, lane, to,
+            [&](uint32_t i, uint32_t r, bool there) { count += before(flag(i, r, there)).y; });
+  uint32_t at = before_wave(count, &all);
+  *moves = all / 2;  // free places all lie before keep, moving keys behind: as many of both
   same = same_before;
-  for (uint32_t i = from; i < to; ++i) {
-    const uint32_t r = rank_at(i);
-    const bool kept = r > known || (r == known && same++ < left);
-    if (i < keep ? kept : !kept) continue;
-    // free places all lie before keep, moving keys behind: as many of both
-    if (i < keep) out[at++].y = i;
-    else out[at++ - *moves].x = i;
-  }
+  each_rank(a, pages, head, late, from, 64, lane, to, [&](uint32_t i, uint32_t r, bool there) {
+    const bool on = flag(i, r, there);
+    const uint2 n = before(on);
+    if (on && i < keep) out[at + n.x].y = i;
+    if (on && i >= keep) out[at + n.x - *moves].x = i;
+    at += n.y;
+  });
 }
 
 // How many of the workgroup's keys with a flag come before a thread's key number r, in the keys' order. counts:

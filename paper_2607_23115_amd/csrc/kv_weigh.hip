@@ -39,8 +39,15 @@ struct WeighArgs {
   const int32_t* positions;
   uint32_t n_tokens, n_seq, own_width;
   uint32_t q_heads, kv_heads, ratio, page_log2, n_pages;
+  uint32_t ratio_mul, ratio_shift;
   float scale_log2;
 };
+
+// row / ratio of rows below 2^31: 2 row times 2^(31 + s) / ratio rounded up, 2^s the power of two that ratio is
+// not above.
+__device__ inline uint32_t token_of(const WeighArgs& a, uint32_t row) {
+  return __umulhi(2 * row, a.ratio_mul) >> a.ratio_shift;
+}
 
 // A sequence as a wave finds it: of its keys, units of the two kinds for each head.
 struct Seq {
@@ -95,7 +102,7 @@ __device__ inline void add_weights(const f32x4& score, float scale, float down, 
 
 // How many keys a row sees: none where there is no such row.
 __device__ inline uint32_t seen_by(const WeighArgs& a, const Seq& seq, uint32_t row) {
-  const int64_t sees = (int64_t)seq.keys - seq.tokens + row / a.ratio + 1;
+  const int64_t sees = (int64_t)seq.keys - seq.tokens + token_of(a, row) + 1;
   return row < seq.tokens * a.ratio && sees > 0 ? (uint32_t)sees : 0;
 }
 
@@ -140,8 +147,9 @@ struct Rows {
     const uint32_t last = seq.tokens * a.ratio - 1;
     auto of = [&](uint32_t r, uint64_t* h) {
       if (r > last) r = last;
-      *h = head * a.ratio + r % a.ratio;
-      return seq.first + (uint64_t)(r / a.ratio);
+      const uint32_t token = token_of(a, r);
+      *h = head * a.ratio + (r - token * a.ratio);
+      return seq.first + (uint64_t)token;
     };
     uint64_t h;
 #pragma unroll
@@ -319,16 +327,30 @@ __device__ __forceinline__ void weigh_many(const WeighArgs& a, const Seq& seq, u
   const bool has = (n >> 2) < kTiles && own < seq.keys;
   const uint32_t page = has ? (uint32_t)a.own_pages[(uint64_t)s * a.own_width + (own >> a.page_log2)] : kNoPage;
   const uint32_t place_mask = (1u << a.page_log2) - 1;
+  // The keys come by way of LDS too, each wave bringing some of the rows.
+  char* const lds_k = lds + kWaves<D> * St::kTile;
+  constexpr int kBring = kTiles * St::kLoads / kWaves<D>;
+  u32x4v bring[kBring];
+#pragma unroll
+  for (int i = 0; i < kBring; ++i) {
+    const uint32_t load = wave * kBring + i, t = load / St::kLoads, row = load % St::kLoads * St::kLoadRows;
+    uint32_t p = (uint32_t)__builtin_amdgcn_readlane((int)page, (int)(4 * t));
+    if (p >= a.n_pages) p = 0;  // not stored
+    bring[i] = load_at<u32x4v>(a.k + (int64_t)p * a.k_page + (int64_t)(((key0 + 16 * t) & place_mask) + row) * a.k_place +
+                                   (int64_t)head * a.k_head,
+                               St::load_row() * (uint32_t)a.k_place + St::piece() * 16);
+  }
+#pragma unroll
+  for (int i = 0; i < kBring; ++i) {
+    const uint32_t load = wave * kBring + i, t = load / St::kLoads, row = load % St::kLoads * St::kLoadRows;
+    *reinterpret_cast<u32x4v*>(lds_k + t * St::kTile + St::at(row + St::load_row(), St::piece())) = bring[i];
+  }
+  __syncthreads();
   Pack8 k[kTiles][kSteps];
 #pragma unroll
-  for (int t = 0; t < kTiles; ++t) {
-    uint32_t p = (uint32_t)__builtin_amdgcn_readlane((int)page, 4 * t);
-    if (p >= a.n_pages) p = 0;  // not stored
-    const uint8_t* const at = a.k + (int64_t)p * a.k_page + (int64_t)((key0 + 16 * t) & place_mask) * a.k_place +
-                              (int64_t)head * a.k_head + n * a.k_place + g * 16;
+  for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) k[t][i].u = *reinterpret_cast<const u32x4v*>(at + i * 64);
-  }
+    for (int i = 0; i < kSteps; ++i) k[t][i] = St::read(lds_k + t * St::kTile, St::at(n, g), i);
   float acc[kTiles][4] = {};
   const uint32_t rows = seq.tokens * a.ratio;
   // the first row that sees the first key, and from where on all see all keys
@@ -400,7 +422,7 @@ __device__ __forceinline__ void weigh_many(const WeighArgs& a, const Seq& seq, u
       const float x = sum_of_16(acc[t][e]);
       if (n == 4 * t + e) sum = x;
     }
-  float(*const sums)[64] = reinterpret_cast<float(*)[64]>(lds + kWaves<D> * St::kTile);
+  float(*const sums)[64] = reinterpret_cast<float(*)[64]>(lds + (kWaves<D> + kTiles) * St::kTile);
   sums[wave][lane] = sum;
   __syncthreads();
   if (wave == 0 && has && page < a.n_pages) {
@@ -418,7 +440,9 @@ __device__ __forceinline__ void weigh_many(const WeighArgs& a, const Seq& seq, u
 // Each wave finds its work by walking over the sequences' lengths, 64 a step.
 template <class T, int D>
 __global__ __launch_bounds__(64 * kWaves<D>) void weigh_kernel(WeighArgs a) {
+  // few rows: kBytes a wave; many: a tile of rows a wave, the keys, and sums
   __shared__ __attribute__((aligned(16))) char lds[kWaves<D> * Staged<D>::kBytes];
+  static_assert((kWaves<D> + kBlock<D> / 16) * Staged<D>::kTile + kWaves<D> * 256 <= sizeof(lds), "");
   const uint32_t lane = threadIdx.x & 63;
   uint64_t blocks = 0, halves = 0;
   Seq mine{};
@@ -572,6 +596,8 @@ extern "C" gleam_status gleam_kv_weigh(const gleam_kv_pages* kv, const gleam_wei
   a.q_heads = in->q_heads;
   a.kv_heads = kv->kv_heads;
   a.ratio = in->q_heads / kv->kv_heads;
+  while (1u << a.ratio_shift < a.ratio) ++a.ratio_shift;
+  a.ratio_mul = (uint32_t)((1ull << (31 + a.ratio_shift)) / a.ratio + 1);
   a.page_log2 = (uint32_t)log2_exact(kv->page_tokens);
   a.n_pages = (uint32_t)kv->n_pages;
   a.scale_log2 = in->scale * kLog2e;

@@ -77,6 +77,30 @@ def test_parents_and_offsets_that_make_no_sense():
             assert torch.equal(seen.cpu(), want) and torch.equal(depth.cpu(), deep)
 
 
+def test_tree_refusals_and_streams():
+    parent, first = forest([13, 20], 1).cuda(), i32([0, 13, 33]).cuda()
+    for message, bad in (("width must be", dict(width=0)), ("width must be", dict(width=(1 << 22) + 1)),
+                         ("parent must be", dict(parent=parent.long())), ("on the GPU", dict(parent=parent.cpu())),
+                         ("q_first", dict(q_first=first.long())), ("q_first", dict(q_first=first[:0])),
+                         ("seen must be", dict(seen=torch.empty(33, 2, dtype=torch.int64, device="cuda"))),
+                         ("seen must be", dict(seen=torch.empty(33, 1, dtype=torch.int32, device="cuda"))),
+                         ("depth holds", dict(depth=torch.empty(32, dtype=torch.int32, device="cuda")))):
+        with pytest.raises(ValueError, match=message):
+            g.draft_tree(**{**dict(parent=parent, q_first=first, width=20), **bad})
+    want, deep = B.tree(parent.cpu(), first.cpu(), 1)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    say("draft_tree stream")
+    seen, depth = g.draft_tree(parent, first, 20, stream=side)
+    side.synchronize()
+    assert torch.equal(seen.cpu(), want) and torch.equal(depth.cpu(), deep)
+    none = torch.empty(0, dtype=torch.int32, device="cuda")
+    seen, depth = g.draft_tree(none, i32([0]).cuda(), 5)
+    assert seen.shape == (0, 1) and depth.shape == (0,)
+    seen, depth = g.draft_tree(parent, i32([0]).cuda(), 5)  # no sequences: tokens of none
+    assert (seen == 0).all() and (depth == 0).all()
+
+
 def test_many_trees_and_a_captured_call():
     n = [1 + i % 70 for i in range(3000)]
     parent, first = forest(n, 5), first_of(n)

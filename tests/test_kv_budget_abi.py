@@ -119,6 +119,7 @@ def test_weights_that_are_refused(bad):
 def test_weigh_limits():
     assert weigh(n_tokens=1 << 30) == g.E_UNSUPPORTED
     assert weigh(n_seq=(1 << 20) + 1) == g.E_UNSUPPORTED
+    assert weigh(kv(k_stride=(1 << 40, 1 << 26, 64))) == g.E_UNSUPPORTED
     for nothing in ({"n_seq": 0}, {"own_width": 0}):
         assert weigh(**nothing) == g.OK
     assert weigh(kv(n_pages=0)) == g.OK
