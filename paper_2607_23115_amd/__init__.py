@@ -1176,12 +1176,17 @@ def draft_tree(parent: torch.Tensor, q_first: torch.Tensor, width: int, seen: to
     first_at = _flat(q_first, "q_first", i32, dev, 1)
     with _on_stream(stream, parent.device) as hs:
         if seen is None:
-            seen = torch.empty((tokens, words), dtype=torch.int64, device=parent.device)
+            seen = parent.new_empty((tokens, words), dtype=torch.int64)
+            seen_at = seen.data_ptr()
         elif _seen_words(seen, tokens) != words:
             raise ValueError(f"seen must be [{tokens}, {words}]")
+        else:
+            seen_at = _flat(seen, "seen", torch.int64, dev)
         if depth is None:
             depth = torch.empty_like(parent)
-        seen_at, depth_at = _flat(seen, "seen", torch.int64, dev), _flat(depth, "depth", i32, dev, tokens)
+            depth_at = depth.data_ptr()
+        else:
+            depth_at = _flat(depth, "depth", i32, dev, tokens)
         _check(lib.gleam_draft_tree(parent_at, first_at, tokens, q_first.numel() - 1, seen_at, words, depth_at, hs))
     return seen, depth
 
@@ -1317,7 +1322,7 @@ def kv_evict(k_pages: torch.Tensor, v_pages: torch.Tensor, own_pages: torch.Tens
                       sinks, recent)
         if ws is None:
             ws_bytes = _evict_ws(kv, args)
-            ws = torch.empty(ws_bytes, dtype=torch.uint8, device=k_pages.device)
+            ws = weights.new_empty(ws_bytes, dtype=torch.uint8)
             ws_at = ws.data_ptr()
         else:
             ws_at, ws_bytes = _flat(ws, "ws", torch.uint8, dev), ws.numel()

@@ -54,11 +54,11 @@ constexpr uint32_t kMostJoins = 2048;  // workgroups of the others: those that t
 // with 512 an item is cut into twice the pieces: 1.6% slower over twelve cases and fourteen drawn ones, 128
 // sequences behind 8,192 keys 70 us for 58.
 constexpr uint32_t kUnits = 256;
-// Of trees of drafts, which fill few tiles and have long histories: with two a CU one's products go on under the
-// other's softmax, which is worth the pieces (4 sequences of 17 to 48 drafts of 28 heads on 4 behind 60,000 keys 276
-// us with 256, 250 with 512; 32 of up to 62 behind up to 2,000 keys and a prefix 102 and 94), but not of one short
-// sequence (26 rows behind 1,021 keys 16.9 and 18.6).
-constexpr uint32_t kTreeUnits = 512;
+// Of trees of drafts, where chunks stay long: two a CU, so that one's products go on under the other's softmax, and
+// some fewer than the CUs hold, as items are cut into whole chunks (4 sequences of 17 to 48 drafts of 28 heads on 4
+// behind 60,000 keys: 288 us with 256, 260 with 512, of which 16 had to wait, 220 with 480; 3 of 30 behind 8,000 to
+// 20,000, whose chunks would be of 10 steps, 43 and 62).
+constexpr uint32_t kTreeUnits = 480;
 
 struct Item {
   uint32_t token_first, tokens;  // rows: tokens * ratio
@@ -104,7 +104,7 @@ struct AttendArgs {
   const uint32_t* seen;  // of trees of drafts: [n_tokens][seen_words]
   uint32_t seen_words;
   uint32_t n_tokens, n_seq, n_groups, own_width, prefix_width;
-  uint32_t q_heads, kv_heads, ratio, page_log2, n_pages, target, head_dim;
+  uint32_t q_heads, kv_heads, ratio, page_log2, n_pages, target, target_long, head_dim;
   float scale_log2;
   uint8_t* out;
   float* lse;
@@ -230,7 +230,7 @@ struct Takes {
 __device__ inline Takes cut_item(const AttendArgs& a, Item& it, const Costs& cost) {
   const uint32_t rows = it.tokens * a.ratio;
   const Cut cut = cut_steps(item_steps(it), chunk_steps(rows, few_rows(rows) ? cost.fews : cost.tiles, a.target,
-                                                    a.head_dim));
+                                                    a.head_dim, a.target_long));
   it.chunks = cut.chunks;
   it.per = cut.per;
   if (cut.chunks > 1) it.partial = 1;
@@ -1416,7 +1416,8 @@ gleam_status validate_attention(const gleam_kv_pages* kv, const gleam_prefix_bat
   shape->n_groups = b->n_groups;
   shape->kv_heads = kv->kv_heads;
   shape->ratio = b->q_heads / kv->kv_heads;
-  shape->target = tree && b->n_tokens * shape->ratio > kMostFew ? kTreeUnits : kUnits;
+  // (heads of 256 have one workgroup a CU, and without rows for a tile there are none)
+  shape->target = tree && kv->head_dim < 256 && b->n_tokens * shape->ratio > kMostFew ? kTreeUnits : kUnits;
   shape->head_dim = kv->head_dim;
   const uint64_t most = steps_of((uint32_t)(b->own_width * kv->page_tokens)) +
                         (uint64_t)steps_of((uint32_t)(b->prefix_width * kv->page_tokens));
@@ -1513,7 +1514,8 @@ gleam_status attend_batch(const gleam_kv_pages* kv, const gleam_prefix_batch* b,
   a.ratio = shape.ratio;
   a.page_log2 = (uint32_t)log2_exact(kv->page_tokens);
   a.n_pages = (uint32_t)kv->n_pages;
-  a.target = shape.target;
+  a.target = kUnits;
+  a.target_long = shape.target > kUnits ? shape.target : 0;
   a.head_dim = kv->head_dim;
   a.scale_log2 = b->scale * kLog2e;
   a.out = static_cast<uint8_t*>(d_out);

@@ -35,7 +35,7 @@ GLEAM_HD uint32_t min_tile_steps(uint32_t head_dim) { return 512 / head_dim; }
 struct PlanShape {  // what the host knows
   uint64_t n_tokens, n_seq, n_groups;
   uint32_t kv_heads, ratio;  // ratio: query heads per key head
-  uint32_t target;           // units of each kind wanted (kUnits of the launch)
+  uint32_t target;           // units of each kind wanted, the most of them where there is a choice
   uint32_t most_steps;       // of an item, from the widths of the page tables
   uint32_t head_dim;
 };
@@ -56,9 +56,14 @@ GLEAM_HD uint32_t tiles_of(uint32_t rows) {
 GLEAM_HD uint64_t item_cost(uint32_t rows, uint32_t steps) { return (uint64_t)tiles_of(rows) * steps; }
 
 // Steps of a chunk of an item of `rows` rows: no more than `target` chunks of all tiles of a kind
-// together, apart from each tile's first. `cost`: of all items of the kind, all key heads.
-GLEAM_HD uint32_t chunk_steps(uint32_t rows, uint64_t cost, uint32_t target, uint32_t head_dim) {
-  const uint64_t c = div_up(cost, target), least = few_rows(rows) ? kMinFewSteps : min_tile_steps(head_dim);
+// together, apart from each tile's first. `cost`: of all items of the kind, all key heads. `target_long`:
+// more of the second kind, where chunks of that many have kLongChunk steps all the same (0: never).
+constexpr uint32_t kLongChunk = 20;
+GLEAM_HD uint32_t chunk_steps(uint32_t rows, uint64_t cost, uint32_t target, uint32_t head_dim,
+                              uint32_t target_long = 0) {
+  uint64_t c = div_up(cost, target);
+  if (target_long && !few_rows(rows) && div_up(cost, target_long) >= kLongChunk) c = div_up(cost, target_long);
+  const uint64_t least = few_rows(rows) ? kMinFewSteps : min_tile_steps(head_dim);
   return c < least ? (uint32_t)least : c > 0x7fffffffu ? 0x7fffffffu : (uint32_t)c;
 }
 
