@@ -270,8 +270,9 @@ __device__ void select_long(const EvictArgs& a, const int32_t* pages, uint32_t h
 template <int kKeys>
 struct Ordered {
   static constexpr int kEntries = kKeys * kWaves / 64;  // a lane's
-  uint32_t flags;  // of the thread's keys, a bit each
-  uint32_t before[kEntries];
+  static_assert(kWaves % kEntries == 0, "");
+  uint32_t flags;   // of the thread's keys, a bit each
+  uint32_t before;  // of the entries number wave % kEntries of each lane's
   uint32_t all;
 
   __device__ void count(uint32_t* counts) {
@@ -285,23 +286,20 @@ struct Ordered {
     if (lane < kKeys) counts[lane * kWaves + wave] = mine;
     __syncthreads();
     uint32_t sum = 0;
+    before = 0;
 #pragma unroll
     for (int i = 0; i < kEntries; ++i) {
-      before[i] = sum;
+      if (wave % kEntries == (uint32_t)i) before = sum;
       sum += counts[lane * kEntries + i];
     }
     const uint32_t upto = wave_scan(sum, SumOp());
     all = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
-#pragma unroll
-    for (int i = 0; i < kEntries; ++i) before[i] += upto - sum;
+    before += upto - sum;
   }
   // (by whole waves)
   __device__ uint32_t of(uint32_t r) const {
-    const uint32_t wave = uniform(threadIdx.x >> 6), entry = r * kWaves + wave;
-    uint32_t x = 0;
-#pragma unroll
-    for (int i = 0; i < kEntries; ++i)  // one of them, chosen by the wave's number
-      if (entry % kEntries == (uint32_t)i) x = (uint32_t)__builtin_amdgcn_readlane((int)before[i], (int)(entry / kEntries));
+    const uint32_t wave = uniform(threadIdx.x >> 6);
+    const uint32_t x = (uint32_t)__builtin_amdgcn_readlane((int)before, (int)((r * kWaves + wave) / kEntries));
     const uint64_t who = __ballot(flags >> r & 1);
     return x + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
   }
