@@ -24,7 +24,8 @@ constexpr int kThreads = 1024, kWaves = kThreads / 64;
 // Keys of a thread, in LDS: for tables of up to 4,096 keys, and for wider ones. Longer sequences than those
 // hold read their weights again for each count.
 constexpr int kNarrowKeys = 4, kWideKeys = 32;
-constexpr uint32_t kBins = 256;
+// Counts of a round, in four copies: weights have few exponents, and lanes that add to the same count wait.
+constexpr uint32_t kBins = 256, kCopies = 4, kRound = kBins * kCopies;
 constexpr int kMoveThreads = 256;
 constexpr uint32_t kMoveGroups = 2048;  // of move_kernel
 constexpr uint64_t kMostPairs = 1ull << 36;
@@ -134,7 +135,9 @@ struct Found {
 };
 __device__ inline Found bin_of(const uint32_t* bins, uint32_t* left) {
   const uint32_t lane = threadIdx.x & 63;
-  const u32x4v c = *reinterpret_cast<const u32x4v*>(bins + kBins - 4 * (lane + 1));
+  u32x4v c = (u32x4v)0u;
+#pragma unroll
+  for (uint32_t i = 0; i < kCopies; ++i) c += *reinterpret_cast<const u32x4v*>(bins + (i + 1) * kBins - 4 * (lane + 1));
   const uint32_t sum = c[0] + c[1] + c[2] + c[3], upto = wave_scan(sum, SumOp());
   const uint32_t at = uniform((uint32_t)__builtin_ctzll(__ballot(upto >= *left)));
   uint32_t rest = *left - (upto - sum), bin = kBins - 4 * lane - 1, count = c[3];  // of lane `at` these hold
@@ -154,12 +157,12 @@ __device__ inline Found bin_of(const uint32_t* bins, uint32_t* left) {
 // for all, it is added to once.
 __device__ inline void count_bins(uint32_t* bins, uint32_t bin, bool counts) {
   if (!counts) return;
-  const uint32_t lead = uniform(bin);
+  const uint32_t copy = threadIdx.x % kCopies * kBins, lead = uniform(bin);
   if (__ballot(bin != lead) == 0) {
     const uint64_t who = __ballot(true);
     if ((threadIdx.x & 63) == (uint32_t)__builtin_ctzll(who)) atomicAdd(&bins[lead], (uint32_t)__popcll(who));
   } else {
-    atomicAdd(&bins[bin], 1u);
+    atomicAdd(&bins[copy + bin], 1u);
   }
 }
 
@@ -219,7 +222,7 @@ __device__ void select_long(const EvictArgs& a, const int32_t* pages, uint32_t h
   uint32_t known = 0, known_mask = 0, left = keep;
 #pragma unroll 1
   for (int shift = 24; shift >= 0; shift -= 8) {
-    uint32_t* const mine = bins + shift / 8 * kBins;
+    uint32_t* const mine = bins + shift / 8 * kRound;
     each_rank(a, pages, head, late, 0, kThreads, threadIdx.x, keys, [&](uint32_t, uint32_t r, bool there) {
       count_bins(mine, (r >> shift) & 255, there && (r & known_mask) == known);
     });
@@ -309,7 +312,7 @@ template <int D, int kKeys>
 __global__ __launch_bounds__(kThreads, kKeys == kNarrowKeys ? 8 : 4) void select_kernel(EvictArgs a) {
   constexpr bool kNarrow = kKeys == kNarrowKeys;
   constexpr int kGroup = kNarrow ? 4 : 8;  // loads of a kind that go out together
-  __shared__ __attribute__((aligned(16))) uint32_t rank[kKeys * kThreads], bins[4 * kBins];
+  __shared__ __attribute__((aligned(16))) uint32_t rank[kKeys * kThreads], bins[4 * kRound];
   __shared__ uint32_t counts[2][kKeys * kWaves];
   const uint32_t tid = threadIdx.x;
   for (uint32_t pair = blockIdx.x; pair < a.n_seq * a.kv_heads; pair += gridDim.x) {
@@ -326,7 +329,7 @@ __global__ __launch_bounds__(kThreads, kKeys == kNarrowKeys ? 8 : 4) void select
     const uint32_t keys = keys_of(a, s), keep = a.keep < keys ? a.keep : keys;
     const int64_t late = (int64_t)a.total[s] - a.recent;
     if (head == 0 && tid == 0) a.len_out[s] = (int32_t)keep;
-    if (tid < 4 * kBins) bins[tid] = 0;
+    for (uint32_t i = tid; i < 4 * kRound; i += kThreads) bins[i] = 0;
 
     // What stays where it is is written on, and the others' places by who copies pairs. For no key a first one's
     // weight is loaded.
@@ -369,7 +372,7 @@ __global__ __launch_bounds__(kThreads, kKeys == kNarrowKeys ? 8 : 4) void select
       uint32_t known = 0, known_mask = 0, left = keep, same = 0;  // same: keys of the last kept one's rank
 #pragma unroll 1
       for (int shift = 24; shift >= 0; shift -= 8) {
-        uint32_t* const mine = bins + shift / 8 * kBins;
+        uint32_t* const mine = bins + shift / 8 * kRound;
 #pragma unroll 4
         for (uint32_t i0 = 0; i0 < keys; i0 += kThreads) {
           const uint32_t r = rank[i0 + tid];  // (of no key, of none of these bits or not counted)
