@@ -113,7 +113,8 @@ struct Staged {
   static constexpr uint32_t kPieces = D / 8, kLoadRows = 64 / kPieces;  // 16-byte pieces of a row, rows of a load
   static constexpr int kLoads = 16 / kLoadRows;                         // of 16 rows
   static constexpr uint32_t kTile = 16 * 2 * D;                         // bytes of 16 rows
-  static constexpr uint32_t kBytes = 2 * kTile;                         // of a wave
+  static constexpr int kHeld = 3;                                       // tiles of few rows that stay in LDS
+  static constexpr uint32_t kBytes = (1 + kHeld) * kTile;               // of a wave
   // rows of one piece each, or of one row all pieces, fall into different banks
   static __device__ uint32_t at(uint32_t row, uint32_t piece) {
     return row * (2 * D) + ((piece ^ (D == 64 ? (row >> 1) & 7 : row & 15)) << 4);
@@ -212,6 +213,21 @@ __device__ __forceinline__ void weigh_few(const WeighArgs& a, const Seq& seq, ui
     seen = seen_by(a, seq, kRows * tile + n);
   };
   if (tiles == 1) take_rows(0);
+  // a few tiles of rows stay in LDS
+  float held_down[St::kHeld];
+  uint32_t held_seen[St::kHeld];
+  const bool held = tiles > 1 && tiles <= St::kHeld;
+#pragma unroll
+  for (int t = 0; t < St::kHeld; ++t) {
+    held_down[t] = 0.f;
+    held_seen[t] = 0;
+    if (!held || (uint32_t)t >= tiles) continue;
+    r.find(a, seq, head, kRows * t);
+    r.load();
+    St::store(lds + (1 + t) * St::kTile, r.q);
+    held_down[t] = -r.lse * kLog2e;
+    held_seen[t] = seen_by(a, seq, kRows * t + n);
+  }
 
   // pages of 16 keys each, 64 of them ahead, a lane each
   auto pages_from = [&](uint32_t half) {
@@ -257,7 +273,7 @@ __device__ __forceinline__ void weigh_few(const WeighArgs& a, const Seq& seq, ui
   auto add = [&](uint32_t half, auto set_) {
     constexpr int set = decltype(set_)::value;
     float acc[2][4] = {};
-    uint64_t next;
+    uint64_t next = ~0ull;
     auto products = [&](const char* keys, int b) {
       f32x4 score = (f32x4)0.f;
 #pragma unroll
@@ -270,6 +286,21 @@ __device__ __forceinline__ void weigh_few(const WeighArgs& a, const Seq& seq, ui
       next = load(half + 2, set_);
 #pragma unroll
       for (int b = 0; b < 2; ++b) products(lds + b * St::kTile, b);
+    } else if (held) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        St::store(lds, kk[set][b]);
+        if (b == 1) next = load(half + 2, set_);
+#pragma unroll
+        for (int t = 0; t < St::kHeld; ++t) {
+          if ((uint32_t)t >= tiles) continue;
+#pragma unroll
+          for (int i = 0; i < kSteps; ++i) q[i] = St::read(lds + (1 + t) * St::kTile, from_lds, i);
+          down = held_down[t];
+          seen = held_seen[t];
+          products(lds, b);
+        }
+      }
     } else {
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
