@@ -65,10 +65,10 @@ __device__ inline uint64_t tracked_at(const EvictArgs& a, const int32_t* pages, 
   return ((uint64_t)page * a.kv_heads + head) << a.page_log2 | (i & ((1u << a.page_log2) - 1));
 }
 
-// A larger number for a larger weight: 0 for NaN, -0 as 0.
+// A larger number for a larger weight: 1 for NaN (0 is a key's in a page that is none), -0 as 0.
 __device__ inline uint32_t order_of(float w) {
   const uint32_t b = __float_as_uint(w + 0.f);
-  return w != w ? 0 : b ^ ((b >> 31) ? ~0u : 0x80000000u);
+  return w != w ? 1 : b ^ ((b >> 31) ? ~0u : 0x80000000u);
 }
 
 // What a key counts for: ~0 for one that is kept whatever its weight.

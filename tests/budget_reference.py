@@ -146,7 +146,7 @@ def evict(k_pages, v_pages, own_pages, own_len, weights, born, total, keep, sink
             def rank(j):
                 p, i = mine[j]
                 if not 0 <= p < pages:
-                    return (2, 0.0, j)
+                    return (3, 0.0, j)
                 x, at = float(weights[p, h, i]), int(born[p, h, i])
                 if at < sinks or at >= int(total[s]) - recent:
                     return (0, 0.0, j)

@@ -340,6 +340,19 @@ def test_many_sequences_and_heads_of_narrow_tables(d):
     Evicted([4000, 3100, 1, 0, 2049, 2047, 4064, 2500], 16, d, 32, F16, 2048, sinks=3, recent=100).check()
 
 
+@pytest.mark.parametrize("own,keep", [(100, 90), (5000, 4990), (40000, 39990)])
+def test_missing_pages_go_before_nan(own, keep):
+    """Ten keys of 16 in a page that is none go, and none of the NaN weights in the page behind it."""
+    c = Evicted([own], 2, 64, 16, F16, keep)
+    gone, behind = int(c.own_pages[0, 1]), int(c.own_pages[0, 2])
+    c.weights[gone], c.born[gone] = math.nan, -9
+    c.weights[behind] = math.nan
+    c.own_pages[0, 1] = -1
+    before = c.kp.clone()
+    c.check()
+    assert torch.equal(bits(c.want()[0][behind]), bits(before[behind]))
+
+
 def test_missing_pages():
     c = Evicted([100, 90], 2, 64, 16, F16, 40, recent=5)
     c.own_pages[0, 1], c.own_pages[0, 5], c.own_pages[1, 3] = -1, c.kp.shape[0], 1 << 30
