@@ -50,7 +50,8 @@ EXPORTS = (
     "gleam_detect_ws_init", "gleam_identify_leaves", "gleam_first_writes_ws_bytes", "gleam_first_writes",
     "gleam_cache_erase_bytes", "gleam_detect_workspace_bytes", "gleam_preload", "gleam_rotary_table",
     "gleam_kv_append", "gleam_prefix_attention_ws_bytes", "gleam_prefix_attention", "gleam_draft_tree",
-    "gleam_tree_attention_ws_bytes", "gleam_tree_attention", "gleam_kv_accept", "gleam_kv_weigh", "gleam_kv_evict_ws_bytes", "gleam_kv_evict",
+    "gleam_tree_attention_ws_bytes", "gleam_tree_attention", "gleam_kv_accept", "gleam_kv_weigh",
+    "gleam_kv_evict_ws_bytes", "gleam_kv_evict",
 )
 
 
