@@ -364,6 +364,8 @@ __device__ __forceinline__ void weigh_many(const WeighArgs& a, const Seq& seq, u
   const bool has = (n >> 2) < kTiles && own < seq.keys;
   const uint32_t page = has ? (uint32_t)a.own_pages[(uint64_t)s * a.own_width + (own >> a.page_log2)] : kNoPage;
   const uint32_t place_mask = (1u << a.page_log2) - 1;
+  const bool stored = has && page < a.n_pages;
+  const uint64_t to = ((uint64_t)(stored ? page : 0) * a.kv_heads + head) << a.page_log2 | (own & place_mask);
   // The keys come by way of LDS too, each wave bringing some of the rows.
   char* const lds_k = lds + kWaves<D> * St::kTile;
   constexpr int kBring = kTiles * St::kLoads / kWaves<D>;
@@ -377,6 +379,7 @@ __device__ __forceinline__ void weigh_many(const WeighArgs& a, const Seq& seq, u
                                    (int64_t)head * a.k_head,
                                St::load_row() * (uint32_t)a.k_place + St::piece() * 16);
   }
+  const float old = a.weights[to];  // (some weight, where none is needed)
 #pragma unroll
   for (int i = 0; i < kBring; ++i) {
     const uint32_t load = wave * kBring + i, t = load / St::kLoads, row = load % St::kLoads * St::kLoadRows;
@@ -462,16 +465,15 @@ __device__ __forceinline__ void weigh_many(const WeighArgs& a, const Seq& seq, u
   float(*const sums)[64] = reinterpret_cast<float(*)[64]>(lds + (kWaves<D> + kTiles) * St::kTile);
   sums[wave][lane] = sum;
   __syncthreads();
-  if (wave == 0 && has && page < a.n_pages) {
-    sum = 0.f;
+  if (wave == 0 && stored) {
+    sum = own < base ? old : 0.f;
+    float added = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves<D>; ++w) sum += sums[w][lane];
-    const uint64_t to = ((uint64_t)page * a.kv_heads + head) << a.page_log2 | (own & place_mask);
-    if (own < base) sum += a.weights[to];
-    a.weights_out[to] = sum;
+    for (int w = 0; w < kWaves<D>; ++w) added += sums[w][lane];
+    a.weights_out[to] = sum + added;
     if (a.born && own >= base) a.born[to] = a.positions[seq.first + (uint32_t)(own - base)];
   }
-  __syncthreads();
+  // No barrier: the next call's keys are written once all have read these, and its sums behind its first barrier.
 }
 
 // Each wave finds its work by walking over the sequences' lengths, 64 a step.
@@ -516,6 +518,7 @@ __global__ __launch_bounds__(64 * kWaves<D>) void weigh_kernel(WeighArgs a) {
       }
       before += all;
     }
+    __syncthreads();  // what follows uses the same LDS otherwise
   }
   if (halves) {
     const uint64_t waves = (uint64_t)gridDim.x * kWaves<D>, wave = (uint64_t)blockIdx.x * kWaves<D> + uniform(threadIdx.x >> 6);
