@@ -7,9 +7,10 @@
 // its keys' exponentials, and the 16 lanes of the same keys add theirs up at the end.
 //   few rows   a wave for itself streams through 32 keys at a time, the next 32 on their way during the
 //              products. All halves of 64 keys of all sequences and heads are dealt out evenly, in order, so
-//              that lengths do not matter. Up to three tiles of rows stay in LDS. The time is that of reading
-//              the keys: 64 sequences of 500 to 4,000, 8 heads of 128, 201 MB in all, 37 us (5.4 TB/s; a plain
-//              read reaches 7.1), of which 4 to 5 go by before the first keys arrive.
+//              that lengths do not matter. Up to three tiles of rows stay in LDS; more are loaded again for each
+//              32 keys, and waited for (64 sequences of 1,500 keys, 5 tiles: 90 us, 3: 45). With few tiles the
+//              time is that of reading the keys: 64 sequences of 500 to 4,000, 8 heads of 128, 201 MB in all,
+//              37 us (5.4 TB/s; a plain read reaches 7.1), of which 4 to 5 go by before the first keys arrive.
 //   many rows  a workgroup keeps 64 keys (of heads of 256, 32) in registers, the same in all waves, and these
 //              share the rows. The time is that of the products and the exponentials: a prompt of 4,097
 //              tokens, 32 heads on 8 of 128, 94 us (730 TFLOP/s), where its products take 28 and the vector
@@ -25,9 +26,11 @@ namespace gleam {
 namespace {
 
 constexpr uint32_t kRows = 16;        // rows of a tile
-// From this many tiles on the rows are shared by a workgroup's waves: 64 sequences of 1,500 keys, 8 heads of 128,
-// with 5 tiles take 117 us as few rows and 180 as many, with 7 148 and 185, with 10 204 and 198.
-constexpr uint32_t kSplitTiles = 8;
+// From this many tiles on the rows are shared by a workgroup's waves. 64 sequences of 1,500 keys, 8 heads of 128, take
+// with 8 tiles 125 us as few rows and 171 as many, with 10 148 and 181, with 12 174 and 186, with 14 196 and 199
+// (heads of 64: 83 and 139, 97 and 146, 112 and 146, 130 and 157; of 256: 160 and 193, 192 and 222, 225 and 226, 258
+// and 248). One sequence of 4,000 keys, whose keys are few for each wave: with 10 tiles 15 and 11.
+constexpr uint32_t kSplitTiles = 12, kSplitTilesOfOne = 8;
 constexpr uint32_t kGroups = 256;     // workgroups: one a CU, and as many waves in it as its registers hold
 template <int D> constexpr int kWaves = D == 256 ? 4 : 8;
 
@@ -47,6 +50,7 @@ struct WeighArgs {
   uint32_t n_tokens, n_seq, own_width;
   uint32_t q_heads, kv_heads, ratio, page_log2, n_pages;
   uint32_t ratio_mul, ratio_shift;
+  uint32_t most_few;  // rows
   float scale_log2;
 };
 
@@ -74,7 +78,7 @@ __device__ inline Seq seq_at(const WeighArgs& a, uint32_t s) {
   r.first = first;
   r.tokens = end > first ? end - first : 0;
   r.keys = a.n_pages ? (uint32_t)clamp_to(a.own_len[s], (int32_t)(a.own_width << a.page_log2)) : 0;
-  if ((uint64_t)r.tokens * a.ratio > kRows * (kSplitTiles - 1)) r.blocks = (r.keys + kBlock<D> - 1) / kBlock<D>;
+  if ((uint64_t)r.tokens * a.ratio > a.most_few) r.blocks = (r.keys + kBlock<D> - 1) / kBlock<D>;
   else r.halves = (r.keys + 31) / 32;
   return r;
 }
@@ -210,16 +214,15 @@ __device__ __forceinline__ void weigh_few(const WeighArgs& a, const Seq& seq, ui
   uint32_t seen = 0;  // keys that the lane's row sees
   float down = 0.f;
   const uint32_t from_lds = St::at(n, g);
-  auto take_rows = [&](uint32_t tile) {
-    r.find(a, seq, head, kRows * tile);
+  if (tiles == 1) {
+    r.find(a, seq, head, 0);
     r.load();
     St::store(lds + St::kTile, r.q);
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) q[i] = St::read(lds + St::kTile, from_lds, i);
     down = -r.lse * kLog2e;
-    seen = seen_by(a, seq, kRows * tile + n);
-  };
-  if (tiles == 1) take_rows(0);
+    seen = seen_by(a, seq, n);
+  }
   // a few tiles of rows stay in LDS
   float held_down[St::kHeld];
   uint32_t held_seen[St::kHeld];
@@ -310,13 +313,19 @@ __device__ __forceinline__ void weigh_few(const WeighArgs& a, const Seq& seq, ui
         }
       }
     } else {
+      // (a tile of rows asked for ahead takes registers that others need: 85 us for 90 with 5 tiles, 47 for 39 with one)
+      St::store(lds, kk[set][0]);
+      St::store(lds + St::kTile, kk[set][1]);
+      for (uint32_t t = 0; t < tiles; ++t) {
+        r.find(a, seq, head, kRows * t);
+        r.load();
+        St::store(lds + 2 * St::kTile, r.q);
+        down = -r.lse * kLog2e;
+        seen = seen_by(a, seq, kRows * t + n);
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        St::store(lds, kk[set][b]);
-        for (uint32_t t = 0; t < tiles; ++t) {
-          take_rows(t);
-          products(lds, b);
-        }
+        for (int i = 0; i < kSteps; ++i) q[i] = St::read(lds + 2 * St::kTile, from_lds, i);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) products(lds + b * St::kTile, b);
       }
       next = load(half + 2, set_);
     }
@@ -640,6 +649,8 @@ extern "C" gleam_status gleam_kv_weigh(const gleam_kv_pages* kv, const gleam_wei
   a.ratio_mul = (uint32_t)((1ull << (31 + a.ratio_shift)) / a.ratio + 1);
   a.page_log2 = (uint32_t)log2_exact(kv->page_tokens);
   a.n_pages = (uint32_t)kv->n_pages;
+  // (fewer sequences times heads than CUs are like one sequence)
+  a.most_few = kRows * ((in->n_seq * kv->kv_heads < kGroups ? kSplitTilesOfOne : kSplitTiles) - 1);
   a.scale_log2 = in->scale * kLog2e;
   const uint64_t halves = in->n_seq * kv->kv_heads * ((in->own_width * kv->page_tokens + 31) / 32);
   hipStream_t s = (hipStream_t)stream;

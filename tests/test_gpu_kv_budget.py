@@ -98,6 +98,14 @@ def test_prompts(n, own):
     Weighed([n, 1, n // 2], [own, 77, n // 2], 3, 1, 128, 64, F16, seed=n).check()
 
 
+@pytest.mark.parametrize("dtype,d", [(F16, 64), (BF16, 128), (F16, 256)])
+def test_new_tokens_of_many_sequences(dtype, d):
+    """3 to 14 tiles of rows each, with as many sequences and heads as there are CUs, and with one fewer."""
+    n = [12 + i % 44 for i in range(128)]
+    Weighed(n, [m + 11 * i % 150 for i, m in enumerate(n)], 8, 2, d, 16, dtype, seed=d).check()
+    Weighed(n[:85], [m + 13 * i % 70 for i, m in enumerate(n[:85])], 12, 3, d, 16, dtype, seed=d).check()
+
+
 @pytest.mark.parametrize("page,head_major", [(16, False), (64, True), (256, False), (4096, True)])
 def test_pages(page, head_major):
     Weighed([1, 2], [page + 1, 2 * page - 1], 4, 2, 64, page, F16, head_major=head_major).check()
