@@ -111,10 +111,11 @@ __device__ inline void add_weights(const f32x4& score, float scale, float down, 
   }
 }
 
-// How many keys a row sees: none where there is no such row.
-__device__ inline uint32_t seen_by(const WeighArgs& a, const Seq& seq, uint32_t row) {
+// How many keys a row sees: none where there is no such row, and none where its lse is +infinity, which leaves it out
+// (its scores may be anything then, and exp(NaN - infinity) is not 0).
+__device__ inline uint32_t seen_by(const WeighArgs& a, const Seq& seq, uint32_t row, float lse) {
   const int64_t sees = (int64_t)seq.keys - seq.tokens + token_of(a, row) + 1;
-  return row < seq.tokens * a.ratio && sees > 0 ? (uint32_t)sees : 0;
+  return row < seq.tokens * a.ratio && sees > 0 && lse != INFINITY ? (uint32_t)sees : 0;
 }
 
 // Rows are loaded whole, and pass through LDS into the products' layout: loads of 64 bytes of 16 rows, straight
@@ -221,7 +222,7 @@ __device__ __forceinline__ void weigh_few(const WeighArgs& a, const Seq& seq, ui
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) q[i] = St::read(lds + St::kTile, from_lds, i);
     down = -r.lse * kLog2e;
-    seen = seen_by(a, seq, n);
+    seen = seen_by(a, seq, n, r.lse);
   }
   // a few tiles of rows stay in LDS
   float held_down[St::kHeld];
@@ -236,7 +237,7 @@ __device__ __forceinline__ void weigh_few(const WeighArgs& a, const Seq& seq, ui
     r.load();
     St::store(lds + (1 + t) * St::kTile, r.q);
     held_down[t] = -r.lse * kLog2e;
-    held_seen[t] = seen_by(a, seq, kRows * t + n);
+    held_seen[t] = seen_by(a, seq, kRows * t + n, r.lse);
   }
 
   // pages of 16 keys each, 64 of them ahead, a lane each
@@ -321,7 +322,7 @@ __device__ __forceinline__ void weigh_few(const WeighArgs& a, const Seq& seq, ui
         r.load();
         St::store(lds + 2 * St::kTile, r.q);
         down = -r.lse * kLog2e;
-        seen = seen_by(a, seq, kRows * t + n);
+        seen = seen_by(a, seq, kRows * t + n, r.lse);
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) q[i] = St::read(lds + 2 * St::kTile, from_lds, i);
 #pragma unroll
@@ -402,14 +403,16 @@ __device__ __forceinline__ void weigh_many(const WeighArgs& a, const Seq& seq, u
     for (int i = 0; i < kSteps; ++i) k[t][i] = St::read(lds_k + t * St::kTile, St::at(n, g), i);
   float acc[kTiles][4] = {};
   const uint32_t rows = seq.tokens * a.ratio;
-  // the first row that sees the first key, and from where on all see all keys
+  // the first row that sees the first key; tiles of whole rows that all see all keys: from which one on, and how many
   const uint32_t row_least = key0 <= base ? 0 : (uint32_t)(key0 - base) * a.ratio;
   const int64_t row_all = ((int64_t)key0 + kBlock<D> - 1 - base) * a.ratio;
+  const uint32_t tile_all = row_all <= 0 ? 0 : (uint32_t)((row_all + kRows - 1) / kRows);
+  const uint32_t tiles_all = rows / kRows > tile_all ? rows / kRows - tile_all : 0;
   // From the last rows to the first that see a key: all blocks of a head that run at a time read the same
   // queries then, from the caches. A wave's tiles are kWaves<D> apart, two are on their way. Where the rows of
   // two such tiles are whole tokens, each lane only steps back over those.
-  const int64_t tile_least = row_least / kRows;
-  int64_t tile = (int64_t)((rows - 1) / kRows) - wave;
+  const int32_t tile_least = (int32_t)(row_least / kRows);
+  int32_t tile = (int32_t)((rows - 1) / kRows) - (int32_t)wave;
   constexpr uint32_t kBack = 2 * kWaves<D> * kRows;
   const bool whole = kBack % a.ratio == 0;
   const int64_t back_q = kBack / a.ratio * a.q_token, back_lse = (int64_t)(kBack / a.ratio) * a.q_heads;
@@ -419,7 +422,7 @@ __device__ __forceinline__ void weigh_many(const WeighArgs& a, const Seq& seq, u
   auto add = [&](auto set_) {
     constexpr int set = decltype(set_)::value;
     St::store(mine, r[set].q);
-    const float down = -r[set].lse * kLog2e;
+    const float lse = r[set].lse, down = -lse * kLog2e;
     if (tile >= 2 * kWaves<D>) {  // otherwise the same again, in vain
       if (whole) r[set].step_back(back_q, back_lse);
       else r[set].find(a, seq, head, (uint32_t)(tile - 2 * kWaves<D>) * kRows);
@@ -434,9 +437,8 @@ __device__ __forceinline__ void weigh_many(const WeighArgs& a, const Seq& seq, u
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) score[t] = Mfma<T>::run(get(k[t][i], T()), get(q, T()), score[t]);
     }
-    const int64_t row0 = tile * kRows;
-    if (row0 + kRows > rows || row0 < row_all) {
-      const uint32_t seen = seen_by(a, seq, (uint32_t)row0 + n);
+    if ((uint32_t)tile - tile_all >= tiles_all || __any(lse == INFINITY)) {
+      const uint32_t seen = seen_by(a, seq, (uint32_t)tile * kRows + n, lse);
 #pragma unroll
       for (int t = 0; t < kTiles; ++t)
         add_weights(score[t], a.scale_log2, down, true, key0 + 16 * t + 4 * g, seen, acc[t]);

@@ -142,6 +142,27 @@ def test_rows_that_are_left_out_and_strided_queries():
     c.check({**c.arguments(), "q": wide.cuda()[:, 2:6]})
 
 
+@pytest.mark.parametrize("dtype,d", [(F16, 64), (BF16, 128), (BF16, 256)])
+@pytest.mark.parametrize("n", [1, 5, 20, 40, 56, 57, 140, 300])
+def test_rows_that_are_left_out_may_hold_anything(n, dtype, d):
+    """Queries of rows whose lse is +infinity, as padded ones have that nobody wrote: NaN, infinite, or so large that
+    their scores overflow. 1 to 7 tiles of rows that are few, and many, whose last tiles see all of a block's keys."""
+    c = Weighed([n, 3], [n + 90, 40], 4, 2, d, 16, dtype, seed=n)
+    anything = (math.nan, math.inf, -math.inf, torch.finfo(dtype).max)
+    rows = [(t, h, anything[i % 4]) for i, (t, h) in enumerate((t, h) for t in {0, n // 2, n - 1, n + 1} for h in range(4)
+                                                               if t != n // 2 or h in (0, 3))]
+    for t, h, _ in rows:
+        c.lse[t, h] = math.inf
+    want, births, tol = c.want()  # of finite queries, whose rows add exp(-infinity) = 0
+    for t, h, x in rows:
+        c.q[t, h] = x
+        c.q[t, h, ::3] *= -1
+    say("kv_weigh", c.what)
+    got, born = c.call()
+    assert torch.equal(born.cpu(), births)
+    R.near(got, want, tol, "weights")
+
+
 @pytest.mark.parametrize("n", [5, 140])
 def test_what_a_row_does_not_see_may_be_anything(n):
     """NaN in a late key reaches that key's weight alone, NaN in a query what the query sees."""
