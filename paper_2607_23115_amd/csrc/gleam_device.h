@@ -96,7 +96,7 @@ __device__ __forceinline__ uint64_t shfl64(uint64_t v, int src) {
   return ((uint64_t)hi << 32) | lo;
 }
 
-// Orders this wave's LDS writes before its later LDS reads (LDS executes one
+// Orders this wave's LDS reads and writes before its later ones (LDS executes one
 // wave's instructions in order; this keeps the compiler from reordering them).
 __device__ __forceinline__ void wave_lds_sync() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");

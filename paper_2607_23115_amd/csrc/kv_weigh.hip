@@ -19,6 +19,7 @@
 
 #include <type_traits>
 
+#include "gleam_device.h"
 #include "kv_device.h"
 #include "launch_shape.h"
 
@@ -131,12 +132,15 @@ struct Staged {
   static __device__ uint32_t at(uint32_t row, uint32_t piece) {
     return row * (2 * D) + ((piece ^ (D == 64 ? (row >> 1) & 7 : row & 15)) << 4);
   }
-  // What the lane loads of 16 rows goes to row load_row() + i * kLoadRows, piece().
+  // What the lane loads of 16 rows goes to row load_row() + i * kLoadRows, piece(). Other lanes of the wave read it:
+  // store() keeps the wave's earlier loads from that place before it and the later ones behind it.
   static __device__ uint32_t load_row() { return (threadIdx.x & 63) / kPieces; }
   static __device__ uint32_t piece() { return (threadIdx.x & 63) % kPieces; }
   static __device__ void store(char* lds, const u32x4v (&x)[kLoads]) {
+    wave_lds_sync();
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4v*>(lds + at(i * kLoadRows + load_row(), piece())) = x[i];
+    wave_lds_sync();
   }
   // The 32 dims from 32 i on of a row, a lane's eight; from: at(row, lane / 16).
   static __device__ Pack8 read(const char* lds, uint32_t from, int i) {
