@@ -744,7 +744,9 @@ gleam_status gleam_prefix_attention(const gleam_kv_pages* kv, const gleam_prefix
  * parent, the parent's parent and so on; d_depth[t] (nullable) = how many of those come before it: its
  * position is the sequence's length before the drafts plus that. Tokens of no sequence get 0.
  *   d_parent  int32[n_tokens]
- *   d_q_first int32[n_seq + 1], non-decreasing (a sequence that ends before it starts has no tokens)
+ *   d_q_first int32[n_seq + 1], non-decreasing (those below 0 or above n_tokens are taken as these). Tokens
+ *             before the first and from the last on are of no sequence; where offsets decrease in between and
+ *             sequences share tokens, any bits and depths may be written for those
  *   d_seen    uint64[n_tokens][seen_words], seen_words 1 to 65536
  * Errors: GLEAM_E_INVALID, GLEAM_E_UNSUPPORTED (more than 2^20 sequences, or 2^31 tokens), GLEAM_E_HIP.
  *

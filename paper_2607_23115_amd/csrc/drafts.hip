@@ -61,9 +61,9 @@ struct TreeArgs {
 __global__ __launch_bounds__(64) void tree_kernel(TreeArgs a) {
   const uint32_t lane = threadIdx.x;
   const int32_t all = (int32_t)a.n_tokens;
+  const uint32_t before = a.n_seq ? (uint32_t)clamp_to(a.q_first[0], all) : 0;
+  const uint32_t behind = a.n_seq ? (uint32_t)clamp_to(a.q_first[a.n_seq], all) : 0;
   if (blockIdx.x >= a.n_seq) {
-    const uint32_t before = a.n_seq ? (uint32_t)clamp_to(a.q_first[0], all) : 0;
-    const uint32_t behind = a.n_seq ? (uint32_t)clamp_to(a.q_first[a.n_seq], all) : 0;
     const uint32_t step = (gridDim.x - a.n_seq) * 64;
     for (uint64_t t = (blockIdx.x - a.n_seq) * 64 + lane; t < a.n_tokens; t += step) {
       if (t >= before && t < behind) continue;
@@ -72,8 +72,11 @@ __global__ __launch_bounds__(64) void tree_kernel(TreeArgs a) {
     }
     return;
   }
-  const uint32_t first = (uint32_t)clamp_to(a.q_first[blockIdx.x], all);
-  const uint32_t end = (uint32_t)clamp_to(a.q_first[blockIdx.x + 1], all);
+  uint32_t first = (uint32_t)clamp_to(a.q_first[blockIdx.x], all);
+  uint32_t end = (uint32_t)clamp_to(a.q_first[blockIdx.x + 1], all);
+  // of offsets that decrease, none that others clear
+  first = first > before ? first : before;
+  end = end < behind ? end : behind;
   if (end <= first) return;
   const uint32_t n = end - first;
   uint64_t* const seen = a.seen + (uint64_t)first * a.words;

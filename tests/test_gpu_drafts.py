@@ -77,6 +77,18 @@ def test_parents_and_offsets_that_make_no_sense():
             assert torch.equal(seen.cpu(), want) and torch.equal(depth.cpu(), deep)
 
 
+@pytest.mark.parametrize("offsets", [[5, 2, 2], [5, 2, 4], [8, 0, 8, 0], [6, 1, 3, 2, 5]])
+def test_offsets_that_decrease_below_the_first(offsets):
+    """What lies before the first offset or behind the last is of no sequence: one of them clears it, none writes it."""
+    parent = forest([8], 3)
+    for _ in range(20):
+        seen = torch.full((8, 1), -1, dtype=torch.int64, device="cuda")
+        depth = torch.full((8,), -1, dtype=torch.int32, device="cuda")
+        say("draft_tree", offsets)
+        g.draft_tree(parent.cuda(), i32(offsets).cuda(), 8, seen=seen, depth=depth)
+        assert (seen == 0).all() and (depth == 0).all()
+
+
 def test_tree_refusals_and_streams():
     parent, first = forest([13, 20], 1).cuda(), i32([0, 13, 33]).cuda()
     for message, bad in (("width must be", dict(width=0)), ("width must be", dict(width=(1 << 22) + 1)),
