@@ -761,7 +761,8 @@ gleam_status gleam_prefix_attention(const gleam_kv_pages* kv, const gleam_prefix
  * them goes to the place of draft e, and d_len_out[s] = the keys before the drafts and those kept. What
  * lies behind is left as it is. Keys in a page that the cache does not have are neither read nor written.
  * The cache's places must not overlap (as for gleam_kv_append), a page must be in one place of the table
- * only, and d_len_out must not overlap d_own_len.
+ * only, and d_len_out must not overlap what the call reads (d_own_len, d_leaf, d_q_first, d_seen,
+ * d_own_pages).
  * Errors: GLEAM_E_INVALID, GLEAM_E_UNSUPPORTED (more than 2^20 sequences, or 2^31 tokens), GLEAM_E_HIP.
  */
 typedef struct gleam_accept {
@@ -814,7 +815,7 @@ gleam_status gleam_kv_accept(const gleam_kv_pages* kv, const gleam_accept* a, vo
  * must be in one place of the table only.
  *   d_weights_out, d_born_out  may be d_weights and d_born themselves, and must not overlap them otherwise;
  *                    written for the first `keep` keys of each sequence
- *   d_len_out        must not overlap d_own_len (other layers' caches still need that)
+ *   d_len_out        must not overlap d_own_len (other layers' caches still need that), d_total or d_own_pages
  *   d_ws             device, 256-byte aligned, >= gleam_kv_evict_ws_bytes(kv, e)
  * Errors: GLEAM_E_INVALID, GLEAM_E_WORKSPACE, GLEAM_E_UNSUPPORTED (more than 2^20 sequences, 2^31 sequences
  * times heads, or 2^36 keys that may move), GLEAM_E_HIP. gleam_kv_evict_ws_bytes returns 0 for arguments

@@ -1224,7 +1224,8 @@ def kv_accept(k_pages: torch.Tensor, v_pages: torch.Tensor, q_first: torch.Tenso
 
     leaf int32 [sequences]: the path's last draft, counted within the sequence, -1 to keep none. The
     drafts that it sees move, in order, to the places of the first drafts, and len_out (int32, not
-    own_len itself: other layers' caches still need that) is the keys before the drafts and theirs."""
+    own_len itself: other layers' caches still need that; nor leaf or q_first) is the keys before the drafts
+    and theirs."""
     kv = _kv_struct(k_pages, v_pages)
     dev, i32 = k_pages.get_device(), torch.int32
     pages_at, width, len_at, n_seq = _ragged(own_pages, own_len, dev)
@@ -1301,7 +1302,7 @@ def kv_evict(k_pages: torch.Tensor, v_pages: torch.Tensor, own_pages: torch.Tens
     total, are kept first, then those of the largest weights; kept keys from place `keep` on move
     into the places before it that come free, weights and births with them (in weights and born
     themselves where weights_out and born_out are not given). len_out int32: not own_len itself, other
-    layers' caches still need that. ws: from kv_evict_workspace()."""
+    layers' caches still need that; nor total. ws: from kv_evict_workspace()."""
     kv = _kv_struct(k_pages, v_pages)
     dev, i32, f32 = k_pages.get_device(), torch.int32, torch.float32
     pages_at, width, len_at, n_seq = _ragged(own_pages, own_len, dev)

@@ -41,6 +41,19 @@ gleam_status validate_sequences(const gleam_kv_pages* kv, uint64_t n_seq, uint64
   return GLEAM_OK;
 }
 
+gleam_status validate_len_out(const int32_t* d_len_out, uint64_t n_seq, const ReadLate* reads, int n_reads,
+                              const char* who) {
+  const uintptr_t to = reinterpret_cast<uintptr_t>(d_len_out);
+  for (int i = 0; i < n_reads; ++i) {
+    const uintptr_t from = reinterpret_cast<uintptr_t>(reads[i].p);
+    if (from < to ? to - from < reads[i].bytes : from - to < 4 * n_seq) {
+      set_error("%s: len_out must not overlap %s", who, reads[i].name);
+      return GLEAM_E_INVALID;
+    }
+  }
+  return GLEAM_OK;
+}
+
 namespace {
 
 // --------------------------------------------------------------------------------------- //
@@ -253,12 +266,12 @@ extern "C" gleam_status gleam_kv_accept(const gleam_kv_pages* kv, const gleam_ac
     set_error("%s: null q_first, leaf or len_out", who);
     return GLEAM_E_INVALID;
   }
-  // workgroups read the lengths at different times
-  const uintptr_t from = reinterpret_cast<uintptr_t>(in->d_own_len), to = reinterpret_cast<uintptr_t>(in->d_len_out);
-  if ((from < to ? to - from : from - to) < 4 * in->n_seq) {
-    set_error("%s: len_out must not overlap own_len", who);
-    return GLEAM_E_INVALID;
-  }
+  const ReadLate reads[] = {{in->d_own_len, 4 * in->n_seq, "own_len"},
+                            {in->d_leaf, 4 * in->n_seq, "leaf"},
+                            {in->d_q_first, 4 * (in->n_seq + 1), "q_first"},
+                            {in->d_seen, 8 * in->n_tokens * in->seen_words, "seen"},
+                            {in->d_own_pages, 4 * in->n_seq * in->own_width, "own_pages"}};
+  if ((st = validate_len_out(in->d_len_out, in->n_seq, reads, 5, who)) != GLEAM_OK) return st;
   AcceptArgs a{};
   a.base[0] = static_cast<uint8_t*>(kv->d_k);
   a.base[1] = static_cast<uint8_t*>(kv->d_v);

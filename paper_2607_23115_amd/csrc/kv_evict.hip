@@ -541,12 +541,10 @@ extern "C" gleam_status gleam_kv_evict(const gleam_kv_pages* kv, const gleam_evi
     set_error("%s: null total or len_out", who);
     return GLEAM_E_INVALID;
   }
-  // workgroups read the lengths at different times
-  const uintptr_t from = reinterpret_cast<uintptr_t>(in->d_own_len), to = reinterpret_cast<uintptr_t>(in->d_len_out);
-  if ((from < to ? to - from : from - to) < 4 * in->n_seq) {
-    set_error("%s: len_out must not overlap own_len", who);
-    return GLEAM_E_INVALID;
-  }
+  const ReadLate reads[] = {{in->d_own_len, 4 * in->n_seq, "own_len"},
+                            {in->d_total, 4 * in->n_seq, "total"},
+                            {in->d_own_pages, 4 * in->n_seq * in->own_width, "own_pages"}};
+  if ((st = validate_len_out(in->d_len_out, in->n_seq, reads, 3, who)) != GLEAM_OK) return st;
   if ((st = validate_tracked(kv, in->d_weights, in->d_weights_out, "weights", who)) != GLEAM_OK) return st;
   if ((st = validate_tracked(kv, in->d_born, in->d_born_out, "born", who)) != GLEAM_OK) return st;
   if (!d_ws || !aligned256(d_ws)) {

@@ -18,6 +18,15 @@ gleam_status validate_seen(const uint64_t* d_seen, uint32_t words, uint64_t n_to
 // A ragged batch's sequences and the rows of their page table.
 gleam_status validate_sequences(const gleam_kv_pages* kv, uint64_t n_seq, uint64_t own_width, const int32_t* d_own_pages,
                                 const int32_t* d_own_len, const char* who);
+// That the lengths a call returns overlap none of what its workgroups read at different times: they may have been
+// written by then.
+struct ReadLate {
+  const void* p;
+  uint64_t bytes;
+  const char* name;
+};
+gleam_status validate_len_out(const int32_t* d_len_out, uint64_t n_seq, const ReadLate* reads, int n_reads,
+                              const char* who);
 // What is kept for each place and key head, 4 bytes in [n_pages][kv_heads][page_tokens], and where it goes.
 gleam_status validate_tracked(const gleam_kv_pages* kv, const void* in, const void* out, const char* name,
                               const char* who);

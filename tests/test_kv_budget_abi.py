@@ -98,6 +98,15 @@ def test_accepted_paths_that_are_refused(bad):
     assert b"gleam_kv_accept" in g.lib.gleam_last_error()
 
 
+@pytest.mark.parametrize("name", ["own_len", "leaf", "q_first", "seen", "own_pages"])
+def test_an_accepted_length_written_over_what_is_read(name):
+    """len_out of 2 sequences is 8 bytes; the fields: 2, 2 and 3 of 4 bytes, 4 of 8, 6 of 4."""
+    size = {"own_len": 8, "leaf": 8, "q_first": 12, "seen": 32, "own_pages": 24}[name]
+    for to in (1 << 20, (1 << 20) - 4, (1 << 20) + size - 4):
+        assert accept(**{name: 1 << 20, "len_out": to}) == g.E_INVALID
+        assert name.encode() in g.lib.gleam_last_error() and b"overlap" in g.lib.gleam_last_error()
+
+
 def test_accept_limits():
     assert accept(kv(k_stride=(2048, 64, 64))) == g.E_INVALID
     assert b"overlap" in g.lib.gleam_last_error()
@@ -133,6 +142,14 @@ def test_weigh_limits():
 def test_evictions_that_are_refused(bad):
     assert evict(**bad) == g.E_INVALID
     assert b"gleam_kv_evict" in g.lib.gleam_last_error()
+
+
+@pytest.mark.parametrize("name", ["own_len", "total", "own_pages"])
+def test_a_budgets_length_written_over_what_is_read(name):
+    size = {"own_len": 8, "total": 8, "own_pages": 24}[name]
+    for to in (1 << 22, (1 << 22) - 4, (1 << 22) + size - 4):
+        assert evict(**{name: 1 << 22, "len_out": to}) == g.E_INVALID
+        assert name.encode() in g.lib.gleam_last_error() and b"overlap" in g.lib.gleam_last_error()
 
 
 def test_eviction_workspaces_and_limits():
