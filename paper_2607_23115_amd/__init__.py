@@ -1057,7 +1057,7 @@ def prefix_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
                      own_pages: torch.Tensor, own_len: torch.Tensor, group_first: torch.Tensor | None = None,
                      prefix_pages: torch.Tensor | None = None, prefix_len: torch.Tensor | None = None,
                      scale: float | None = None, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
-                     want_lse: bool = False, ws: torch.Tensor | None = None, stream=None, _seen=None):
+                     want_lse: bool = False, ws: torch.Tensor | None = None, stream=None):
     """Attention of a ragged batch over the paged cache: (out [tokens, q_heads, head_dim], lse
     float32 [tokens, q_heads] or None).
 
@@ -1068,6 +1068,13 @@ def prefix_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
     page tables -1. scale: head_dim ** -0.5 where none is given. ws: a workspace from
     prefix_attention_workspace() of these shapes. There is no gradient: tensors that require one
     are refused while torch records them."""
+    return _attend(None, 0, q, k_pages, v_pages, q_first, own_pages, own_len, group_first, prefix_pages, prefix_len,
+                   scale, out, lse, want_lse, ws, stream)
+
+
+def _attend(seen, words, q, k_pages, v_pages, q_first, own_pages, own_len, group_first, prefix_pages, prefix_len, scale,
+            out, lse, want_lse, ws, stream):
+    """prefix_attention(); of trees of drafts with their bits, `words` of 64 for each token."""
     kv = _kv_struct(k_pages, v_pages)
     dtype, dev, d = k_pages.dtype, k_pages.get_device(), kv.head_dim
     q_at, tokens, heads, q_token, q_head = _heads(q, "q", dtype, dev, d)
@@ -1107,24 +1114,24 @@ def prefix_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
             lse = q.new_empty((tokens, heads), dtype=torch.float32)
             lse_at = lse.data_ptr()
         if ws is None:
-            ws_bytes = _attention_ws(kv, b, _seen)
+            ws_bytes = _attention_ws(kv, b, seen is not None)
             ws = q.new_empty(ws_bytes, dtype=torch.uint8)
             ws_at = ws.data_ptr()
         else:
             ws_at, ws_bytes = _flat(ws, "ws", torch.uint8, dev), ws.numel()
         if (q.requires_grad or k_pages.requires_grad or v_pages.requires_grad or out.requires_grad
                 or lse is not None and lse.requires_grad or not _forward or _forward._current_level >= 0):
-            _no_gradient("tree_attention" if _seen else "prefix_attention", q=q, k_pages=k_pages, v_pages=v_pages,
-                         out=out, lse=lse)
-        if _seen:  # tree_attention's: (tensor, words)
-            seen_at = _flat(_seen[0], "seen", torch.int64, dev, tokens * _seen[1])
-            _check(lib.gleam_tree_attention(kv, b, seen_at, _seen[1], out_at, lse_at, ws_at, ws_bytes, hs))
-        else:
+            _no_gradient("prefix_attention" if seen is None else "tree_attention", q=q, k_pages=k_pages,
+                         v_pages=v_pages, out=out, lse=lse)
+        if seen is None:
             _check(lib.gleam_prefix_attention(kv, b, out_at, lse_at, ws_at, ws_bytes, hs))
+        else:
+            seen_at = _flat(seen, "seen", torch.int64, dev, tokens * words)
+            _check(lib.gleam_tree_attention(kv, b, seen_at, words, out_at, lse_at, ws_at, ws_bytes, hs))
     return out, lse
 
 
-def _attention_ws(kv: _KvPages, b: _PrefixBatch, tree=None) -> int:
+def _attention_ws(kv: _KvPages, b: _PrefixBatch, tree: bool = False) -> int:
     n = lib.gleam_tree_attention_ws_bytes(kv, b) if tree else lib.gleam_prefix_attention_ws_bytes(kv, b)
     if n == 0:
         raise GleamError(E_INVALID, lib.gleam_last_error().decode())
@@ -1205,8 +1212,8 @@ def tree_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor
     in its row of seen (int64 [tokens, words], draft_tree()'s or any other). ws: a workspace from
     tree_attention_workspace(). Everything else is prefix_attention()'s."""
     words = _seen_words(seen, q.shape[0] if isinstance(q, torch.Tensor) and q.dim() else None)
-    return prefix_attention(q, k_pages, v_pages, q_first, own_pages, own_len, group_first, prefix_pages, prefix_len,
-                            scale, out, lse, want_lse, ws, stream, (seen, words))
+    return _attend(seen, words, q, k_pages, v_pages, q_first, own_pages, own_len, group_first, prefix_pages, prefix_len,
+                   scale, out, lse, want_lse, ws, stream)
 
 
 def tree_attention_workspace(k_pages: torch.Tensor, v_pages: torch.Tensor, tokens: int, q_heads: int, n_seq: int,

@@ -3,6 +3,7 @@ is enqueued, and the binding's structures are laid out as the header's. The plai
 tests compare with are held against small cases written out."""
 
 import ctypes
+import inspect
 import math
 import os
 import shutil
@@ -202,6 +203,11 @@ def test_the_binding_refuses_host_tensors():
 
 def i32(x):
     return torch.tensor(x, dtype=torch.int32)
+
+
+def test_public_calls_have_no_private_parameters():
+    for call in (g.prefix_attention, g.tree_attention, g.draft_tree, g.kv_accept, g.kv_weigh, g.kv_evict, g.kv_append):
+        assert not [p for p in inspect.signature(call).parameters if p.startswith("_")], call.__name__
 
 
 def test_a_small_tree_written_out():
