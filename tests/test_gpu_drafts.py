@@ -10,6 +10,7 @@ import kv_reference as R
 import paper_2607_23115_amd as g
 from gpu_util import say
 from test_gpu_prefix_attention import Case
+from test_prefix_plan import LONG_TREES
 
 pytestmark = pytest.mark.gpu
 F16, BF16 = torch.float16, torch.bfloat16
@@ -225,6 +226,18 @@ def test_a_chain_is_prefix_attention():
 def test_long_histories_of_few_and_many_drafts():
     TreeCase([5], [9000], [], 4, 1, 128, 64, BF16, random_bits=True).check()
     TreeCase([40], [2500], [(0, 1, 700)], 4, 1, 64, 16, F16, random_bits=True).check()
+
+
+@pytest.mark.parametrize("seqs", LONG_TREES)
+@pytest.mark.parametrize("more", [0, 70])
+def test_on_both_sides_of_where_trees_take_more_units(seqs, more):
+    """The batches of the plan's test: their tiles cost 9,120 steps, cut for 256 units, and 9,129, cut for 480; with
+    more sequences (without keys that cost tiles anything) the plan is not made in a wave but by a kernel."""
+    n, own = map(list, zip(*seqs))
+    c = TreeCase(n + [1] * more, own + [9] * more, [], 32, 1, 64, 4096, BF16, seed=more, random_bits=True)
+    out, _ = c.check()
+    again = g.tree_attention(**c.arguments())[0]
+    assert torch.equal(out, again)
 
 
 @pytest.mark.parametrize("n", [6, 70])
