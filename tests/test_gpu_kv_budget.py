@@ -200,6 +200,105 @@ def test_many_sequences():
     Weighed(n, own, 2, 1, 64, 16, F16).check()
 
 
+class Streamed:
+    """Long sequences, made and weighed on the GPU: the plain computation in 64 bits takes all keys of a sequence and
+    head at once. Units of work are halves of 64 keys of each sequence and head, dealt out evenly to 2,048 waves (1,024
+    of heads of 256)."""
+
+    def __init__(self, n, own, hq, hkv, d, page, dtype, seed=0):
+        gen = torch.Generator("cuda").manual_seed(seed)
+        self.n, self.own, self.hkv, self.d, self.page = n, own, hkv, d, page
+        counts = [-(-m // page) for m in own]
+        order = torch.randperm(sum(counts) + 1, generator=gen, device="cuda")
+        self.kp = torch.randn(sum(counts) + 1, page, hkv, d, generator=gen, device="cuda", dtype=dtype)
+        table = torch.full((len(own), max(counts) + 1), -1, dtype=torch.int32, device="cuda")
+        self.pages, at = [], 0
+        for s, count in enumerate(counts):
+            self.pages.append(order[at:at + count])
+            table[s, :count] = self.pages[-1].int()
+            at += count
+        self.q = torch.randn(sum(n), hq, d, generator=gen, device="cuda", dtype=dtype)
+        self.lse = torch.randn(sum(n), hq, generator=gen, device="cuda") * 2 + math.log(max(own))
+        self.weights = torch.rand(self.kp.shape[0], hkv, page, generator=gen, device="cuda") * 3
+        self.born = torch.randint(0, 999, self.weights.shape, generator=gen, device="cuda", dtype=torch.int32)
+        self.positions = torch.randint(1000, 9999, (sum(n),), generator=gen, device="cuda", dtype=torch.int32)
+        self.q_first, self.table, self.own_len = (x.cuda() for x in (i32([sum(n[:i]) for i in range(len(n) + 1)]), table,
+                                                                     i32(own)))
+
+    def halves(self):
+        return sum(-(-m // 32) for m in self.own) * self.hkv
+
+    def want(self):
+        """(weights, born, bound), the bound being B.weigh's."""
+        out, births, tol = self.weights.double(), self.born.clone(), torch.zeros_like(self.weights, dtype=torch.float64)
+        ratio, scale = self.q.shape[1] // self.hkv, self.d ** -0.5
+        t0 = 0
+        for n, own, pages in zip(self.n, self.own, self.pages):
+            j = torch.arange(own, device="cuda")
+            p, i = pages[j // self.page], j % self.page
+            for h in range(self.hkv):
+                k = self.kp[p, i, h].double()
+                total = torch.where(j < own - n, out[p, h, i], 0.0)
+                bound = torch.zeros(own, dtype=torch.float64, device="cuda")
+                for t in range(n):
+                    for r in range(h * ratio, (h + 1) * ratio):
+                        x, l = self.q[t0 + t, r].double(), self.lse[t0 + t, r].double()
+                        score, size = (k * x).sum(-1) * scale, (k * x).abs().sum(-1) * scale
+                        e = torch.where(j < own - n + t + 1, torch.exp(score - l), 0.0)
+                        total = total + e
+                        bound += 2 * e * ((self.d + 4) * 2.0 ** -24 * size + 2.0 ** -22 * (1 + score.abs() + l.abs()))
+                out[p, h, i] = total
+                tol[p, h, i] = bound + (n * ratio / 16 + 12) * 2.0 ** -24 * total.abs() + 2.0 ** -120
+                births[p[own - n:], h, i[own - n:]] = self.positions[t0:t0 + n]
+            t0 += n
+        return out, births, tol
+
+    def call(self):
+        weights, born = self.weights.clone(), self.born.clone()
+        g.kv_weigh(self.q, self.kp, self.q_first, self.table, self.own_len, self.lse, weights, born, self.positions)
+        torch.cuda.synchronize()
+        return weights, born
+
+    def check(self):
+        say("kv_weigh", f"n={self.n} own={self.own} heads={self.q.shape[1]}/{self.hkv} d={self.d} page={self.page}",
+            self.kp.dtype)
+        got, born = self.call()
+        want, births, tol = self.want()
+        assert torch.equal(born, births)
+        R.near(got, want.cpu(), tol.cpu(), "weights")
+        again, _ = self.call()
+        assert torch.equal(got, again)
+
+
+def test_the_plain_sums_of_long_sequences():
+    """The computation that takes all keys at once is the one that takes one at a time."""
+    c = Streamed([2, 1, 9], [40, 17, 70], 4, 2, 64, 16, BF16)
+    want, births, tol = (x.cpu() for x in c.want())
+    one, born, bound = B.weigh(*(x.cpu() for x in (c.q, c.kp, c.q_first, c.table, c.own_len, c.lse, c.weights, c.born,
+                                                   c.positions)))
+    assert torch.equal(births, born) and float((want - one).abs().max()) < 1e-12
+    assert float((tol - bound).abs().max()) < 1e-12
+    c.check()
+
+
+@pytest.mark.parametrize("dtype,d", [(F16, 64), (BF16, 128), (BF16, 256)])
+@pytest.mark.parametrize("n", [[1, 1, 1, 2, 1, 3], [9, 4, 12, 8, 10, 12], [20, 28, 13, 25, 18, 24]])
+def test_waves_that_go_from_one_head_and_sequence_to_the_next(n, dtype, d):
+    """One tile of rows, two and three (which stay in LDS), and 4 to 7 (loaded again); several halves a wave."""
+    c = Streamed(n, [60001, n[1], 90000, 26000, 777, 58000], 8, 2, d, 16, dtype, seed=d)
+    assert c.halves() > 7 * 2048 and c.halves() % 2048
+    c.check()
+
+
+@pytest.mark.parametrize("dtype,d,own", [(BF16, 64, 2_400_017), (F16, 128, 2_400_017), (BF16, 256, 1_200_017)])
+@pytest.mark.parametrize("n", [1, 11])
+def test_waves_that_look_up_pages_again(n, dtype, d, own):
+    """More than 32 halves a wave: pages are looked up for 32 at a time."""
+    c = Streamed([n], [own], 4, 1, d, 64, dtype, seed=n)
+    assert c.halves() > 36 * (1024 if d == 256 else 2048)
+    c.check()
+
+
 def test_twice_on_a_stream_and_in_a_graph():
     c = Weighed([1, 60, 1], [900, 300, 44], 8, 2, 128, 16, BF16)
     a = c.arguments()
