@@ -290,6 +290,15 @@ def test_waves_that_go_from_one_head_and_sequence_to_the_next(n, dtype, d):
     c.check()
 
 
+@pytest.mark.parametrize("dtype,d", [(BF16, 64), (F16, 128), (BF16, 256)])
+def test_many_sequences_of_several_halves_a_wave(dtype, d):
+    """More sequences than are looked at in one step, some of them with rows for a workgroup (15 tiles)."""
+    n = [60 if i in (3, 70, 149) else 1 + i % 3 for i in range(150)]
+    c = Streamed(n, [m + 97 * i % 5000 for i, m in enumerate(n)], 8, 2, d, 32, dtype, seed=d)
+    assert c.halves() > 10 * 2048
+    c.check()
+
+
 @pytest.mark.parametrize("dtype,d,own", [(BF16, 64, 2_400_017), (F16, 128, 2_400_017), (BF16, 256, 1_200_017)])
 @pytest.mark.parametrize("n", [1, 11])
 def test_waves_that_look_up_pages_again(n, dtype, d, own):
