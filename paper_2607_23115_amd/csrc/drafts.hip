@@ -1,6 +1,6 @@
 // Trees of drafted tokens: who sees whom, and what becomes of the keys of the path that was accepted.
-// Both calls are a few loads long that wait for each other, and bound by those: a tree of 13 takes 1.7 us, 96 of
-// up to 160 5.6 (three rounds of 64 drafts); the path of one sequence, 32 heads of 128, 3.4, those of 128, of up to
+// Both calls are a few loads long that wait for each other, and bound by those: a tree of 13 takes 1.8 us, 96 of
+// up to 160 5.8 (three rounds of 64 drafts); the path of one sequence, 32 heads of 128, 3.4, those of 128, of up to
 // 20 drafts and 8 heads of 256, 7.2 (6 MB read and written; 11.2 where each row's pages were looked up in turn).
 
 #include "kv_device.h"

@@ -13,9 +13,10 @@
 //              37 us (5.4 TB/s; a plain read reaches 7.1), of which 4 to 5 go by before the first keys arrive.
 //   many rows  a workgroup keeps 64 keys (of heads of 256, 32) in registers, the same in all waves, and these
 //              share the rows. The time is that of the products and the exponentials: a prompt of 4,097
-//              tokens, 32 heads on 8 of 128, 94 us (730 TFLOP/s), where its products take 28 and the vector
-//              instructions 50 of a SIMD's two waves, which overlap in part. Products of one tile under the
-//              exponentials of the one before, in one wave, took too many registers (120 us).
+//              tokens, 32 heads on 8 of 128, 91 us (755 TFLOP/s) once the GPU's clocks are up, after some 40 ms
+//              of work, and 106 to 117 before, where its products take 28 and the vector instructions 50 of a
+//              SIMD's two waves, which overlap in part. Products of one tile under the exponentials of the one
+//              before, in one wave, took too many registers (120 us).
 
 #include <type_traits>
 
@@ -27,10 +28,12 @@ namespace gleam {
 namespace {
 
 constexpr uint32_t kRows = 16;        // rows of a tile
-// From this many tiles on the rows are shared by a workgroup's waves. 64 sequences of 1,500 keys, 8 heads of 128, take
-// with 8 tiles 125 us as few rows and 171 as many, with 10 148 and 181, with 12 174 and 186, with 14 196 and 199
-// (heads of 64: 83 and 139, 97 and 146, 112 and 146, 130 and 157; of 256: 160 and 193, 192 and 222, 225 and 226, 258
-// and 248). One sequence of 4,000 keys, whose keys are few for each wave: with 10 tiles 15 and 11.
+// From this many tiles on the rows are shared by a workgroup's waves: one number for all widths, that at which heads of
+// 256 break even. 64 sequences of 1,500 keys, 4 heads of 256, take with 8 tiles 159 us as few rows and 186 as many, with
+// 10 192 and 221, with 12 226 and 225, with 14 259 and 250. Narrower heads break even later, and lose some by it: 8
+// of 128 with 8 tiles 123 and 165, 10 144 and 175, 12 169 and 179, 14 190 and 192, 16 214 and 195; 8 of 64 83 and 138,
+// 97 and 147, 111 and 146, 128 and 157, 152 and 157. One sequence of 4,000 keys, whose keys are few for each wave, a
+// whole call: with 8 tiles 15.7 and 15.5, 10 16.3 and 15, 14 19 and 15.
 constexpr uint32_t kSplitTiles = 12, kSplitTilesOfOne = 8;
 constexpr uint32_t kGroups = 256;     // workgroups: one a CU, and as many waves in it as its registers hold
 template <int D> constexpr int kWaves = D == 256 ? 4 : 8;

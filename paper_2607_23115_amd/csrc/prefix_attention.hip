@@ -56,8 +56,8 @@ constexpr uint32_t kMostJoins = 2048;  // workgroups of the others: those that t
 constexpr uint32_t kUnits = 256;
 // Of trees of drafts, where chunks stay long: two a CU, so that one's products go on under the other's softmax, and
 // some fewer than the CUs hold, as items are cut into whole chunks (4 sequences of 17 to 48 drafts of 28 heads on 4
-// behind 60,000 keys: 288 us with 256, 260 with 512, of which 16 had to wait, 220 with 480; 3 of 30 behind 8,000 to
-// 20,000, whose chunks would be of 10 steps, 43 and 62).
+// behind 60,000 keys: 256 us with 256; with 512 the rounding made 528, of which 16 had to wait, 260 where 480, of
+// which it makes 504, took 220 then and take 188 now). Which batches gain: at kLongChunk.
 constexpr uint32_t kTreeUnits = 480;
 
 struct Item {
