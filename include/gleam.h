@@ -796,7 +796,7 @@ gleam_status gleam_kv_accept(const gleam_kv_pages* kv, const gleam_accept* a, vo
  * bits. A row whose lse is +infinity adds nothing. For the new tokens' keys born = d_positions of the
  * token. What is not an own key of a sequence is left as it is, a shared prefix too: no sequence may drop
  * its keys by itself. Only the cache's keys are read (d_v may be d_k). A page in two places of the table
- * gets either's weights.
+ * gets either's weights, or (where d_weights_out is d_weights) one's added to the other's.
  *   q                as gleam_prefix_attention's; d_q_first as gleam_draft_tree's
  *   d_lse            float[n_tokens][q_heads]
  *   d_weights_out    may be d_weights itself, and must not overlap it otherwise
