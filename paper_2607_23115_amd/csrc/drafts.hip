@@ -46,6 +46,7 @@ gleam_status validate_len_out(const int32_t* d_len_out, uint64_t n_seq, const Re
   const uintptr_t to = reinterpret_cast<uintptr_t>(d_len_out);
   for (int i = 0; i < n_reads; ++i) {
     const uintptr_t from = reinterpret_cast<uintptr_t>(reads[i].p);
+    if (reads[i].bytes == 0) continue;
     if (from < to ? to - from < reads[i].bytes : from - to < 4 * n_seq) {
       set_error("%s: len_out must not overlap %s", who, reads[i].name);
       return GLEAM_E_INVALID;

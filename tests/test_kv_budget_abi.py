@@ -153,6 +153,12 @@ def test_a_budgets_length_written_over_what_is_read(name):
         assert name.encode() in g.lib.gleam_last_error() and b"overlap" in g.lib.gleam_last_error()
 
 
+def test_what_is_empty_does_not_overlap():
+    """A table without pages at the lengths' address: the call goes on to the next thing that it checks."""
+    assert evict(own_width=0, own_pages=512, ws=None) == g.E_INVALID
+    assert b"workspace" in g.lib.gleam_last_error()
+
+
 def test_eviction_workspaces_and_limits():
     assert evict(kv(v_stride=(2048, 128, 0))) == g.E_INVALID
     assert b"overlap" in g.lib.gleam_last_error()
